@@ -384,6 +384,139 @@ kda_status kda_recurrent_steps(const kda_dims *dims, const kda_prologue *prologu
 kda_status kda_clear_unowned_rows(const int32_t *cu_seqlens, int32_t num_seqs, int64_t tokens, int32_t num_arrays,
                                   void *const *arrays, const size_t *row_bytes, void *hip_stream);
 
+/*
+ * ---- Softmax attention: the other layers of a hybrid stack ----
+ *
+ * The paper's model interleaves KDA with layers of softmax attention (Section 4, "Hybrid model architecture").  These entry points
+ * compute them: causal attention with grouped heads over fixed or packed batches, forward and backward, for local layers with a
+ * sliding window and a few first tokens (sinks) that stay visible; and its serving form over a paged cache held in 8 bits
+ * (kda_cache_append, kda_cache_attn).
+ *
+ * Query i of a sequence sees key j of it when  j <= i  and  (window == 0  or  i - j < window  or  j < sinks).
+ * heads_q is a multiple of heads_kv; query head h reads key head h / (heads_q / heads_kv).
+ */
+typedef struct {
+    int32_t   batch;       /* B                                                                        */
+    int64_t   seqlen;      /* T per batch row, or total packed tokens (as in kda_dims)                  */
+    int32_t   heads_q, heads_kv;
+    int32_t   dim;         /* head dimension of q, k and v: 64 or 128                                   */
+    int32_t   num_seqs;    /* N: == batch, or the sequences of a packed batch                           */
+    kda_dtype in_dtype;    /* KDA_BF16                                                                  */
+    kda_dtype out_dtype;   /* dtype of o (kda_window_attn_bwd: KDA_BF16)                                */
+    float     scale;       /* multiplies q . k; in [1e-30, 1e30], usually dim^-0.5                      */
+    int64_t   window;      /* visible tokens before a query, itself included; 0: all                    */
+    int32_t   sinks;       /* first tokens of a sequence visible beyond the window, 0..64               */
+    int64_t   q_stride, k_stride, v_stride;    /* elements from a token to the next: 0 = contiguous     */
+                           /* (heads x dim), else at least that, a multiple of 8, at most 2^24          */
+                           /* (q, k and v may be slices of one projection's output)                     */
+} kda_attn_dims;
+
+/*
+ *   q          [B,T,heads_q,dim]   k, v [B,T,heads_kv,dim]    bf16, 16-byte aligned
+ *   cu_seqlens [N+1]               int32, device memory, as for kda_chunk_fwd, or NULL
+ *   o          [B,T,heads_q,dim]   out_dtype; rows of tokens owned by no sequence are left untouched
+ *   lse        [B,heads_q,T]       fp32: log sum_j exp(scale q_i . k_j) over the keys that i sees, or NULL
+ * Products on the bf16 matrix cores with fp32 accumulation, softmax statistics in fp32, its terms rounded to bf16 ahead of the
+ * product with v.  Values that are not finite reach the outputs of the queries that see them and no others: a query that sees a
+ * value of v that is not finite gets NaN or an infinity there, in every channel concerned, one that sees a key that is not
+ * finite, or is not finite itself, NaN.  (Such a tile is worked through twice.)  No workspace.
+ */
+kda_status kda_window_attn_fwd(const kda_attn_dims *dims, const void *q, const void *k, const void *v, const int32_t *cu_seqlens,
+                               void *o, float *lse, void *hip_stream);
+
+/*
+ * Gradients of sum(o . d_o) with respect to q, k and v.
+ *   o, lse     what kda_window_attn_fwd gave for the same dims and inputs, o in bf16
+ *   d_o        [B,T,heads_q,dim]   bf16
+ *   dq         [B,T,heads_q,dim]   dk, dv [B,T,heads_kv,dim]    bf16, contiguous, written; rows of tokens owned by no sequence are
+ *                                  left untouched.  No gradient may alias an input or another gradient.
+ *   workspace                      at least kda_window_attn_bwd_workspace_size(dims) bytes, 256-byte aligned
+ * Sums in fp32 in an order that depends on the sizes alone (no atomics: the same call gives the same bits); the softmax's terms and
+ * their gradients are rounded to bf16 ahead of the products, and each gradient once when it is stored.  What is not finite
+ * reaches the gradients that depend on it and no others.
+ */
+size_t kda_window_attn_bwd_workspace_size(const kda_attn_dims *dims);
+kda_status kda_window_attn_bwd(const kda_attn_dims *dims, const void *q, const void *k, const void *v, const int32_t *cu_seqlens,
+                               const void *o, const float *lse, const void *d_o, void *dq, void *dk, void *dv,
+                               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * ---- The serving form: a paged cache of keys and values held in 8 bits ----
+ *
+ * Keys and values of heads_kv heads stand in pages of page_size tokens as e4m3 codes (OCP: no infinities, 448 the largest), with one
+ * fp32 scale for each page and head: value = code * scale.
+ *   k, v           [num_pages,heads_kv,page_size,dim]   codes, 16-byte aligned
+ *   k_scale, v_scale [num_pages,heads_kv]               fp32
+ *   block_table    [num_seqs,max_pages]   int32: token t of sequence n stands in page block_table[n][t / page_size], at t % page_size.
+ *                                         An entry outside [0, num_pages) is no page: what would be appended there is dropped, and
+ *                                         its tokens are not visible.  Sequences may share pages that they only read.
+ *   kv_lens        [num_seqs]             int32: see the calls
+ */
+typedef struct {
+    int32_t  num_seqs;
+    int32_t  heads_q, heads_kv;    /* heads_q a multiple of heads_kv                                          */
+    int32_t  dim;                  /* 64 or 128                                                               */
+    int32_t  page_size;            /* 16, 32, 64 or 128                                                       */
+    int64_t  num_pages;
+    int32_t  max_pages;            /* columns of block_table; max_pages * page_size below 2^31                */
+    void    *k, *v;
+    float   *k_scale, *v_scale;
+    const int32_t *block_table, *kv_lens;
+} kda_cache;
+
+/*
+ * Position rotation: channel pair i of a token at position p turns by the angle p * inv_freq[i].  Pairs are (i, i + num_freqs)
+ * or, interleaved, (2 i, 2 i + 1); channels from 2 * num_freqs on stay as they are.
+ */
+typedef struct {
+    const float *inv_freq;         /* [num_freqs] fp32, device memory                                         */
+    int32_t      num_freqs;        /* a multiple of 8, at most dim / 2                                        */
+    int32_t      interleaved;
+} kda_rope;
+
+/*
+ * Appends new tokens to the cache: sequence n holds kv_lens[n] tokens before the call (a negative entry skips the sequence), and its
+ * new ones take the positions from there on.  kv_lens is not changed: the caller adds to it.
+ *   seqlen, cu_seqlens   tokens of each sequence, or with cu_seqlens [num_seqs+1] (as for kda_chunk_fwd) all of a packed batch's
+ *   k, v           [..,heads_kv,dim]   bf16, [num_seqs,seqlen] or packed rows; strides in elements from a token to the next as in kda_attn_dims
+ *   rope           rotation of k (and q), or NULL: as they are
+ *   k_out          [..,heads_kv,dim]   bf16: the rotated keys, for a prefill that follows, or NULL
+ *   q, q_out       [..,heads_q,dim]    bf16: queries to be rotated at their tokens' positions, and where to; NULL both or neither
+ * Scales: powers of two.  A page and head's scale is the smallest (2^-100 at least) with which its largest new value is at most 448 codes'
+ * steps, or the one it has, if that is larger and the page holds older tokens; where it grows, the older tokens' codes are rounded again
+ * to the new scale.  Codes are rounded to nearest even from the fp32 rotation; values that are not finite are stored as NaN and leave the
+ * scale alone.  Rows of k_out and q_out of skipped sequences and of tokens owned by none are left untouched, as is whatever stands in a
+ * page behind the sequence's last token.  A page that is appended to must belong to one sequence.
+ */
+kda_status kda_cache_append(const kda_cache *cache, int64_t seqlen, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
+                            const int32_t *cu_seqlens, const kda_rope *rope, void *k_out, const void *q, int64_t q_stride, void *q_out,
+                            void *hip_stream);
+
+/* A call of kda_cache_attn. */
+typedef struct {
+    int32_t   tokens;              /* new tokens of every sequence: 0..8                                      */
+    int64_t   q_stride;            /* elements from a token of q to the next, as in kda_attn_dims             */
+    int64_t   window;              /* as in kda_attn_dims                                                     */
+    int32_t   sinks;               /* 0..64                                                                   */
+    float     scale;               /* in [1e-30, 1e30]                                                        */
+    int64_t   max_kv_len;          /* upper bound of kv_lens, 0 = unknown (max_pages * page_size): it sets how */
+                                   /* far the keys are split, and is not needed for correctness               */
+    kda_dtype out_dtype;
+} kda_cache_query;
+
+/*
+ * Attention of each sequence's newest tokens over the cache: kv_lens[n] counts the tokens it holds, the new ones (appended before) among
+ * them, so that new token t stands at position kv_lens[n] - tokens + t and sees what it sees of kda_window_attn_fwd.  A token that sees
+ * nothing (kv_lens[n] <= 0, a position below zero: a batch of sequences with fewer new tokens is padded in front) gets zeros.
+ *   q [num_seqs,tokens,heads_q,dim] bf16      o [num_seqs,tokens,heads_q,dim] out_dtype
+ *   workspace   at least kda_cache_attn_workspace_size bytes (0 for some calls), 256-byte aligned
+ * Scales may be any finite numbers here.  What is not finite reaches the rows that see it and no others, whatever stands behind the
+ * last token of a page.
+ */
+size_t kda_cache_attn_workspace_size(const kda_cache *cache, const kda_cache_query *query);
+kda_status kda_cache_attn(const kda_cache *cache, const kda_cache_query *query, const void *q, void *o, void *workspace,
+                          size_t workspace_bytes, void *hip_stream);
+
 /* Static description of a status code (never NULL). */
 const char *kda_status_string(kda_status status);
 

@@ -12,3 +12,5 @@ from .kda import (KdaDims, KdaError, KdaEpilogue, KdaPrologue, kda_chunk_fwd, kd
                   kda_chunk_fwd_scalar_gate, kda_recurrent_steps_pooled_scalar_gate, kda_chunk_bwd,
                   kda_chunk_bwd_workspace_size, kda_chunk_fwd_static_scratch, kda_static_scratch_size,
                   kda_status_string, kda_version, library_path, load_library)
+from .attn import (KdaAttnDims, KdaCache, KdaCacheQuery, KdaRope, kda_cache_append, kda_cache_attn, kda_window_attn_bwd,  # noqa: F401
+                   kda_window_attn_bwd_workspace_size, kda_window_attn_fwd)

@@ -1,0 +1,178 @@
+// Softmax attention, forward: o_i = sum_j exp(x_ij - lse_i) v_j over the keys j that query i sees, x_ij = scale q_i . k_j.
+//
+// One pass over the keys with a running maximum m and sum l per query: a tile of 64 keys gives X^T = K Q^T, P^T = 2^(X^T c - m)
+// (c = scale log2 e, fp32) and O^T = O^T 2^(m_old - m) + V^T P^T, P rounded to bf16 (2^-9 a term, the operand type of the
+// matrix cores; l sums the unrounded values).  m is moved only when a maximum passes it by more than 8, i.e. terms grow to 2^8 at most,
+// which costs no precision and leaves most tiles without the 64 multiplications of O.
+#include <type_traits>
+
+#include "kda_attn_tile.h"
+
+namespace kda {
+namespace attn {
+
+template <int D, bool kOutBf16>
+__global__ __launch_bounds__(kThreads, 2) void kda_attn_fwd_kernel(const Shape s, const uint16_t *q, const uint16_t *k, const uint16_t *v,
+                                                                  void *o, float *lse)
+{
+    extern __shared__ __align__(16) uint8_t lds_raw[];
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds_raw;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, x = lane & 31, h = lane >> 5;
+    uint32_t slot, kv, sub;
+    split_block(blockIdx.x, s.heads_kv, s.group, slot, kv, sub);
+    const int head = kv * s.group + sub;
+    const Place at = place_of(s, s.slots - 1 - slot);
+    if (at.first >= at.len || at.first < 0) return;
+
+    const int64_t wq0 = at.first + 32 * wave;                            // the wave's first query
+    const int64_t query = wq0 + x, last = at.first + kCols - 1 < at.len - 1 ? at.first + kCols - 1 : at.len - 1;
+    const int64_t wlast = wq0 > last ? -1 : wq0 + 31 < last ? wq0 + 31 : last;            // -1: the wave has no query
+
+    // Q, B operand: 8 channels 16 s + 8 h .. of the lane's query (a query behind the last reads the last one's)
+    bf16x8 qf[D / 16];
+    {
+        const uint16_t *row = q + (at.row0 + (query < at.len ? query : at.len - 1)) * s.q_stride + (int64_t)head * D + 8 * h;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(row + 16 * i));
+    }
+    TileReader<D> rd;
+    rd.init(lane);
+    TileLoader<D> lk, lv;
+    lk.init(wave, lane, s.k_stride * 2);
+    lv.init(wave, lane, s.v_stride * 2);
+    const uint16_t *kh = k + at.row0 * s.k_stride + (int64_t)kv * D, *vh = v + at.row0 * s.v_stride + (int64_t)kv * D;
+    constexpr uint32_t kT = kTileBytes<D>;
+
+    // tiles: that of the sinks, if the window begins behind it, then from the window's first to the last query's
+    const int64_t low = s.window && at.first >= s.window ? (at.first - s.window + 1) / kTile : 0, high = last / kTile;
+    const bool sink_first = s.sinks > 0 && low > 0;
+    const int64_t steps = high - low + 1 + (sink_first ? 1 : 0);
+    const float c = s.scale * kLog2e;
+
+    auto tile_of = [&](int64_t it) { return sink_first ? (it == 0 ? 0 : low + it - 1) : low + it; };
+    auto issue = [&](int64_t it) {
+        const int64_t k0 = tile_of(it) * kTile;
+        const uint32_t buf = lds + (uint32_t)(it & 1) * 2 * kT;
+        lk.issue(buf, wave, rows_descriptor(kh + k0 * s.k_stride, at.len - k0, s.k_stride * 2));
+        lv.issue(buf + kT, wave, rows_descriptor(vh + k0 * s.v_stride, at.len - k0, s.v_stride * 2));
+    };
+
+    f32x16 acc[D / 32];
+    float m, mref, l;
+    auto walk = [&](auto careful) {
+        constexpr bool kCareful = decltype(careful)::value;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) acc[db] = zeros16();
+        m = -kInf;
+        mref = 0.f;
+        l = 0.f;
+        issue(0);
+        for (int64_t it = 0; it < steps; ++it) {
+            tile_barrier();
+            if (it + 1 < steps) issue(it + 1);
+            const int64_t k0 = tile_of(it) * kTile;
+            const uint32_t kt = lds + (uint32_t)(it & 1) * 2 * kT, vt = kt + kT;
+            // no query of the wave sees a key of the tile
+            if (k0 > wlast || (s.window && k0 + kTile - 1 <= wq0 - s.window && k0 >= s.sinks)) continue;
+            const bool edge = k0 + kTile - 1 > wq0 || (s.window && wq0 + 31 - k0 >= s.window);
+
+            f32x16 st[2] = {zeros16(), zeros16()};
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) st[b] = mfma(rd.rows(kt, b, i), qf[i], st[b]);
+
+            uint32_t seen = 0xffffffffu;
+            if (edge) seen = mask_tile(st, edges_of(query, k0, s.window, s.sinks), h);
+            float top = st[0][0];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) top = fmaxf(top, st[b][j]);
+            top = fmaxf(top, other_half(top));
+            top *= c;
+            if (__any(top > m + 8.f)) {
+                const float mn = fmaxf(m, top), f = mn == -kInf ? 1.f : fast_exp2(m - mn);
+                m = mn;
+                mref = mn == -kInf ? 0.f : mn;
+                l *= f;
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[db][j] *= f;
+            }
+            bf16x8 p[4];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                float e[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    e[j] = fast_exp2(fmaf(st[b][j], c, -mref));
+                    l += e[j];
+                }
+                p[2 * b] = pack8(e);
+                p[2 * b + 1] = pack8(e + 8);
+            }
+            if (kCareful && edge) {
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db) careful_product<D, 4>(acc[db], rd, vt, db, 0, p, seen);
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                    for (int db = 0; db < D / 32; ++db) acc[db] = mfma(rd.transposed(vt, db, ks), p[ks], acc[db]);
+            }
+        }
+    };
+    walk(std::false_type{});
+    if (repeat(acc, acc)) walk(std::true_type{});
+
+    l += other_half(l);
+    if (query >= at.len) return;
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : __builtin_nanf("");
+    const int64_t token = at.row0 + query;
+    if (lse && h == 0) lse[((int64_t)at.batch * s.heads_q + head) * s.tokens + token - (int64_t)at.batch * s.tokens] = l == 0.f ? -kInf : (mref + __log2f(l)) * 0.6931471805599453f;
+    const int64_t out = (token * s.heads_q + head) * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            float e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = acc[db][4 * b + j] * inv;
+            const int64_t w = out + 32 * db + 8 * b + 4 * h;
+            if constexpr (kOutBf16) {
+                const u32x2 y = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3])};
+                *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(o) + w) = y;
+            } else {
+                const f32x4 y = {e[0], e[1], e[2], e[3]};
+                *reinterpret_cast<f32x4 *>(static_cast<float *>(o) + w) = y;
+            }
+        }
+}
+
+}  // namespace attn
+}  // namespace kda
+
+using namespace kda;
+using namespace kda::attn;
+
+namespace kda {
+
+template <int D, bool kOutBf16>
+static hipError_t launch_fwd(const Shape &s, const void *q, const void *k, const void *v, void *o, float *lse, hipStream_t st)
+{
+    constexpr int kLds = 4 * kTileBytes<D>;                  // K and V of the tile in work and of the next
+    hipLaunchKernelGGL((kda_attn_fwd_kernel<D, kOutBf16>), dim3((uint32_t)s.slots * s.heads_q), dim3(kThreads), kLds, st, s,
+                       static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k), static_cast<const uint16_t *>(v), o, lse);
+    return hipGetLastError();
+}
+
+kda_status attn_fwd_dispatch(const Shape &s, int dim, bool out_bf16, const void *q, const void *k, const void *v, void *o, float *lse, hipStream_t st)
+{
+    const hipError_t e = dim == 128 ? (out_bf16 ? launch_fwd<128, true>(s, q, k, v, o, lse, st) : launch_fwd<128, false>(s, q, k, v, o, lse, st))
+                                    : (out_bf16 ? launch_fwd<64, true>(s, q, k, v, o, lse, st) : launch_fwd<64, false>(s, q, k, v, o, lse, st));
+    return e == hipSuccess ? KDA_OK : fail(KDA_ERR_LAUNCH, "kda_window_attn_fwd: %s", hipGetErrorString(e));
+}
+
+}  // namespace kda

@@ -1,0 +1,362 @@
+// Appending keys and values to a paged cache of e4m3 codes, with the position rotation of keys (and queries) on the way.
+//
+//     k'_t = R(p) k_t at position p = len + t: channel pairs (a, b) -> (a cos - b sin, a sin + b cos), angle p f_i
+//     s    = max(s_old, the smallest power of two with |x| <= 448 s for every new x of the page and head)
+//     code = e4m3(x / s), older codes of the page rounded again where s grew
+//
+// Scales are powers of two, so that a page that grows costs its older codes only the bits that fall below the smallest step, however
+// often it grows, and every cached value is a bf16 number.  Angles are formed as revolutions in 64 bits, p (f / 2 pi) less its nearest
+// whole number: at position 2^31 they are still good to 1e-6, where a product in 32 bits would be off by whole turns.
+//
+// A workgroup has one page of one sequence and head, keys or values: rows of 8-channel pieces in registers, one pass for the largest
+// value, one for the codes.  Further workgroups turn the queries, a token's angles once for several heads.
+#include "kda_cache.h"
+
+namespace kda {
+namespace cache {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ int64_t cu_at(const Append &a, int n)
+{
+    const int64_t v = a.cu[n];
+    return v < 0 ? 0 : v < a.tokens ? v : a.tokens;
+}
+
+// Which channels the 8-channel piece c of a row turns with, and by which frequencies (revolutions a position).
+struct Piece {
+    bool on, second, interleaved;    // it is rotated; it is the second half's
+    int shift;                       // lanes to the piece of the other half
+    int first;                       // its first frequency: interleaved four of them, else eight
+    __device__ __forceinline__ void init(const Append &a, int c)
+    {
+        interleaved = a.interleaved;
+        on = 8 * c < 2 * a.n_freq;
+        second = !interleaved && 8 * c >= a.n_freq;
+        shift = interleaved || !on ? 0 : (second ? -1 : 1) * (a.n_freq / 8);
+        first = interleaved ? 4 * c : 8 * c - (second ? a.n_freq : 0);
+    }
+    // revolutions of pair e at position pos, less the nearest whole number: exact to 2^-20 of a revolution at 2^31
+    __device__ __forceinline__ double turns(const Append &a, int e, int64_t pos) const
+    {
+        const double t = on ? (double)pos * ((double)a.inv_freq[first + e] * 0.15915494309189535) : 0.0;
+        return t - __builtin_rint(t);
+    }
+};
+// cos and sin of 2 pi r, |r| <= 1/2, in 64 bits: Taylor's series about the nearest quarter, 16 terms (2^-54 at pi / 4).
+struct Angle { double c, s; };
+__device__ __forceinline__ Angle angle64(double r)
+{
+    const double q = __builtin_rint(4.0 * r), x = (r - 0.25 * q) * 6.283185307179586, y = x * x;
+    double c = 4.779477332387385e-14, s = -7.647163731819816e-13;                            // 1/16!, -1/15!
+    c = fma(c, y, -1.1470745597729725e-11);
+    s = fma(s, y, 1.6059043836821613e-10);
+    c = fma(c, y, 2.08767569878681e-09);
+    s = fma(s, y, -2.505210838544172e-08);
+    c = fma(c, y, -2.755731922398589e-07);
+    s = fma(s, y, 2.7557319223985893e-06);
+    c = fma(c, y, 2.48015873015873e-05);
+    s = fma(s, y, -0.0001984126984126984);
+    c = fma(c, y, -0.001388888888888889);
+    s = fma(s, y, 0.008333333333333333);
+    c = fma(c, y, 0.041666666666666664);
+    s = fma(s, y, -0.16666666666666666);
+    c = fma(c, y, -0.5);
+    s = fma(s * y, x, x);
+    c = fma(c, y, 1.0);
+    const int k = (int)q & 3;
+    const double cc = k & 1 ? s : c, ss = k & 1 ? c : s;
+    return {k == 1 || k == 2 ? -cc : cc, k & 2 ? -ss : ss};
+}
+__device__ __forceinline__ Angle operator*(const Angle &a, const Angle &b) { return {fma(a.c, b.c, -a.s * b.s), fma(a.c, b.s, a.s * b.c)}; }
+
+__device__ __forceinline__ void unpack8(const u32x4 &w, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack_bf16x2(w[i], x[2 * i], x[2 * i + 1]);
+}
+// The other half's piece, from the lane that has it.  (Every lane takes part.)
+__device__ __forceinline__ u32x4 partner(const u32x4 &w, int shift)
+{
+    u32x4 o;
+    const int from = ((int)(threadIdx.x & 63) + shift) * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_ds_bpermute(from, w[i]);
+    return o;
+}
+// The piece turned by the angles of its pairs, in T and rounded once to fp32.
+template <typename T>
+__device__ __forceinline__ void turn(const Piece &t, const T (&cs)[8], const T (&sn)[8], const u32x4 &w, float (&x)[8])
+{
+    unpack8(w, x);
+    if (t.interleaved) {
+        if (!t.on) return;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const T a = x[e], b = x[e + 1];
+            x[e] = (float)(a * cs[e / 2] - b * sn[e / 2]);
+            x[e + 1] = (float)(a * sn[e / 2] + b * cs[e / 2]);
+        }
+    } else {
+        float y[8];
+        unpack8(partner(w, t.shift), y);
+        if (!t.on) return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const T own = (T)x[e] * cs[e], other = (T)y[e] * sn[e];
+            x[e] = (float)(t.second ? own + other : own - other);
+        }
+    }
+}
+__device__ __forceinline__ u32x4 pack8(const float (&x)[8])
+{
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+    return w;
+}
+// e4m3 codes of eight values, round to nearest even; what is not finite becomes NaN.
+__device__ __forceinline__ u32x2 codes8(const float (&x)[8], float inv)
+{
+    u32x2 w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int r = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * inv, x[4 * i + 1] * inv, 0, false);
+        w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * inv, x[4 * i + 3] * inv, r, true);
+    }
+    return w;
+}
+// The smallest power of two s >= 2^-100 with top <= 448 s (448 = 1.75 * 2^8); top is finite.
+__device__ __forceinline__ float scale_for(float top)
+{
+    const uint32_t b = __float_as_uint(top);
+    int e = (int)(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
+    e = e < 27 ? 27 : e;
+    return __uint_as_float((uint32_t)e << 23);
+}
+
+template <int D, int kThreads, int kIters>
+__global__ __launch_bounds__(kThreads) void kda_cache_append_kernel(const Cache c, const Append a)
+{
+    constexpr int kPieces = D / 8, kRows = kThreads / kPieces;           // pieces of a row, rows at a time
+    const int tid = threadIdx.x, piece = tid % kPieces, row0 = tid / kPieces;
+    if ((int)blockIdx.x >= a.page_blocks) {
+        // ---- queries: a token's angles, then its heads ----
+        const int parts = (c.heads_q + a.q_heads - 1) / a.q_heads;
+        const int64_t item = ((int64_t)blockIdx.x - a.page_blocks) * kRows + row0;
+        const int64_t token = item / parts;
+        const int h0 = (int)(item - token * parts) * a.q_heads;
+        int64_t pos = -1;
+        if (token < a.tokens) {
+            if (a.slots_per_seq) {
+                const int n = (int)(token / a.per_seq);
+                const int64_t len = c.lens[n];
+                if (len >= 0) pos = len + token - n * a.per_seq;
+            } else if (token >= cu_at(a, 0) && token < cu_at(a, c.num_seqs)) {
+                int lo = 0, hi = c.num_seqs - 1;
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (cu_at(a, mid) <= token) lo = mid; else hi = mid - 1;
+                }
+                const int64_t len = c.lens[lo];
+                if (len >= 0) pos = len + token - cu_at(a, lo);
+            }
+        }
+        Piece t;
+        t.init(a, piece);
+        float cs[8], sn[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float r = (float)t.turns(a, t.interleaved ? e & 3 : e, pos);
+            cs[e] = __builtin_amdgcn_cosf(r);                // (of 2 pi r)
+            sn[e] = __builtin_amdgcn_sinf(r);
+        }
+        const bool in = pos >= 0;
+        const uint16_t *from = a.q + (in ? token : 0) * a.q_stride + 8 * piece;
+        uint16_t *to = a.q_out + (in ? token : 0) * (int64_t)c.heads_q * D + 8 * piece;
+        // (no lane leaves early: the pieces of a row exchange their halves)
+        const int last = c.heads_q - 1;
+        for (int h = h0; h < h0 + a.q_heads; h += 4) {
+            u32x4 w[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (u < a.q_heads) w[u] = *reinterpret_cast<const u32x4 *>(from + (int64_t)(h + u < last ? h + u : last) * D);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (u >= a.q_heads) break;                   // (the same for every lane)
+                float x[8];
+                turn(t, cs, sn, w[u], x);
+                if (in && h + u <= last) *reinterpret_cast<u32x4 *>(to + (int64_t)(h + u) * D) = pack8(x);
+            }
+        }
+        return;
+    }
+
+    // ---- one page of one sequence and head ----
+    const bool values = blockIdx.x & 1;
+    const int head = (int)((blockIdx.x >> 1) % c.heads_kv), slot = (int)((blockIdx.x >> 1) / c.heads_kv);
+    int n, index;
+    int64_t first_row, count;                                // of the sequence's new tokens
+    if (a.slots_per_seq) {
+        n = slot / a.slots_per_seq;
+        index = slot - n * a.slots_per_seq;
+        first_row = n * a.per_seq;
+        count = a.per_seq;
+    } else {
+        // slots from cu[n] / page_size + 2 n on are sequence n's: at least as many as the pages it can touch
+        int lo = 0, hi = c.num_seqs - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if ((cu_at(a, mid) >> c.page_log2) + 2 * mid <= slot) lo = mid; else hi = mid - 1;
+        }
+        n = lo;
+        first_row = cu_at(a, n);
+        count = cu_at(a, n + 1) - first_row;
+        index = slot - (int)((first_row >> c.page_log2) + 2 * n);
+    }
+    const int64_t len = c.lens[n];
+    if (len < 0 || count <= 0 || index < 0) return;
+    const int64_t logical = (len >> c.page_log2) + index, page0 = logical << c.page_log2;
+    const int64_t begin = page0 > len ? page0 : len, end = page0 + c.page_size < len + count ? page0 + c.page_size : len + count;
+    if (begin >= end) return;
+    const int rows = (int)(end - begin), older = (int)(begin - page0);
+    const int32_t page = page_at(c, n, logical);
+    if (page < 0 && (values || !a.k_out)) return;
+
+    // (the rows' new tokens, 16 bytes a lane)
+    const int64_t row = first_row + begin - len;
+    const uint16_t *from = values ? a.v + row * a.v_stride : a.k + row * a.k_stride;
+    const int64_t stride = values ? a.v_stride : a.k_stride;
+    u32x4 w[kIters];
+#pragma unroll
+    for (int i = 0; i < kIters; ++i) {
+        const int r = i * kRows + row0;
+        w[i] = u32x4{0, 0, 0, 0};
+        if (r < rows) w[i] = *reinterpret_cast<const u32x4 *>(from + r * stride + (int64_t)head * D + 8 * piece);
+    }
+    float *scale_at = (values ? c.v_scale : c.k_scale) + (int64_t)page * c.heads_kv + head;
+    const float scale_old = page >= 0 && older ? *scale_at : 0.f;
+    float x[kIters][8], top = 0.f;
+    if (!values && a.n_freq) {
+        // Angles in 64 bits, so that the codes are those of the exact rotation (in 32 bits one in 2^21 was another): computed for the first
+        // row and for the distance to the next, then multiplied, 4 operations a pair instead of 30.
+        Piece t;
+        t.init(a, piece);
+        double cs[8], sn[8];
+        Angle next[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int f = t.interleaved ? e & 3 : e;
+            const Angle z = angle64(t.turns(a, f, begin + row0));
+            cs[e] = z.c;
+            sn[e] = z.s;
+            if (kIters > 1) next[e] = angle64(t.turns(a, f, kRows));
+        }
+#pragma unroll
+        for (int i = 0; i < kIters; ++i) {
+            if (i * kRows >= rows) break;                    // (the same for every lane)
+            const int r = i * kRows + row0;
+            turn(t, cs, sn, w[i], x[i]);
+            if (a.k_out && r < rows) *reinterpret_cast<u32x4 *>(a.k_out + ((row + r) * c.heads_kv + head) * D + 8 * piece) = pack8(x[i]);
+            if (i + 1 < kIters) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const Angle z = Angle{cs[e], sn[e]} * next[e];
+                    cs[e] = z.c;
+                    sn[e] = z.s;
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kIters; ++i) {
+            if (i * kRows >= rows) break;
+            const int r = i * kRows + row0;
+            unpack8(w[i], x[i]);
+            if (!values && a.k_out && r < rows) *reinterpret_cast<u32x4 *>(a.k_out + ((row + r) * c.heads_kv + head) * D + 8 * piece) = w[i];
+        }
+    }
+    if (page < 0) return;
+#pragma unroll
+    for (int i = 0; i < kIters; ++i) {
+        if (i * kRows >= rows) break;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float y = fabsf(x[i][e]);
+            top = fmaxf(top, y < __builtin_huge_valf() ? y : 0.f);
+        }
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if constexpr (kThreads > 64) {
+        __shared__ float tops[kThreads / 64];
+        if ((tid & 63) == 0) tops[tid >> 6] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kThreads / 64; ++i) top = fmaxf(top, tops[i]);
+    }
+    const float scale = fmaxf(scale_old, scale_for(top)), inv = 1.f / scale;
+    uint8_t *codes = (values ? c.v : c.k) + ((int64_t)page * c.heads_kv + head) * c.page_size * D + 8 * piece;
+    if (scale > scale_old && older) {
+        const float again = scale_old * inv;
+        for (int r = row0; r < older; r += kRows) {
+            u32x2 *at = reinterpret_cast<u32x2 *>(codes + r * D);
+            const u32x2 y = *at;
+            float z[8];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], true);
+                z[4 * i] = lo[0];
+                z[4 * i + 1] = lo[1];
+                z[4 * i + 2] = hi[0];
+                z[4 * i + 3] = hi[1];
+            }
+            *at = codes8(z, again);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kIters; ++i) {
+        const int r = i * kRows + row0;
+        if (i * kRows >= rows) break;
+        if (r < rows) *reinterpret_cast<u32x2 *>(codes + (int64_t)(older + r) * D) = codes8(x[i], inv);
+    }
+    if (tid == 0) *scale_at = scale;
+}
+
+}  // namespace cache
+
+using namespace cache;
+
+template <int D, int kThreads, int kIters>
+static hipError_t launch_append(const Cache &c, Append a, hipStream_t st)
+{
+    constexpr int kRows = kThreads / (D / 8);
+    int64_t q_blocks = 0;
+    if (a.q) {
+        // several heads a thread share its angles once there are threads enough: 2^17 of them
+        a.q_heads = 1;
+        while (a.q_heads < 8 && a.tokens * c.heads_q * (D / 8) / a.q_heads > 1 << 17) a.q_heads *= 2;
+        const int64_t items = a.tokens * ((c.heads_q + a.q_heads - 1) / a.q_heads);
+        q_blocks = (items + kRows - 1) / kRows;
+    }
+    a.page_blocks = a.slots * c.heads_kv * 2;
+    if (a.page_blocks + q_blocks == 0) return hipSuccess;
+    hipLaunchKernelGGL((kda_cache_append_kernel<D, kThreads, kIters>), dim3((uint32_t)(a.page_blocks + q_blocks)), dim3(kThreads), 0, st, c, a);
+    return hipGetLastError();
+}
+
+kda_status cache_append_dispatch(const Cache &c, const Append &a, int dim, hipStream_t st)
+{
+    // up to 8 new tokens a sequence: a wave has them all; else a page's rows by 16 (d 128) or 32
+    const bool few = a.slots_per_seq && a.per_seq <= 8;
+    hipError_t e;
+    if (dim == 128)
+        e = few ? launch_append<128, 64, 2>(c, a, st) : c.page_size == 128 ? launch_append<128, 256, 8>(c, a, st)
+                : c.page_size == 64 ? launch_append<128, 256, 4>(c, a, st) : launch_append<128, 256, 2>(c, a, st);
+    else
+        e = few ? launch_append<64, 64, 1>(c, a, st) : c.page_size == 128 ? launch_append<64, 256, 4>(c, a, st) : launch_append<64, 256, 2>(c, a, st);
+    return e == hipSuccess ? KDA_OK : fail(KDA_ERR_LAUNCH, "kda_cache_append: %s", hipGetErrorString(e));
+}
+
+}  // namespace kda

@@ -124,6 +124,19 @@ def load_library():
     lib.kda_recurrent_steps_fused.argtypes = [dp, pp, ep, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.kda_recurrent_steps.restype = ctypes.c_int
     lib.kda_recurrent_steps.argtypes = [dp, pp, ep, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_uint32, vp]
+    lib.kda_window_attn_fwd.restype = ctypes.c_int
+    lib.kda_window_attn_fwd.argtypes = [vp] * 8
+    lib.kda_window_attn_bwd_workspace_size.restype = sz
+    lib.kda_window_attn_bwd_workspace_size.argtypes = [vp]
+    lib.kda_window_attn_bwd.restype = ctypes.c_int
+    lib.kda_window_attn_bwd.argtypes = [vp] * 12 + [sz, vp]
+    i64 = ctypes.c_int64
+    lib.kda_cache_append.restype = ctypes.c_int
+    lib.kda_cache_append.argtypes = [vp, i64, vp, vp, i64, i64, vp, vp, vp, vp, i64, vp, vp]
+    lib.kda_cache_attn_workspace_size.restype = sz
+    lib.kda_cache_attn_workspace_size.argtypes = [vp, vp]
+    lib.kda_cache_attn.restype = ctypes.c_int
+    lib.kda_cache_attn.argtypes = [vp, vp, vp, vp, vp, sz, vp]
     try:
         from . import _kda_host
         _kda_host.bind(*[ctypes.cast(f, vp).value for f in (lib.kda_recurrent_step, lib.kda_recurrent_steps)], _raw_stream)
