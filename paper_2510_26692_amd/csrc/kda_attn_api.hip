@@ -57,11 +57,12 @@ kda_status check(const kda_attn_dims *d, const int32_t *cu, attn::Shape &s)
     s.scale = d->scale;
     s.cu = cu;
     // a window that no two tokens are apart by is none
-    s.window = d->window >= d->seqlen ? 0 : d->window;
+    s.window = d->window >= d->seqlen ? 0 : (int32_t)d->window;
     if (s.window == 0) s.sinks = 0;
+    if (d->seqlen > 1 << 30) return fail(KDA_ERR_UNSUPPORTED, "more than 2^30 tokens of a row");
     const int64_t tiles = (d->seqlen + attn::kCols - 1) / attn::kCols;
     const int64_t slots = cu ? d->seqlen / attn::kCols + d->num_seqs : tiles * d->batch;
-    if (tiles > 0x7fffffffLL || slots * (d->heads_q > 0 ? d->heads_q : 1) > 0x7fffffffLL)
+    if (slots * (d->heads_q > 0 ? d->heads_q : 1) > 0x7fffffffLL)
         return fail(KDA_ERR_UNSUPPORTED, "more than 2^31 tiles of %d tokens and heads", attn::kCols);
     s.slots = (int32_t)slots;
     s.tiles = cu ? 0 : (int32_t)tiles;

@@ -7,6 +7,8 @@
 // of every sum is fixed.  A key head's gradients sum over its group's query heads inside a workgroup; where that leaves too few
 // workgroups, over parts of the group, whose fp32 sums a last kernel adds.  The sinks' keys are seen by every later query: what lies beyond
 // their window is walked by workgroups of its own, in parts.
+#include <type_traits>
+
 #include "kda_attn_tile.h"
 
 namespace kda {
@@ -28,11 +30,10 @@ struct Back {
 // elements of one part of dK or dV
 __device__ __forceinline__ int64_t part_size(const Shape &s, int d) { return (s.cu ? s.tokens : s.tokens * s.num_seqs) * s.heads_kv * d; }
 __device__ __forceinline__ int64_t stats_size(const Shape &s) { return (s.cu ? s.tokens : s.tokens * s.num_seqs) * s.heads_q; }
-__device__ __forceinline__ int32_t clamp_key(int64_t v) { return v < -(1 << 20) ? -(1 << 20) : v > 1 << 20 ? 1 << 20 : (int32_t)v; }
 // tiles of 64 queries that the first key tile's own walk covers
-__device__ __forceinline__ int64_t first_walk_tiles(const Shape &s, int64_t len)
+__device__ __forceinline__ int first_walk_tiles(const Shape &s, int len)
 {
-    const int64_t all = (len + kTile - 1) / kTile, own = s.window ? (kCols + s.window - 2) / kTile + 1 : all;
+    const int all = (len + kTile - 1) / kTile, own = s.window ? (kCols + s.window - 2) / kTile + 1 : all;
     return own < all ? own : all;
 }
 
@@ -46,9 +47,9 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
     const Place at = place_of(s, s.slots - 1 - slot);
     if (at.first >= at.len || at.first < 0) return false;
 
-    const int64_t wq0 = at.first + 32 * wave;
-    const int64_t query = wq0 + x, last = at.first + kCols - 1 < at.len - 1 ? at.first + kCols - 1 : at.len - 1;
-    const int64_t wlast = wq0 > last ? -1 : wq0 + 31 < last ? wq0 + 31 : last;
+    const int wq0 = at.first + 32 * wave;
+    const int query = wq0 + x, last = min(at.first + kCols - 1, at.len - 1);
+    const int wlast = wq0 > last ? -1 : min(wq0 + 31, last);
     const int64_t token = at.row0 + (query < at.len ? query : at.len - 1), stat = ((int64_t)at.batch * (s.heads_q - 1) + head) * s.tokens + token;
 
     bf16x8 qf[D / 16], df[D / 16];
@@ -74,37 +75,44 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
     const float lse = g.lse[stat], lse2 = lse == -kInf ? kInf : lse * kLog2e;
     if (query < at.len) g.stats[stat + (h ? stats_size(s) : 0)] = h ? delta : lse2;
 
+    arrived(qf);
+    arrived(df);
     TileReader<D> rd;
     rd.init(lane);
     TileLoader<D> lk, lv;
-    lk.init(wave, lane, s.k_stride * 2);
-    lv.init(wave, lane, s.v_stride * 2);
+    const uint32_t ks_bytes = s.k_stride * 2, vs_bytes = s.v_stride * 2;
+    lk.init(wave, lane, ks_bytes);
+    lv.init(wave, lane, vs_bytes);
     const uint16_t *kh = g.k + at.row0 * s.k_stride + (int64_t)kv * D, *vh = g.v + at.row0 * s.v_stride + (int64_t)kv * D;
     constexpr uint32_t kT = kTileBytes<D>;
-    const int64_t low = s.window && at.first >= s.window ? (at.first - s.window + 1) / kTile : 0, high = last / kTile;
-    const bool sink_first = s.sinks > 0 && low > 0;
-    const int64_t steps = high - low + 1 + (sink_first ? 1 : 0);
+    const int low = s.window && at.first >= s.window ? (at.first - s.window + 1) / kTile : 0, high = last / kTile;
+    const int sink_first = s.sinks > 0 && low > 0, steps = high - low + 1 + sink_first;
     const float c = s.scale * kLog2e;
-    auto tile_of = [&](int64_t it) { return sink_first ? (it == 0 ? 0 : low + it - 1) : low + it; };
-    auto issue = [&](int64_t it) {
-        const int64_t k0 = tile_of(it) * kTile;
-        const uint32_t buf = lds + (uint32_t)(it & 1) * 2 * kT;
-        lk.issue(buf, wave, rows_descriptor(kh + k0 * s.k_stride, at.len - k0, s.k_stride * 2));
-        lv.issue(buf + kT, wave, rows_descriptor(vh + k0 * s.v_stride, at.len - k0, s.v_stride * 2));
+    auto first_key = [&](int it) { return (sink_first ? (it == 0 ? 0 : low + it - 1) : low + it) * kTile; };
+    auto issue = [&](int it, uint32_t buf) {
+        const int k0 = first_key(it);
+        lk.issue(lds + 2 * buf * kT, wave, rows_descriptor(kh + k0 * s.k_stride, at.len - k0, ks_bytes));
+        lv.issue(lds + (2 * buf + 1) * kT, wave, rows_descriptor(vh + k0 * s.v_stride, at.len - k0, vs_bytes));
     };
 
     f32x16 acc[D / 32];
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) acc[db] = zeros16();
-    issue(0);
-    for (int64_t it = 0; it < steps; ++it) {
+    issue(0, 0);
+    auto step = [&](int it, auto parity) {
+        constexpr int P = decltype(parity)::value;
         tile_barrier();
-        if (it + 1 < steps) issue(it + 1);
-        const int64_t k0 = tile_of(it) * kTile;
-        const uint32_t kt = lds + (uint32_t)(it & 1) * 2 * kT, vt = kt + kT;
-        if (k0 > wlast || (s.window && k0 + kTile - 1 <= wq0 - s.window && k0 >= s.sinks)) continue;
+        if (it + 1 < steps) issue(it + 1, P ^ 1);
+        const int k0 = first_key(it);
+        const uint32_t kt = lds + 2 * P * kT, vt = kt + kT;
+        if (k0 > wlast || (s.window && k0 + kTile - 1 <= wq0 - s.window && k0 >= s.sinks)) return;
         const bool edge = k0 + kTile - 1 > wq0 || (s.window && wq0 + 31 - k0 >= s.window);
-        const Edges ed = edges_of(query, k0, s.window, s.sinks);
+        Seen seen;
+        if (edge) {
+            seen = seen_keys(query, k0, s.window, s.sinks);
+            seen.w[0] >>= 4 * h;
+            seen.w[1] >>= 4 * h;
+        }
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             f32x16 st = zeros16(), dp = zeros16();
@@ -113,32 +121,32 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
                 st = mfma(rd.rows(kt, b, i), qf[i], st);
                 dp = mfma(rd.rows(vt, b, i), df[i], dp);
             }
+            reads_ahead<8, 1, D / 8, D / 8>();
             float e[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) e[j] = fast_exp2(fmaf(st[j], c, -lse2)) * (dp[j] - delta);
-            uint32_t seen = 0xffffu;
             if (edge) {
-                seen = 0;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const bool ok = sees(ed, 32 * b + 8 * (j >> 2) + 4 * h + (j & 3));
-                    e[j] = ok ? e[j] : 0.f;
-                    seen |= (ok ? 1u : 0u) << j;
-                }
+                for (int j = 0; j < 16; ++j) e[j] = where_seen(seen_bit(seen.w[b], j), e[j], 0.f);
             }
             const bf16x8 ds[2] = {pack8(e), pack8(e + 8)};
             if (kCareful && edge) {
 #pragma unroll
-                for (int db = 0; db < D / 32; ++db) careful_product<D, 2>(acc[db], rd, kt, db, 2 * b, ds, seen);
+                for (int db = 0; db < D / 32; ++db) careful_product<D, 2>(acc[db], rd, kt, db, 2 * b, ds, seen.w + b);
             } else {
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
                     for (int db = 0; db < D / 32; ++db) acc[db] = mfma(rd.transposed(kt, db, 2 * b + ks), ds[ks], acc[db]);
+                reads_ahead<8, 2, D / 8, D / 16>();
             }
         }
+    };
+    for (int it = 0; it < steps; it += 2) {
+        step(it, std::integral_constant<int, 0>{});
+        if (it + 1 < steps) step(it + 1, std::integral_constant<int, 1>{});
     }
-    if (!kCareful && repeat(acc, acc)) return true;
+    if (!kCareful && repeat(acc, acc, lds)) return true;
     if (query >= at.len) return false;
     uint16_t *out = g.dq + (token * s.heads_q + head) * D;
 #pragma unroll
@@ -159,7 +167,8 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void kda_attn_dq_kern
     if (dq_tile<D, false>(s, g, lds)) dq_tile_again<D>(s, g, lds);
 }
 
-// dK and dV of 128 keys (kSink: the sinks' part of the first 64, each half of the waves on every other tile of queries).
+// dK and dV of 128 keys, or (the first workgroups) the sinks' part of a sequence's first 64, each half of the waves on every other tile of
+// queries.
 //
 // At d 128 a wave's sums take 128 registers, K 32 and a block's X and dP 32 more: two waves a SIMD have no room for V, which is read from LDS
 // as the tiles are, and the tiles are of 32 queries, so that V, Q and dO of two workgroups fit a compute unit.
@@ -170,21 +179,23 @@ template <int D> struct DkvLayout {
     static constexpr uint32_t kV = 2 * kBuf;
     static constexpr uint32_t kBytes = kV + (kVInLds ? 2 * kTileBytes<D> : 0);
 };
-template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_tile(const Shape &s, const Back &g, const uint32_t lds)
+template <int D, bool kCareful> __device__ __forceinline__ bool dkv_tile(const Shape &s, const Back &g, const uint32_t lds)
 {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, x = lane & 31, h = lane >> 5;
     uint32_t slot, kv, sub;
-    split_block(blockIdx.x, s.heads_kv, g.splits, slot, kv, sub);
+    const uint32_t sink_blocks = (uint32_t)g.sink_slots * s.heads_kv * g.splits;
+    const bool sink = blockIdx.x < sink_blocks;
+    split_block(sink ? blockIdx.x : blockIdx.x - sink_blocks, s.heads_kv, g.splits, slot, kv, sub);
     const int heads = s.group / g.splits, head0 = kv * s.group + sub * heads;
     using L = DkvLayout<D>;
     constexpr int kRows = L::kRows;
     constexpr uint32_t kT = L::kT, kBuf = L::kBuf;
     Place at;
-    int64_t tile0, tiles;                                    // of queries
-    if constexpr (kSink) {
+    int tile0, tiles;                                        // of queries
+    if (sink) {
         int32_t part;
         if (g.sink_parts) {
-            at = {(int64_t)(slot / g.sink_parts) * s.tokens, s.tokens, 0, (int32_t)(slot / g.sink_parts)};
+            at = {(int64_t)(slot / g.sink_parts) * s.tokens, (int32_t)s.tokens, 0, (int32_t)(slot / g.sink_parts)};
             part = slot % g.sink_parts;
         } else {
             const int64_t per = (int64_t)kTile * g.sink_tiles;               // (slots as in place_of)
@@ -195,24 +206,23 @@ template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_
             }
             const int64_t a = cu_at(s, lo), e = cu_at(s, lo + 1), p = (int64_t)slot - (a / per + lo);
             if (p < 0) return false;
-            at = {a, e - a, 0, 0};
+            at = {a, (int32_t)(e - a), 0, 0};
             part = (int32_t)p;
         }
         if (at.len <= 0) return false;
-        const int64_t all = (at.len + kTile - 1) / kTile;
-        const int64_t from = first_walk_tiles(s, at.len) + (int64_t)part * g.sink_tiles, n = all - from < g.sink_tiles ? all - from : g.sink_tiles;
+        const int all = (at.len + kTile - 1) / kTile, from = first_walk_tiles(s, at.len) + part * g.sink_tiles, n = min(all - from, g.sink_tiles);
         if (n <= 0) return false;
         tile0 = from * kTile / kRows;
         tiles = n * kTile / kRows;
     } else {
         at = place_of(s, slot);
         if (at.first >= at.len || at.first < 0) return false;
-        const int64_t last = s.window && at.first + kCols + s.window - 2 < at.len - 1 ? at.first + kCols + s.window - 2 : at.len - 1;
+        const int last = s.window ? min(at.first + kCols + s.window - 2, at.len - 1) : at.len - 1;
         tile0 = at.first / kRows;
         tiles = last / kRows - tile0 + 1;
         if (at.first == 0 && s.sinks) tiles = first_walk_tiles(s, at.len) * (kTile / kRows);          // (the sinks' walks begin behind them)
     }
-    const int64_t kw0 = at.first + 32 * (kSink ? wave & 1 : wave), key = kw0 + x;
+    const int kw0 = at.first + 32 * (sink ? wave & 1 : wave), key = kw0 + x;
     const int64_t token = at.row0 + (key < at.len ? key : at.len - 1);
 
     bf16x8 kf[D / 16], vf[L::kVInLds ? 1 : D / 16];
@@ -229,11 +239,13 @@ template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_
         lv.init(wave, lane, s.v_stride * 2);
         const uint16_t *vh = g.v + (at.row0 + at.first) * s.v_stride + (int64_t)kv * D;
 #pragma unroll
-        for (int i = 0; i < (kSink ? 1 : 2); ++i)
+        for (int i = 0; i < 2; ++i)
             lv.issue(lds + L::kV + i * kTileBytes<D>, wave, rows_descriptor(vh + i * kTile * s.v_stride, at.len - at.first - i * kTile, s.v_stride * 2));
     }
     const uint32_t vt = lds + L::kV + ((kw0 - at.first) / kTile) * kTileBytes<D>;         // the wave's 32 rows of V: block vb of this tile
     const int vb = ((kw0 - at.first) / 32) & 1;
+    arrived(kf);
+    if constexpr (!L::kVInLds) arrived(vf);
     TileReader<D> rd;
     rd.init(lane);
     TileLoader<D, kRows> lq, ld;
@@ -241,14 +253,13 @@ template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_
     lq.init(wave, lane, s.q_stride * 2);
     ld.init(wave, lane, do_stride * 2);
     const float c = s.scale * kLog2e;
-    const int64_t steps = tiles * heads;
+    const int steps = tiles * heads;
 
-    int32_t issue_head = 0;
-    int64_t issue_tile = 0;                                  // the step to be issued next: (head, tile), tiles fastest
-    auto issue = [&](int64_t it) {
+    int issue_head = 0, issue_tile = 0;                                  // the step to be issued next: (head, tile), tiles fastest
+    auto issue = [&](uint32_t parity) {
         const int head = head0 + issue_head;
-        const int64_t q0 = (tile0 + issue_tile) * kRows, rows = at.len - q0;
-        const uint32_t buf = lds + (uint32_t)(it & 1) * kBuf;
+        const int q0 = (tile0 + issue_tile) * kRows, rows = at.len - q0;
+        const uint32_t buf = lds + parity * kBuf;
         lq.issue(buf, wave, rows_descriptor(g.q + (at.row0 + q0) * s.q_stride + (int64_t)head * D, rows, s.q_stride * 2));
         ld.issue(buf + kT, wave, rows_descriptor(g.d_o + (at.row0 + q0) * do_stride + (int64_t)head * D, rows, do_stride * 2));
         if (wave < 2) {                                      // lse, then d: 64 values each
@@ -262,20 +273,26 @@ template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) dk[db] = dv[db] = zeros16();
     issue(0);
-    int64_t tile = 0;
-    for (int64_t it = 0; it < steps; ++it) {
+    int tile = 0;
+    for (int it = 0; it < steps; ++it) {
         tile_barrier();
-        if (it + 1 < steps) issue(it + 1);
-        const int64_t q0 = (tile0 + tile) * kRows;
+        if (it + 1 < steps) issue((it + 1) & 1);
+        const int q0 = (tile0 + tile) * kRows;
         if (++tile == tiles) tile = 0;
         const uint32_t qt = lds + (uint32_t)(it & 1) * kBuf, dt = qt + kT, stats = qt + 2 * kT;
-        if (kSink && kRows == 32 && (int)(it & 1) != wave >> 1) continue;
+        if (sink && (int)(it & 1) != wave >> 1) continue;
         if (kw0 >= at.len || q0 + kRows - 1 < kw0 || (s.window && q0 - (kw0 + 31) >= s.window && kw0 >= s.sinks)) continue;
         const bool edge = q0 < kw0 + 31 || (s.window && q0 + kRows - 1 - kw0 >= s.window);
-        // the key is seen by the tile's queries first .. end
-        const int32_t first = clamp_key(kw0 - q0) + x, end = s.window && x >= clamp_key(s.sinks - kw0) ? clamp_key(kw0 + s.window - 1 - q0) + x : kTile;
+        // the key is seen by its own query and later ones, to the window's end
+        Seen seen;
+        if (edge) {
+            const int32_t last = s.window && key >= s.sinks ? key + s.window - 1 - q0 : kTile;
+            seen = seen_rows(key - q0, last);
+            seen.w[0] >>= 4 * h;
+            seen.w[1] >>= 4 * h;
+        }
 #pragma unroll
-        for (int b = kSink && kRows == 64 ? wave >> 1 : 0; b < (kSink && kRows == 64 ? (wave >> 1) + 1 : kRows / 32); ++b) {
+        for (int b = 0; b < kRows / 32; ++b) {
             if constexpr (D == 128) rd.forget();
             f32x16 st = zeros16(), dp = zeros16();
 #pragma unroll
@@ -285,7 +302,6 @@ template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_
                 if constexpr (L::kVInLds) dp = mfma(rd.rows(dt, b, i), rd.rows(vt, vb, i), dp);
                 else dp = mfma(rd.rows(dt, b, i), vf[i], dp);
             }
-            uint32_t seen = 0xffffu;
             bf16x8 pb[2], ds[2];
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
@@ -304,11 +320,9 @@ template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_
                 if (edge) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const int32_t row = 32 * b + 16 * ks + 8 * (j >> 2) + 4 * h + (j & 3);
-                        const bool ok = row >= first && row <= end;
-                        p[j] = ok ? p[j] : 0.f;
-                        e[j] = ok ? e[j] : 0.f;
-                        seen &= ok ? 0xffffu : ~(1u << (8 * ks + j));
+                        const uint32_t bit = seen_bit(seen.w[b], 8 * ks + j);
+                        p[j] = where_seen(bit, p[j], 0.f);
+                        e[j] = where_seen(bit, e[j], 0.f);
                     }
                 }
                 pb[ks] = pack8(p);
@@ -317,8 +331,8 @@ template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_
             if (kCareful && edge) {
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db) {
-                    careful_product<D, 2>(dv[db], rd, dt, db, 2 * b, pb, seen);
-                    careful_product<D, 2>(dk[db], rd, qt, db, 2 * b, ds, seen);
+                    careful_product<D, 2>(dv[db], rd, dt, db, 2 * b, pb, seen.w + b);
+                    careful_product<D, 2>(dk[db], rd, qt, db, 2 * b, ds, seen.w + b);
                 }
             } else {
 #pragma unroll
@@ -331,8 +345,8 @@ template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_
             }
         }
     }
-    if (!kCareful && repeat(dk, dv)) return true;
-    if (!kSink && key >= at.len) return false;
+    if (!kCareful && repeat(dk, dv, lds)) return true;
+    if (!sink && key >= at.len) return false;
     const int64_t row = (token * s.heads_kv + kv) * D;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
@@ -345,7 +359,7 @@ template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_
                 yk[j] = dk[db][4 * b + j] * s.scale;
                 yv[j] = dv[db][4 * b + j];
             }
-            if constexpr (kSink) {
+            if (sink) {
                 const int64_t w = ((((int64_t)slot * 2 + (wave >> 1)) * g.splits + sub) * s.heads_kv + kv) * kTile * D + (int64_t)key * D + ch;
                 *reinterpret_cast<f32x4 *>(g.sink_k + w) = yk;
                 *reinterpret_cast<f32x4 *>(g.sink_v + w) = yv;
@@ -361,15 +375,12 @@ template <int D, bool kSink, bool kCareful> __device__ __forceinline__ bool dkv_
         }
     return false;
 }
-template <int D, bool kSink> __device__ __noinline__ void dkv_tile_again(const Shape s, const Back g, const uint32_t lds)
-{
-    dkv_tile<D, kSink, true>(s, g, lds);
-}
-template <int D, bool kSink> __global__ __launch_bounds__(kThreads, 2) void kda_attn_dkv_kernel(const Shape s, const Back g)
+template <int D> __device__ __noinline__ void dkv_tile_again(const Shape s, const Back g, const uint32_t lds) { dkv_tile<D, true>(s, g, lds); }
+template <int D> __global__ __launch_bounds__(kThreads, 2) void kda_attn_dkv_kernel(const Shape s, const Back g)
 {
     extern __shared__ __align__(16) uint8_t lds_raw[];
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds_raw;
-    if (dkv_tile<D, kSink, false>(s, g, lds)) dkv_tile_again<D, kSink>(s, g, lds);
+    if (dkv_tile<D, false>(s, g, lds)) dkv_tile_again<D>(s, g, lds);
 }
 
 // Sums of the parts: a thread has four channels of a token and key head.
@@ -403,7 +414,7 @@ __global__ __launch_bounds__(256) void kda_attn_join_kernel(const Shape s, const
         yv += *reinterpret_cast<const f32x4 *>(g.part_v + w);
     }
     if (g.sink_slots && index < kTile) {
-        const int64_t left = (len + kTile - 1) / kTile - first_walk_tiles(s, len), parts = (left + g.sink_tiles - 1) / g.sink_tiles;
+        const int64_t left = (len + kTile - 1) / kTile - first_walk_tiles(s, (int)len), parts = (left + g.sink_tiles - 1) / g.sink_tiles;
         const int64_t inner = i - token * (int64_t)D * s.heads_kv, kv = inner / D, ch = inner - kv * D;
         for (int64_t p = 0; p < parts * 2 * g.splits; ++p) {
             const int64_t w = ((first_slot * 2 * g.splits + p) * s.heads_kv + kv) * kTile * D + index * D + ch;
@@ -437,9 +448,9 @@ Plan plan_of(const Shape &s, int dim)
     p.splits = 1;
     while (p.splits < s.group && (s.group % p.splits || (int64_t)s.slots * s.heads_kv * p.splits < 2048)) ++p.splits;
     if (s.sinks) {
-        // a sink workgroup walks a tile in half the time of another: twice the tiles of the longest window walk, and 16 at least
-        const int64_t want = (s.window + kCols) / (kTile / 2);
-        p.sink_tiles = (int32_t)(want < 16 ? 16 : want > (1 << 20) ? 1 << 20 : want);
+        // as many tiles as the window's walk of another workgroup, and 8 at least
+        const int64_t want = (s.window + kCols) / kTile;
+        p.sink_tiles = (int32_t)(want < 8 ? 8 : want > (1 << 20) ? 1 << 20 : want);
         const int64_t per = (int64_t)kTile * p.sink_tiles, parts = (s.tokens + per - 1) / per;
         p.sink_parts = s.cu ? 0 : (int32_t)parts;
         p.sink_slots = (int32_t)(s.cu ? s.tokens / per + s.num_seqs : parts * s.num_seqs);
@@ -462,8 +473,7 @@ template <int D> hipError_t launch_bwd(const Shape &s, Back g, const Plan &p, hi
     static_assert(kLds <= 80 << 10 && kLdsStats <= 80 << 10, "two workgroups a compute unit");
     hipLaunchKernelGGL(kda_attn_dq_kernel<D>, dim3((uint32_t)s.slots * s.heads_q), dim3(kThreads), kLds, st, s, g);
     const uint32_t per_slot = (uint32_t)s.heads_kv * p.splits;
-    hipLaunchKernelGGL((kda_attn_dkv_kernel<D, false>), dim3((uint32_t)s.slots * per_slot), dim3(kThreads), kLdsStats, st, s, g);
-    if (p.sink_slots) hipLaunchKernelGGL((kda_attn_dkv_kernel<D, true>), dim3((uint32_t)p.sink_slots * per_slot), dim3(kThreads), kLdsStats, st, s, g);
+    hipLaunchKernelGGL(kda_attn_dkv_kernel<D>, dim3(((uint32_t)s.slots + p.sink_slots) * per_slot), dim3(kThreads), kLdsStats, st, s, g);
     if (!p.direct) {
         const int64_t tokens = rows_of(s), threads = tokens * s.heads_kv * (D / 4);
         hipLaunchKernelGGL(kda_attn_join_kernel<D>, dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, st, s, g, tokens);

@@ -11,8 +11,13 @@
 namespace kda {
 namespace attn {
 
+// Keys of a tile: as many as leave registers for three waves a SIMD, whose products and exponentials overlap.  us with 32 keys and three
+// waves / 64 and two: d 128, 65536 tokens x 16 heads, window 1024: 678 / 702, 4 x 4096 x 16 causal 318 / 318; d 64 with 64 keys and three /
+// two: 8 x 4096 x 32 causal 648 / 681, 32768 x 16, window 256: 83 / 100.
+template <int D> constexpr int kFwdKeys = D == 128 ? 32 : 64;
+
 template <int D, bool kOutBf16>
-__global__ __launch_bounds__(kThreads, 2) void kda_attn_fwd_kernel(const Shape s, const uint16_t *q, const uint16_t *k, const uint16_t *v,
+__global__ __launch_bounds__(kThreads, 3) void kda_attn_fwd_kernel(const Shape s, const uint16_t *q, const uint16_t *k, const uint16_t *v,
                                                                   void *o, float *lse)
 {
     extern __shared__ __align__(16) uint8_t lds_raw[];
@@ -24,38 +29,45 @@ __global__ __launch_bounds__(kThreads, 2) void kda_attn_fwd_kernel(const Shape s
     const Place at = place_of(s, s.slots - 1 - slot);
     if (at.first >= at.len || at.first < 0) return;
 
-    const int64_t wq0 = at.first + 32 * wave;                            // the wave's first query
-    const int64_t query = wq0 + x, last = at.first + kCols - 1 < at.len - 1 ? at.first + kCols - 1 : at.len - 1;
-    const int64_t wlast = wq0 > last ? -1 : wq0 + 31 < last ? wq0 + 31 : last;            // -1: the wave has no query
+    const int wq0 = at.first + 32 * wave;                                 // the wave's first query
+    const int query = wq0 + x, last = min(at.first + kCols - 1, at.len - 1);
+    const int wlast = wq0 > last ? -1 : min(wq0 + 31, last);              // -1: the wave has no query
 
+    TileReader<D> rd;
+    rd.init(lane);
+    constexpr int kKeys = kFwdKeys<D>;
+    TileLoader<D, kKeys> lk, lv;
+    const uint32_t ks_bytes = s.k_stride * 2, vs_bytes = s.v_stride * 2;
+    lk.init(wave, lane, ks_bytes);
+    lv.init(wave, lane, vs_bytes);
+    const uint16_t *kh = k + at.row0 * s.k_stride + (int64_t)kv * D, *vh = v + at.row0 * s.v_stride + (int64_t)kv * D;
+    constexpr uint32_t kT = kKeys * D * 2;
+
+    // tiles: that of the sinks, if the window begins behind it, then from the window's first to the last query's
+    const int low = s.window && at.first >= s.window ? (at.first - s.window + 1) / kKeys : 0, high = last / kKeys;
+    const int sink_steps = min((s.sinks + kKeys - 1) / kKeys, low), steps = high - low + 1 + sink_steps;
+    const float c = s.scale * kLog2e;
+
+    auto first_key = [&](int it) { return (it < sink_steps ? it : low + it - sink_steps) * kKeys; };
+    // LDS: K and V of one tile, then of another
+    auto issue = [&](int it, uint32_t buf) {
+        const int k0 = first_key(it);
+        lk.issue(lds + 2 * buf * kT, wave, rows_descriptor(kh + k0 * s.k_stride, at.len - k0, ks_bytes));
+        lv.issue(lds + (2 * buf + 1) * kT, wave, rows_descriptor(vh + k0 * s.v_stride, at.len - k0, vs_bytes));
+    };
+    // some query of the wave sees some key of the tile; some does not see some
+    auto needed = [&](int k0) { return k0 <= wlast && !(s.window && k0 + kKeys - 1 <= wq0 - s.window && k0 >= s.sinks); };
+    auto partial = [&](int k0) { return k0 + kKeys - 1 > wq0 || (s.window && wq0 + 31 - k0 >= s.window); };
+
+    issue(0, 0);
     // Q, B operand: 8 channels 16 s + 8 h .. of the lane's query (a query behind the last reads the last one's)
     bf16x8 qf[D / 16];
     {
-        const uint16_t *row = q + (at.row0 + (query < at.len ? query : at.len - 1)) * s.q_stride + (int64_t)head * D + 8 * h;
+        const uint16_t *row = q + (at.row0 + min(query, at.len - 1)) * s.q_stride + (int64_t)head * D + 8 * h;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(row + 16 * i));
     }
-    TileReader<D> rd;
-    rd.init(lane);
-    TileLoader<D> lk, lv;
-    lk.init(wave, lane, s.k_stride * 2);
-    lv.init(wave, lane, s.v_stride * 2);
-    const uint16_t *kh = k + at.row0 * s.k_stride + (int64_t)kv * D, *vh = v + at.row0 * s.v_stride + (int64_t)kv * D;
-    constexpr uint32_t kT = kTileBytes<D>;
-
-    // tiles: that of the sinks, if the window begins behind it, then from the window's first to the last query's
-    const int64_t low = s.window && at.first >= s.window ? (at.first - s.window + 1) / kTile : 0, high = last / kTile;
-    const bool sink_first = s.sinks > 0 && low > 0;
-    const int64_t steps = high - low + 1 + (sink_first ? 1 : 0);
-    const float c = s.scale * kLog2e;
-
-    auto tile_of = [&](int64_t it) { return sink_first ? (it == 0 ? 0 : low + it - 1) : low + it; };
-    auto issue = [&](int64_t it) {
-        const int64_t k0 = tile_of(it) * kTile;
-        const uint32_t buf = lds + (uint32_t)(it & 1) * 2 * kT;
-        lk.issue(buf, wave, rows_descriptor(kh + k0 * s.k_stride, at.len - k0, s.k_stride * 2));
-        lv.issue(buf + kT, wave, rows_descriptor(vh + k0 * s.v_stride, at.len - k0, s.v_stride * 2));
-    };
+    arrived(qf);
 
     f32x16 acc[D / 32];
     float m, mref, l;
@@ -66,31 +78,37 @@ __global__ __launch_bounds__(kThreads, 2) void kda_attn_fwd_kernel(const Shape s
         m = -kInf;
         mref = 0.f;
         l = 0.f;
-        issue(0);
-        for (int64_t it = 0; it < steps; ++it) {
+        auto step = [&](int it, auto parity) {
+            constexpr int P = decltype(parity)::value;
             tile_barrier();
-            if (it + 1 < steps) issue(it + 1);
-            const int64_t k0 = tile_of(it) * kTile;
-            const uint32_t kt = lds + (uint32_t)(it & 1) * 2 * kT, vt = kt + kT;
-            // no query of the wave sees a key of the tile
-            if (k0 > wlast || (s.window && k0 + kTile - 1 <= wq0 - s.window && k0 >= s.sinks)) continue;
-            const bool edge = k0 + kTile - 1 > wq0 || (s.window && wq0 + 31 - k0 >= s.window);
-
-            f32x16 st[2] = {zeros16(), zeros16()};
+            if (it + 1 < steps) issue(it + 1, P ^ 1);
+            const int k0 = first_key(it);
+            const uint32_t kt = lds + 2 * P * kT, vt = kt + kT;
+            if (!needed(k0)) return;
+            const bool edge = partial(k0);
+            f32x16 st[kKeys / 32];
+#pragma unroll
+            for (int b = 0; b < kKeys / 32; ++b) st[b] = zeros16();
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) st[b] = mfma(rd.rows(kt, b, i), qf[i], st[b]);
-
-            uint32_t seen = 0xffffffffu;
-            if (edge) seen = mask_tile(st, edges_of(query, k0, s.window, s.sinks), h);
+                for (int b = 0; b < kKeys / 32; ++b) st[b] = mfma(rd.rows(kt, b, i), qf[i], st[b]);
+            Seen seen;
+            if (edge) {
+                seen = seen_keys(query, k0, s.window, s.sinks);
+#pragma unroll
+                for (int b = 0; b < kKeys / 32; ++b) {
+                    seen.w[b] >>= 4 * h;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) st[b][j] = where_seen(seen_bit(seen.w[b], j), st[b][j], -kInf);
+                }
+            }
             float top = st[0][0];
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < kKeys / 32; ++b)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) top = fmaxf(top, st[b][j]);
-            top = fmaxf(top, other_half(top));
-            top *= c;
+            top = fmaxf(top, other_half(top)) * c;
             if (__any(top > m + 8.f)) {
                 const float mn = fmaxf(m, top), f = mn == -kInf ? 1.f : fast_exp2(m - mn);
                 m = mn;
@@ -101,9 +119,9 @@ __global__ __launch_bounds__(kThreads, 2) void kda_attn_fwd_kernel(const Shape s
 #pragma unroll
                     for (int j = 0; j < 16; ++j) acc[db][j] *= f;
             }
-            bf16x8 p[4];
+            bf16x8 p[kKeys / 16];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            for (int b = 0; b < kKeys / 32; ++b) {
                 float e[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
@@ -115,17 +133,26 @@ __global__ __launch_bounds__(kThreads, 2) void kda_attn_fwd_kernel(const Shape s
             }
             if (kCareful && edge) {
 #pragma unroll
-                for (int db = 0; db < D / 32; ++db) careful_product<D, 4>(acc[db], rd, vt, db, 0, p, seen);
+                for (int db = 0; db < D / 32; ++db) careful_product<D, kKeys / 16>(acc[db], rd, vt, db, 0, p, seen.w);
             } else {
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
+                for (int ks = 0; ks < kKeys / 16; ++ks)
 #pragma unroll
                     for (int db = 0; db < D / 32; ++db) acc[db] = mfma(rd.transposed(vt, db, ks), p[ks], acc[db]);
             }
+        };
+        int it = 0;
+        for (; it + 1 < steps; it += 2) {
+            step(it, std::integral_constant<int, 0>{});
+            step(it + 1, std::integral_constant<int, 1>{});
         }
+        if (it < steps) step(it, std::integral_constant<int, 0>{});
     };
     walk(std::false_type{});
-    if (repeat(acc, acc)) walk(std::true_type{});
+    if (repeat(acc, acc, lds)) {
+        issue(0, 0);
+        walk(std::true_type{});
+    }
 
     l += other_half(l);
     if (query >= at.len) return;
@@ -162,7 +189,7 @@ namespace kda {
 template <int D, bool kOutBf16>
 static hipError_t launch_fwd(const Shape &s, const void *q, const void *k, const void *v, void *o, float *lse, hipStream_t st)
 {
-    constexpr int kLds = 4 * kTileBytes<D>;                  // K and V of the tile in work and of the next
+    constexpr int kLds = 4 * kFwdKeys<D> * D * 2;                  // K and V of the tile in work and of the next
     hipLaunchKernelGGL((kda_attn_fwd_kernel<D, kOutBf16>), dim3((uint32_t)s.slots * s.heads_q), dim3(kThreads), kLds, st, s,
                        static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k), static_cast<const uint16_t *>(v), o, lse);
     return hipGetLastError();

@@ -34,7 +34,7 @@ struct Shape {
     int32_t num_seqs, heads_q, heads_kv, group;
     int32_t slots;                   // tiles of kCols tokens in the grid, for every head
     int32_t tiles;                   // of a sequence of a fixed batch; 0: packed
-    int64_t window;                  // 0: none
+    int32_t window;                  // 0: none; below 2^30
     int32_t sinks;
     float scale;
     int64_t q_stride, k_stride, v_stride;
@@ -46,8 +46,8 @@ struct Shape {
 // pass its end give empty or short sequences, never a row outside.)
 struct Place {
     int64_t row0;                    // first token of the sequence in the tensors
-    int64_t len;                     // its tokens
-    int64_t first;                   // first token of the tile, relative to row0; len or beyond: nothing to do
+    int32_t len;                     // its tokens
+    int32_t first;                   // first token of the tile, relative to row0; len or beyond: nothing to do
     int32_t batch;                   // row of the batch (0: packed)
 };
 __device__ __forceinline__ int64_t cu_at(const Shape &s, int n)
@@ -59,7 +59,7 @@ __device__ __forceinline__ Place place_of(const Shape &s, int slot)
 {
     if (s.tiles) {
         const int b = slot / s.tiles;
-        return {(int64_t)b * s.tokens, s.tokens, (int64_t)(slot - b * s.tiles) * kCols, b};
+        return {(int64_t)b * s.tokens, (int32_t)s.tokens, (slot - b * s.tiles) * kCols, b};
     }
     int lo = 0, hi = s.num_seqs - 1;                         // the last sequence whose base is not beyond the slot
     while (lo < hi) {
@@ -67,18 +67,36 @@ __device__ __forceinline__ Place place_of(const Shape &s, int slot)
         if (cu_at(s, mid) / kCols + mid <= slot) lo = mid; else hi = mid - 1;
     }
     const int64_t a = cu_at(s, lo), e = cu_at(s, lo + 1);
-    return {a, e - a, (slot - (a / kCols + lo)) * kCols, 0};
+    return {a, (int32_t)(e - a), (int32_t)(slot - (a / kCols + lo)) * kCols, 0};
 }
 
-// A query sees a key that is not later and in the window or among the sinks.  For the query's 64 keys from k0 on: the keys (relative)
-// low .. high, and below `sinks` those up to high.
-struct Edges { int32_t low, high, sinks; };
-__device__ __forceinline__ int32_t clamp_tile(int64_t v) { return v < -1 ? -1 : v > kTile ? kTile : (int32_t)v; }
-__device__ __forceinline__ Edges edges_of(int64_t query, int64_t k0, int64_t window, int32_t sinks)
+// What a column of a tile of 64 rows sees, as bits: row 32 b + r of the tile is bit r of w[b].  seen_rows: rows first .. last.
+struct Seen { uint32_t w[2]; };
+__device__ __forceinline__ int32_t clamp_tile(int32_t v) { return v < -1 ? -1 : v > kTile ? kTile : v; }
+__device__ __forceinline__ Seen seen_rows(int32_t first, int32_t last)
 {
-    return {window ? clamp_tile(query - k0 - window + 1) : 0, clamp_tile(query - k0), clamp_tile(sinks - k0)};
+    const uint64_t below = last < 0 ? 0ull : last >= 63 ? ~0ull : (2ull << last) - 1, m = below & (first <= 0 ? ~0ull : first > 63 ? 0ull : ~0ull << first);
+    return {{(uint32_t)m, (uint32_t)(m >> 32)}};
 }
-__device__ __forceinline__ bool sees(const Edges &e, int32_t key) { return key <= e.high && (key >= e.low || key < e.sinks); }
+// The keys k0 .. k0 + 63 that a query sees: not later, and in the window or among the sinks.
+__device__ __forceinline__ Seen seen_keys(int32_t query, int32_t k0, int32_t window, int32_t sinks)
+{
+    const int32_t last = clamp_tile(query - k0), sink = clamp_tile(sinks - k0 - 1);
+    Seen a = seen_rows(window ? clamp_tile(query - k0 - window + 1) : 0, last);
+    const Seen b = seen_rows(0, last < sink ? last : sink);
+    a.w[0] |= b.w[0];
+    a.w[1] |= b.w[1];
+    return a;
+}
+// All ones where accumulator register j of a lane in half h (the word shifted by 4 h) is seen.
+__device__ __forceinline__ uint32_t seen_bit(uint32_t shifted, int j)
+{
+    return (uint32_t)((int32_t)(shifted << (31 - (8 * (j >> 2) + (j & 3)))) >> 31);
+}
+__device__ __forceinline__ float where_seen(uint32_t bit, float x, float other)
+{
+    return __uint_as_float((__float_as_uint(x) & bit) | (__float_as_uint(other) & ~bit));
+}
 
 // ---- LDS tiles of [kTile rows][D] bf16.  The 16-byte chunks of a row stand permuted so that both ways of reading a tile meet every
 // bank once: 16 lanes on the same chunk of 16 rows (A operand of the first product), and 4 rows x 64 contiguous bytes (transposed). ----
@@ -89,11 +107,11 @@ template <int D> __device__ __forceinline__ constexpr int swizzle(int row)
 template <int D> constexpr int kTileBytes = kTile * D * 2;
 
 // Descriptor of the rows of one tile: reads behind `rows` rows give zeros.
-__device__ __forceinline__ u32x4 rows_descriptor(const void *p, int64_t rows, int64_t stride_bytes)
+__device__ __forceinline__ u32x4 rows_descriptor(const void *p, int32_t rows, uint32_t stride_bytes)
 {
     const uint64_t at = reinterpret_cast<uint64_t>(p);
-    const int64_t n = rows < 0 ? 0 : rows > kTile ? kTile : rows;
-    u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32), (uint32_t)(n * stride_bytes), 0x00020000u};
+    const uint32_t n = rows < 0 ? 0 : rows > kTile ? kTile : rows;
+    u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32), n * stride_bytes, 0x00020000u};
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
     return r;
@@ -115,25 +133,23 @@ __device__ __forceinline__ void dma16(uint32_t m0, uint32_t voff, const u32x4 &r
                  "buffer_load_dwordx4 %1, %2, 0 offen lds"
                  :: "s"(m0), "v"(voff), "s"(rsrc) : "memory", "m0");
 }
-// A wave's quarter of a tile of kRows rows, 1 KiB an instruction.  (The chunk's permutation differs from instruction to instruction by a
-// constant.)
+// A wave's quarter of a tile of kRows rows, 1 KiB an instruction.
 template <int D, int kRows = kTile> struct TileLoader {
     static constexpr int kPer = 1024 / (2 * D);             // rows an instruction
     static constexpr int kLoads = kRows / 4 / kPer;
-    uint32_t row, chunk, step;
-    __device__ __forceinline__ void init(int wave, int lane, int64_t stride_bytes)
+    uint32_t voff[kLoads];
+    __device__ __forceinline__ void init(int wave, int lane, uint32_t stride_bytes)
     {
-        const int r = kRows / 4 * wave + lane / (64 / kPer);
-        row = (uint32_t)(r * stride_bytes);
-        chunk = 16 * ((lane % (64 / kPer)) ^ swizzle<D>(r));
-        step = (uint32_t)(kPer * stride_bytes);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int r = kRows / 4 * wave + kPer * j + lane / (64 / kPer);
+            voff[j] = r * stride_bytes + 16 * ((lane % (64 / kPer)) ^ swizzle<D>(r));
+        }
     }
     __device__ __forceinline__ void issue(uint32_t lds, int wave, const u32x4 &rsrc) const
     {
-        static_assert(swizzle<D>(kPer) == (D == 128 ? 1 : 2) && swizzle<D>(kPer * (kLoads - 1)) == swizzle<D>(kPer) * (kLoads - 1), "a constant apart");
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-            dma16(__builtin_amdgcn_readfirstlane(lds + wave * kRows / 4 * 2 * D + j * 1024), row + j * step + (chunk ^ (16 * swizzle<D>(kPer * j))), rsrc);
+        for (int j = 0; j < kLoads; ++j) dma16(__builtin_amdgcn_readfirstlane(lds + wave * kRows / 4 * 2 * D + j * 1024), voff[j], rsrc);
     }
 };
 // every wave's part of the tile has landed, and every wave has left the tile before
@@ -146,7 +162,8 @@ __device__ __forceinline__ void tile_barrier()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// Reads of a tile at LDS byte `tile`: A operands of the two products.
+// Reads of a tile at LDS byte `tile`: A operands of the two products.  The kernels keep no LDS but their own, from byte 0 on, so that
+// where `tile` and what follows it are constants a read is its instruction alone, with one of 16 addresses that stay in registers.
 typedef __attribute__((address_space(3))) const u32x4 *lds_u4;
 typedef __attribute__((address_space(3))) s16x4 *lds_s4;
 template <int D> struct TileReader {
@@ -163,14 +180,13 @@ template <int D> struct TileReader {
             tr_x[u] = ((2 * g + ((i >> 1) & 1)) ^ swizzle<D>(row)) * 16;
         }
     }
-    // The permuted addresses cost an exclusive or each; kept across a walk they would cost 16 registers, which the kernels that need
-    // this do not have (the compiler then spills them): what this touches has to be formed again.
+    // The permuted addresses cost an operation or two each; kept across a walk they take 16 registers, which the dK / dV kernel
+    // does not have (the compiler then spills them): what this touches has to be formed again.
     __device__ __forceinline__ void forget() { asm volatile("" : "+v"(row_x), "+v"(tr_x[0]), "+v"(tr_x[1])); }
     // row 32 block + x, channels 16 s + 8 h ..
     __device__ __forceinline__ bf16x8 rows(uint32_t tile, int block, int s) const
     {
-        const uint32_t at = tile + row_base + (row_x ^ (32 * s)) + block * 32 * 2 * D;
-        return __builtin_bit_cast(bf16x8, *reinterpret_cast<lds_u4>(at));
+        return __builtin_bit_cast(bf16x8, *reinterpret_cast<lds_u4>((row_base + (row_x ^ (32 * s))) + (tile + block * 32 * 2 * D)));
     }
     // channel 32 db + x, rows 16 ks + {4 h + 0..3, 8 + 4 h + 0..3}
     __device__ __forceinline__ bf16x8 transposed(uint32_t tile, int db, int ks) const
@@ -178,7 +194,7 @@ template <int D> struct TileReader {
         s16x4 r[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-            r[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s4>(tile + tr_base[u] + (tr_x[u] ^ (64 * db)) + ks * 16 * 2 * D));
+            r[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s4>((tr_base[u] + (tr_x[u] ^ (64 * db))) + (tile + ks * 16 * 2 * D)));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(r[0], r[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
@@ -187,26 +203,23 @@ __device__ __forceinline__ f32x16 mfma(const bf16x8 &a, const bf16x8 &b, const f
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
+// Waits for operands loaded ahead of a walk.  Left to their first use, inside it, the wait would stand in every step, and as loads come
+// back in order it would wait for the next tile's as well.
+template <int N> __device__ __forceinline__ void arrived(bf16x8 (&f)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        u32x4 w = __builtin_bit_cast(u32x4, f[i]);
+        asm volatile("" : "+v"(w));
+        f[i] = __builtin_bit_cast(bf16x8, w);
+    }
+}
 __device__ __forceinline__ f32x16 zeros16()
 {
     f32x16 z;
 #pragma unroll
     for (int j = 0; j < 16; ++j) z[j] = 0.f;
     return z;
-}
-// -inf in the places of a tile's accumulators (rows: keys) that the column's query does not see; returns the others as bits 16 b + j.
-__device__ __forceinline__ uint32_t mask_tile(f32x16 (&st)[2], const Edges &e, int h)
-{
-    uint32_t seen = 0;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const bool ok = sees(e, 32 * b + 8 * (j >> 2) + 4 * h + (j & 3));
-            st[b][j] = ok ? st[b][j] : -kInf;
-            seen |= (ok ? 1u : 0u) << (16 * b + j);
-        }
-    return seen;
 }
 // the other half wave's value beside this one's: reductions over the rows of a column
 __device__ __forceinline__ float other_half(float v)
@@ -220,6 +233,33 @@ __device__ __forceinline__ bf16x8 pack8(const float *p)
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
     return __builtin_bit_cast(bf16x8, w);
+}
+
+// The order in which a stretch without branches is issued: `lead` LDS reads first, then `per` of them behind each MFMA while there are
+// any of the `reads`, then the rest of the `mfmas`.  Left to itself the compiler has one or two reads in flight and every MFMA, 32 cycles
+// long, waits some 100 for its operand.
+template <int lead, int per, int reads, int mfmas> __device__ __forceinline__ void reads_ahead()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, lead, 0);
+    constexpr int steps = (reads - lead) / per;
+#pragma unroll
+    for (int i = 0; i < steps; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, per, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, mfmas - steps, 0);
+}
+
+// The same with `valu` vector instructions behind every MFMA.
+template <int lead, int valu, int mfmas> __device__ __forceinline__ void reads_among()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, lead, 0);
+#pragma unroll
+    for (int i = 0; i < mfmas; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, valu, 0);
+        if (i < mfmas - lead) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
 }
 
 // ---- values that are not finite in masked places.  A product takes P = 0 times such a value for NaN.  Where that happened (the
@@ -238,9 +278,9 @@ __device__ __forceinline__ bf16x8 without_nonfinite(const bf16x8 &v, bf16x8 &mar
     marks = __builtin_bit_cast(bf16x8, m);
     return __builtin_bit_cast(bf16x8, w);
 }
-// Y += A P for `nk` K-steps of one channel block, A read transposed; bit j of seen: accumulator row j of the step's rows is visible.
+// Y += A P for NK K-steps of one channel block, A read transposed; seen: a word for each 32 rows, shifted by 4 h.
 template <int D, int NK>
-__device__ __forceinline__ void careful_product(f32x16 &y, const TileReader<D> &rd, uint32_t tile, int db, int ks0, const bf16x8 *p, uint32_t seen)
+__device__ __forceinline__ void careful_product(f32x16 &y, const TileReader<D> &rd, uint32_t tile, int db, int ks0, const bf16x8 *p, const uint32_t *seen)
 {
     f32x16 count = zeros16();
 #pragma unroll
@@ -251,22 +291,32 @@ __device__ __forceinline__ void careful_product(f32x16 &y, const TileReader<D> &
         y = mfma(a, p[k], y);
         u32x4 v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = ((seen >> (8 * k + 2 * i)) & 1u ? 0x3f80u : 0u) | ((seen >> (8 * k + 2 * i + 1)) & 1u ? 0x3f800000u : 0u);
+        for (int i = 0; i < 4; ++i)
+            v[i] = (seen_bit(seen[k / 2], 8 * (k % 2) + 2 * i) & 0x3f80u) | (seen_bit(seen[k / 2], 8 * (k % 2) + 2 * i + 1) & 0x3f800000u);
         count = mfma(marks, __builtin_bit_cast(bf16x8, v), count);
     }
 #pragma unroll
     for (int j = 0; j < 16; ++j) y[j] = count[j] > 0.f ? __builtin_nanf("") : y[j];
 }
 
-// Whether any sum of the workgroup is not finite (0 times an infinity or NaN is NaN): the walk is then repeated with care.
-template <int N> __device__ __forceinline__ bool repeat(const f32x16 (&a)[N], const f32x16 (&b)[N])
+// Whether any sum of the workgroup is not finite (0 times an infinity or NaN is NaN): the walk is then repeated with care.  LDS is
+// free when this is called, and when it returns.
+template <int N> __device__ __forceinline__ bool repeat(const f32x16 (&a)[N], const f32x16 (&b)[N], uint32_t lds)
 {
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int j = 0; j < 16; ++j) sum += &a == &b ? a[i][j] * 0.f : (a[i][j] + b[i][j]) * 0.f;
-    return __syncthreads_or(!(sum == 0.f));
+    typedef __attribute__((address_space(3))) uint32_t *lds_u1;
+    typedef __attribute__((address_space(3))) u32x4 *lds_w4;
+    const uint32_t any = __any(!(sum == 0.f));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) *reinterpret_cast<lds_u1>(lds + (threadIdx.x >> 4)) = any;
+    __syncthreads();
+    const u32x4 w = *reinterpret_cast<lds_w4>(lds);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(w[0] | w[1] | w[2] | w[3]) != 0;
 }
 
 // Workgroup -> (slot, query head or key head): heads fastest, a group's key head fastest of all, so that the tiles that read the same
