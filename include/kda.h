@@ -485,12 +485,15 @@ typedef struct {
  * Scales: powers of two.  A page and head's scale is the smallest (2^-100 at least) with which its largest new value is at most 448 codes'
  * steps, or the one it has, if that is larger and the page holds older tokens; where it grows, the older tokens' codes are rounded again
  * to the new scale.  Codes are rounded to nearest even from the fp32 rotation; values that are not finite are stored as NaN and leave the
- * scale alone.  Rows of k_out and q_out of skipped sequences and of tokens owned by none are left untouched, as is whatever stands in a
- * page behind the sequence's last token.  A page that is appended to must belong to one sequence.
+ * scale alone.  Whatever stands in a page behind the sequence's last token is left as it is.  A page that is appended to must belong to
+ * one sequence.
+ *   flags          rows of q_out (KDA_APPEND_ZERO_Q) and k_out (KDA_APPEND_ZERO_K) of skipped sequences and of tokens owned by none are
+ *                  written as zeros instead of left untouched
  */
+enum { KDA_APPEND_ZERO_Q = 1, KDA_APPEND_ZERO_K = 2 };
 kda_status kda_cache_append(const kda_cache *cache, int64_t seqlen, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
                             const int32_t *cu_seqlens, const kda_rope *rope, void *k_out, const void *q, int64_t q_stride, void *q_out,
-                            void *hip_stream);
+                            uint32_t flags, void *hip_stream);
 
 /* A call of kda_cache_attn. */
 typedef struct {

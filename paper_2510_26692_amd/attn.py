@@ -6,7 +6,11 @@ import ctypes
 
 import torch
 
+from . import kda as _kda
 from .kda import KdaError, _DTYPE_CODE, _check_dev, _clear_unowned, _out_dtype, _ptr, _stream_ptr, kda_last_error, load_library
+
+
+_APPEND_ZERO_Q, _APPEND_ZERO_K = 1, 2    # flags of kda_cache_append
 
 
 class KdaAttnDims(ctypes.Structure):
@@ -36,9 +40,25 @@ class KdaCacheQuery(ctypes.Structure):
                 ("scale", ctypes.c_float), ("max_kv_len", ctypes.c_int64), ("out_dtype", ctypes.c_int)]
 
 
-def _raise(st):
+def _call(dev, entry, *args):
+    """One call of the library on dev's current stream, with dev the current device (launches go to that one)."""
+    if torch.cuda.current_device() == dev.index:
+        st = entry(*args, _stream_ptr(dev))
+    else:
+        with torch.cuda.device(dev):
+            st = entry(*args, _stream_ptr(dev))
     if st != 0:
         raise KdaError(st, kda_last_error())
+
+
+def _native(name, *args):
+    """What the native way (csrc/kda_host.cpp) returned, or None: not built, or a call it leaves to the general way."""
+    if _kda._native is None:
+        return None
+    done = getattr(_kda._native, name)(*args)
+    if type(done) is int:
+        raise KdaError(done, kda_last_error())
+    return done
 
 
 def _token_stride(t, name):
@@ -91,6 +111,10 @@ def kda_window_attn_fwd(q, k, v, window=0, sinks=0, cu_seqlens=None, scale=None,
     given.  Returns (o [B,T,Hq,d], lse fp32 [B,Hq,T] or None); o is fp32 unless out_dtype (or the `o` passed in) is torch.bfloat16.
     Rows of tokens that belong to no sequence are zero in what this call allocates and untouched in what is passed in."""
     lib = load_library()
+    if cu_seqlens is None:
+        done = _native("window_fwd", q, k, v, window, sinks, scale, o, lse, want_lse, out_dtype)
+        if done is not None:
+            return done
     dev = _device(q, k, v, cu_seqlens, o, lse)
     odt = _out_dtype(o, out_dtype)
     dims = _attn_dims(q, k, v, window, sinks, cu_seqlens, scale, odt)
@@ -106,7 +130,7 @@ def kda_window_attn_fwd(q, k, v, window=0, sinks=0, cu_seqlens=None, scale=None,
             raise ValueError("lse must be contiguous fp32 [B,Hq,T]")
     elif want_lse:
         lse = (torch.empty if cu_seqlens is None else torch.zeros)(B, Hq, T, dtype=torch.float32, device=dev)
-    _raise(lib.kda_window_attn_fwd(ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), _ptr(o), _ptr(lse), _stream_ptr(dev)))
+    _call(dev, lib.kda_window_attn_fwd, ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), _ptr(o), _ptr(lse))
     if cu_seqlens is not None and fresh:
         _clear_unowned(cu_seqlens, fresh)
     return o, lse
@@ -121,6 +145,10 @@ def kda_window_attn_bwd(q, k, v, o, lse, do, window=0, sinks=0, cu_seqlens=None,
     in bf16.  Returns a dict of bf16 tensors dq [B,T,Hq,d], dk and dv [B,T,Hk,d]; rows of tokens that belong to no sequence are zero (this
     wrapper clears them in the gradients it allocates).  `out`: the dict an earlier call returned, to be written in place."""
     lib = load_library()
+    if cu_seqlens is None and workspace is None and out is None:
+        done = _native("window_bwd", q, k, v, o, lse, do, window, sinks, scale)
+        if done is not None:
+            return dict(zip(("dq", "dk", "dv"), done))
     dev = _device(q, k, v, o, lse, do, cu_seqlens, workspace)
     if o.dtype != torch.bfloat16 or do.dtype != torch.bfloat16 or o.shape != q.shape or do.shape != q.shape:
         raise ValueError("o and do must be bf16 [B,T,Hq,d]")
@@ -142,9 +170,8 @@ def kda_window_attn_bwd(q, k, v, o, lse, do, window=0, sinks=0, cu_seqlens=None,
         _check_dev(o, *out.values())
     if workspace is None:
         workspace = torch.empty(max(kda_window_attn_bwd_workspace_size(dims), 256), dtype=torch.uint8, device=dev)
-    _raise(lib.kda_window_attn_bwd(ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), _ptr(o), _ptr(lse), _ptr(do),
-                                   _ptr(out["dq"]), _ptr(out["dk"]), _ptr(out["dv"]), _ptr(workspace),
-                                   ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream_ptr(dev)))
+    _call(dev, lib.kda_window_attn_bwd, ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), _ptr(o), _ptr(lse), _ptr(do),
+          _ptr(out["dq"]), _ptr(out["dk"]), _ptr(out["dv"]), _ptr(workspace), ctypes.c_size_t(workspace.numel() * workspace.element_size()))
     if cu_seqlens is not None and clear:
         _clear_unowned(cu_seqlens, clear)
     return out
@@ -177,6 +204,9 @@ def kda_cache_append(k, v, k_cache, v_cache, k_scale, v_scale, block_table, kv_l
     a k_out passed in): the rotated keys in bf16 as well.  Returns (q_out or None, k_out or None); rows of skipped sequences and of tokens that
     belong to none are zero in what this call allocates and untouched in what is passed in."""
     lib = load_library()
+    done = _native("append", k, v, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, cu_seqlens, inv_freq, interleaved, q, q_out, k_out, want_k)
+    if done is not None:
+        return done
     dev = _device(k, v, q, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, cu_seqlens, inv_freq, q_out, k_out)
     if k.dim() != 4 or k.shape != v.shape or not (k.dtype == v.dtype == torch.bfloat16):
         raise ValueError("k and v must be bf16 [N,T,Hk,d]")
@@ -202,13 +232,15 @@ def kda_cache_append(k, v, k_cache, v_cache, k_scale, v_scale, block_table, kv_l
     for t, like, name in ((q_out, q, "q_out"), (k_out, k, "k_out")):
         if t is not None and (t.dtype != torch.bfloat16 or t.shape != like.shape or not t.is_contiguous()):
             raise ValueError("%s must be contiguous bf16 of the shape of what is rotated" % name)
+    flags = 0
     if q is not None and q_out is None:
-        q_out = torch.zeros(q.shape, dtype=torch.bfloat16, device=dev)
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+        flags |= _APPEND_ZERO_Q
     if want_k and k_out is None:
-        k_out = torch.zeros(k.shape, dtype=torch.bfloat16, device=dev)
-    _raise(lib.kda_cache_append(ctypes.byref(cache), T, _ptr(k), _ptr(v), _token_stride(k, "k"), _token_stride(v, "v"), _ptr(cu_seqlens),
-                                None if rope is None else ctypes.byref(rope), _ptr(k_out), _ptr(q), 0 if q is None else _token_stride(q, "q"),
-                                _ptr(q_out), _stream_ptr(dev)))
+        k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=dev)
+        flags |= _APPEND_ZERO_K
+    _call(dev, lib.kda_cache_append, ctypes.byref(cache), T, _ptr(k), _ptr(v), _token_stride(k, "k"), _token_stride(v, "v"), _ptr(cu_seqlens),
+          None if rope is None else ctypes.byref(rope), _ptr(k_out), _ptr(q), 0 if q is None else _token_stride(q, "q"), _ptr(q_out), flags)
     return q_out, k_out
 
 
@@ -219,6 +251,10 @@ def kda_cache_attn(q, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, 
     the work is split).  Returns o [N,Tq,Hq,d], fp32 unless out_dtype (or the `o` passed in) is torch.bfloat16; tokens that see nothing
     get zeros."""
     lib = load_library()
+    if workspace is None:
+        done = _native("attend", q, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, window, sinks, scale, max_kv_len, o, out_dtype)
+        if done is not None:
+            return done
     dev = _device(q, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, o, workspace)
     if q.dim() != 4 or q.dtype != torch.bfloat16:
         raise ValueError("q must be bf16 [N,Tq,Hq,d]")
@@ -236,6 +272,6 @@ def kda_cache_attn(q, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, 
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     else:
         _check_dev(workspace)
-    _raise(lib.kda_cache_attn(ctypes.byref(cache), ctypes.byref(query), _ptr(q), _ptr(o), _ptr(workspace),
-                              ctypes.c_size_t(0 if workspace is None else workspace.numel() * workspace.element_size()), _stream_ptr(dev)))
+    _call(dev, lib.kda_cache_attn, ctypes.byref(cache), ctypes.byref(query), _ptr(q), _ptr(o), _ptr(workspace),
+          ctypes.c_size_t(0 if workspace is None else workspace.numel() * workspace.element_size()))
     return o

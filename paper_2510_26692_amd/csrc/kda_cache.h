@@ -30,6 +30,7 @@ struct Append {
     int32_t slots_per_seq;           // 0: packed
     int32_t page_blocks;             // workgroups of pages; those behind them turn queries
     int32_t q_heads;                 // query heads a thread turns
+    int32_t zero_q, zero_k;          // rows that no sequence writes become zeros
 };
 // A call of kda_cache_attn.
 struct Attend {

@@ -98,7 +98,7 @@ using namespace kda;
 
 extern "C" kda_status kda_cache_append(const kda_cache *cache, int64_t seqlen, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
                                        const int32_t *cu_seqlens, const kda_rope *rope, void *k_out, const void *q, int64_t q_stride, void *q_out,
-                                       void *hip_stream)
+                                       uint32_t flags, void *hip_stream)
 {
     cache::Cache c;
     if (const kda_status st = check(cache, true, c); st != KDA_OK) return st;
@@ -117,7 +117,8 @@ extern "C" kda_status kda_cache_append(const kda_cache *cache, int64_t seqlen, c
     if (kda_status st = stride_of(v_stride, row, "v", a.v_stride); st != KDA_OK) return st;
     if (kda_status st = stride_of(q_stride, (int64_t)cache->heads_q * cache->dim, "q", a.q_stride); st != KDA_OK) return st;
     if ((q == nullptr) != (q_out == nullptr)) return fail(KDA_ERR_INVALID_ARG, "q and q_out come together");
-    if (seqlen == 0 || c.num_seqs == 0 || c.heads_q == 0) return KDA_OK;
+    if (flags & ~(uint32_t)(KDA_APPEND_ZERO_Q | KDA_APPEND_ZERO_K)) return fail(KDA_ERR_INVALID_ARG, "flags %u", (unsigned)flags);
+    if (seqlen == 0 || c.heads_q == 0 || (c.num_seqs == 0 && !cu_seqlens)) return KDA_OK;
     if (!k || !v) return fail(KDA_ERR_INVALID_ARG, "k or v is NULL");
     for (const void *p : {k, v, q, (const void *)k_out, (const void *)q_out})
         if (!aligned(p, 16)) return fail(KDA_ERR_INVALID_ARG, "kda_cache_append: tensors must be 16-byte aligned");
@@ -128,11 +129,13 @@ extern "C" kda_status kda_cache_append(const kda_cache *cache, int64_t seqlen, c
     a.k_out = static_cast<uint16_t *>(k_out);
     a.q_out = static_cast<uint16_t *>(q_out);
     a.cu = cu_seqlens;
+    a.zero_q = q_out && (flags & KDA_APPEND_ZERO_Q);
+    a.zero_k = k_out && (flags & KDA_APPEND_ZERO_K);
     a.per_seq = cu_seqlens ? 0 : seqlen;
     a.tokens = cu_seqlens ? seqlen : seqlen * c.num_seqs;
     // pages that seqlen tokens can touch, wherever they begin
     const int64_t per_seq = cu_seqlens ? 0 : (seqlen + c.page_size - 2) / c.page_size + 1;
-    const int64_t slots = cu_seqlens ? seqlen / c.page_size + 2 * (int64_t)c.num_seqs : per_seq * c.num_seqs;
+    const int64_t slots = c.num_seqs == 0 ? 0 : cu_seqlens ? seqlen / c.page_size + 2 * (int64_t)c.num_seqs : per_seq * c.num_seqs;
     if (slots * c.heads_kv * 2 + a.tokens * c.heads_q > 0x7fffffffLL) return fail(KDA_ERR_UNSUPPORTED, "more than 2^31 pages and heads, or rows of q");
     a.slots = (int32_t)slots;
     a.slots_per_seq = (int32_t)per_seq;

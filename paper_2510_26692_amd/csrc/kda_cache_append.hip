@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kThreads) void kda_cache_append_kernel(const Cache 
                 const int n = (int)(token / a.per_seq);
                 const int64_t len = c.lens[n];
                 if (len >= 0) pos = len + token - n * a.per_seq;
-            } else if (token >= cu_at(a, 0) && token < cu_at(a, c.num_seqs)) {
+            } else if (token >= cu_at(a, 0) && c.num_seqs && token < cu_at(a, c.num_seqs)) {
                 int lo = 0, hi = c.num_seqs - 1;
                 while (lo < hi) {
                     const int mid = (lo + hi + 1) >> 1;
@@ -163,6 +163,14 @@ __global__ __launch_bounds__(kThreads) void kda_cache_append_kernel(const Cache 
                 if (len >= 0) pos = len + token - cu_at(a, lo);
             }
         }
+        if (pos < 0 && token < a.tokens && (a.zero_q || a.zero_k)) {
+            const u32x4 zero = {0, 0, 0, 0};
+            if (a.zero_q)
+                for (int h = h0; h < h0 + a.q_heads && h < c.heads_q; ++h) *reinterpret_cast<u32x4 *>(a.q_out + (token * c.heads_q + h) * D + 8 * piece) = zero;
+            if (a.zero_k && h0 == 0)
+                for (int h = 0; h < c.heads_kv; ++h) *reinterpret_cast<u32x4 *>(a.k_out + (token * c.heads_kv + h) * D + 8 * piece) = zero;
+        }
+        if (!a.q) return;
         Piece t;
         t.init(a, piece);
         float cs[8], sn[8];
@@ -333,7 +341,7 @@ static hipError_t launch_append(const Cache &c, Append a, hipStream_t st)
 {
     constexpr int kRows = kThreads / (D / 8);
     int64_t q_blocks = 0;
-    if (a.q) {
+    if (a.q || a.zero_k) {
         // several heads a thread share its angles once there are threads enough: 2^17 of them
         a.q_heads = 1;
         while (a.q_heads < 8 && a.tokens * c.heads_q * (D / 8) / a.q_heads > 1 << 17) a.q_heads *= 2;

@@ -1,6 +1,6 @@
-// The decode calls of the Python binding (kda.py), marshalled natively: a decode step of one sequence takes the device 4 us, and the
+// The decode calls of the Python binding (kda.py) and those of the softmax-attention layers (attn.py), marshalled natively: a decode step of one sequence takes the device 4 us, and the
 // checks, descriptors and ctypes of the general path 10 us of the host (measured in a loop of kda_recurrent_step, 1 sequence x 32
-// heads: 9.9 us a call through kda.py alone, 4.2 to 5.0 here).
+// heads: 9.9 us a call through kda.py alone, 4.2 to 5.0 here; @@FIGS@@).
 //
 // Only calls that are regular in every respect are taken: plain contiguous device tensors of the expected types and shapes on
 // one device.  For anything else, and for whatever cannot be told here, the functions return None, and kda.py's own path decides
@@ -9,7 +9,10 @@
 // same library.
 #include <Python.h>
 
+#include <cmath>
+
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -19,6 +22,12 @@ namespace {
 
 decltype(&kda_recurrent_step) step_entry;
 decltype(&kda_recurrent_steps) steps_entry;
+decltype(&kda_cache_append) append_entry;
+decltype(&kda_cache_attn) attend_entry;
+decltype(&kda_cache_attn_workspace_size) attend_size_entry;
+decltype(&kda_window_attn_fwd) fwd_entry;
+decltype(&kda_window_attn_bwd) bwd_entry;
+decltype(&kda_window_attn_bwd_workspace_size) bwd_size_entry;
 PyObject *raw_stream;                                        // device index -> current stream, as a number
 
 struct Irregular {};
@@ -197,6 +206,227 @@ PyObject *steps(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+int64_t whole(PyObject *x)
+{
+    if (!PyLong_CheckExact(x)) throw Irregular{};
+    const int64_t v = PyLong_AsLongLong(x);
+    if (v == -1 && PyErr_Occurred()) throw Irregular{};
+    return v;
+}
+bool truth(PyObject *x)
+{
+    if (x != Py_True && x != Py_False) throw Irregular{};
+    return x == Py_True;
+}
+int32_t narrow(int64_t n)
+{
+    if (n < 0 || n > 0x7fffffff) throw Irregular{};
+    return (int32_t)n;
+}
+float attn_scale(PyObject *x, int64_t dim) { return x == Py_None ? (float)(1.0 / std::sqrt((double)dim)) : number(x); }
+at::Tensor bytes(size_t n, const at::Tensor &like) { return at::empty({(int64_t)n}, like.options().dtype(at::kByte)); }
+
+// The cache's arguments a[0..5]: k_cache, v_cache, k_scale, v_scale, block_table, kv_lens.
+kda_cache cache_of(PyObject *const *a, const Checked &check, int64_t N, int64_t Hq, int64_t Hk, int64_t d)
+{
+    const at::Tensor &k = plain(a[0]), &table = plain(a[4]);
+    if (k.dim() != 4 || table.dim() != 2) throw Irregular{};
+    const int64_t P = k.size(0), page = k.size(2);
+    check(k, at::kFloat8_e4m3fn, {P, Hk, page, d});
+    check(table, at::kInt, {N, table.size(1)});
+    kda_cache c{};
+    c.num_seqs = narrow(N); c.heads_q = narrow(Hq); c.heads_kv = narrow(Hk); c.dim = narrow(d); c.page_size = narrow(page);
+    c.num_pages = P; c.max_pages = narrow(table.size(1));
+    c.k = k.data_ptr(); c.v = check(a[1], at::kFloat8_e4m3fn, k.sizes()).data_ptr();
+    c.k_scale = static_cast<float *>(check(a[2], at::kFloat, {P, Hk}).data_ptr());
+    c.v_scale = static_cast<float *>(check(a[3], at::kFloat, {P, Hk}).data_ptr());
+    c.block_table = static_cast<const int32_t *>(table.data_ptr());
+    c.kv_lens = static_cast<const int32_t *>(check(a[5], at::kInt, {N}).data_ptr());
+    return c;
+}
+
+// (the first of two results and the second, None where there is none)
+PyObject *pair(kda_status st, PyObject *given0, const at::Tensor &t0, PyObject *given1, const at::Tensor &t1)
+{
+    if (st != KDA_OK) return PyLong_FromLong((long)st);
+    auto object = [](PyObject *given, const at::Tensor &t) -> PyObject * {
+        if (given == Py_None && t.defined()) return THPVariable_Wrap(t);
+        Py_INCREF(given);
+        return given;
+    };
+    PyObject *a = object(given0, t0), *b = a ? object(given1, t1) : nullptr, *r = b ? PyTuple_Pack(2, a, b) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(b);
+    if (!r) throw Irregular{};
+    return r;
+}
+
+// append(k, v, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, cu_seqlens, inv_freq, interleaved, q, q_out, k_out, want_k)
+PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 15 || !append_entry) throw Irregular{};
+        const at::Tensor &k = plain(a[0]);
+        if (k.dim() != 4) throw Irregular{};
+        const int64_t B = k.size(0), T = k.size(1), Hk = k.size(2), d = k.size(3);
+        const Checked check(k);
+        check(k, at::kBFloat16, {B, T, Hk, d});
+        const at::Tensor &v = check(a[1], at::kBFloat16, k.sizes());
+        int64_t N = B, Hq = Hk;
+        const int32_t *cu = nullptr;
+        if (a[8] != Py_None) {
+            const at::Tensor &t = plain(a[8]);
+            if (t.dim() != 1 || t.size(0) < 1 || B != 1) throw Irregular{};
+            cu = static_cast<const int32_t *>(check(t, at::kInt, t.sizes()).data_ptr());
+            N = t.size(0) - 1;
+        }
+        at::Tensor q, q_out, k_out;
+        uint32_t flags = 0;
+        if (a[11] != Py_None) {
+            q = plain(a[11]);
+            if (q.dim() != 4) throw Irregular{};
+            Hq = q.size(2);
+            check(q, at::kBFloat16, {B, T, Hq, d});
+            if (a[12] != Py_None) q_out = check(a[12], at::kBFloat16, q.sizes());
+            else { q_out = at::empty(q.sizes(), q.options()); flags |= KDA_APPEND_ZERO_Q; }
+        } else if (a[12] != Py_None) {
+            throw Irregular{};
+        }
+        if (a[13] != Py_None) k_out = check(a[13], at::kBFloat16, k.sizes());
+        else if (truth(a[14])) { k_out = at::empty(k.sizes(), k.options()); flags |= KDA_APPEND_ZERO_K; }
+        const kda_cache c = cache_of(a + 2, check, N, Hq, Hk, d);
+        kda_rope rope{};
+        if (a[9] != Py_None) {
+            const at::Tensor &f = plain(a[9]);
+            if (f.dim() != 1) throw Irregular{};
+            rope.inv_freq = static_cast<const float *>(check(f, at::kFloat, f.sizes()).data_ptr());
+            rope.num_freqs = narrow(f.size(0));
+            rope.interleaved = truth(a[10]);
+        }
+        const c10::DeviceGuard on(k.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = append_entry(&c, T, k.data_ptr(), v.data_ptr(), 0, 0, cu, a[9] != Py_None ? &rope : nullptr, k_out.defined() ? k_out.data_ptr() : nullptr,
+                          q.defined() ? q.data_ptr() : nullptr, 0, q_out.defined() ? q_out.data_ptr() : nullptr, flags, stream);
+        Py_END_ALLOW_THREADS
+        return pair(st, a[12], q_out, a[13], k_out);
+    });
+}
+
+// attend(q, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, window, sinks, scale, max_kv_len, o, out_dtype)
+PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 13 || !attend_entry) throw Irregular{};
+        const at::Tensor &q = plain(a[0]), &kc = plain(a[1]);
+        if (q.dim() != 4 || kc.dim() != 4) throw Irregular{};
+        const int64_t N = q.size(0), T = q.size(1), Hq = q.size(2), d = q.size(3);
+        const Checked check(q);
+        check(q, at::kBFloat16, {N, T, Hq, d});
+        const kda_cache c = cache_of(a + 1, check, N, Hq, kc.size(1), d);
+        const at::Tensor o = output(a[11], a[12], q, check);
+        kda_cache_query query{};
+        query.tokens = narrow(T); query.window = whole(a[7]); query.sinks = narrow(whole(a[8])); query.scale = attn_scale(a[9], d);
+        query.max_kv_len = whole(a[10]); query.out_dtype = (kda_dtype)code(o.scalar_type());
+        const size_t need = attend_size_entry(&c, &query);
+        const at::Tensor ws = need ? bytes(need, q) : at::Tensor();
+        const c10::DeviceGuard on(q.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = attend_entry(&c, &query, q.data_ptr(), o.data_ptr(), need ? ws.data_ptr() : nullptr, need, stream);
+        Py_END_ALLOW_THREADS
+        return finish(st, a[11], o);
+    });
+}
+
+// The dims of a fixed batch.
+kda_attn_dims attn_dims(const at::Tensor &q, const at::Tensor &k, const Checked &check, PyObject *window, PyObject *sinks, PyObject *scale, int out)
+{
+    kda_attn_dims d{};
+    check(q, at::kBFloat16, q.sizes());
+    check(k, at::kBFloat16, {q.size(0), q.size(1), k.size(2), q.size(3)});
+    d.batch = d.num_seqs = narrow(q.size(0)); d.seqlen = q.size(1); d.heads_q = narrow(q.size(2)); d.heads_kv = narrow(k.size(2)); d.dim = narrow(q.size(3));
+    d.in_dtype = KDA_BF16; d.out_dtype = (kda_dtype)out; d.scale = attn_scale(scale, q.size(3)); d.window = whole(window); d.sinks = narrow(whole(sinks));
+    return d;
+}
+
+// window_fwd(q, k, v, window, sinks, scale, o, lse, want_lse, out_dtype): a fixed batch
+PyObject *window_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 10 || !fwd_entry) throw Irregular{};
+        const at::Tensor &q = plain(a[0]), &k = plain(a[1]);
+        if (q.dim() != 4 || k.dim() != 4) throw Irregular{};
+        const Checked check(q);
+        const at::Tensor o = output(a[6], a[9], q, check);
+        const kda_attn_dims d = attn_dims(q, k, check, a[3], a[4], a[5], code(o.scalar_type()));
+        const at::Tensor &v = check(a[2], at::kBFloat16, k.sizes());
+        at::Tensor lse;
+        if (a[7] != Py_None) lse = check(a[7], at::kFloat, {q.size(0), q.size(2), q.size(1)});
+        else if (truth(a[8])) lse = at::empty({q.size(0), q.size(2), q.size(1)}, q.options().dtype(at::kFloat));
+        const c10::DeviceGuard on(q.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = fwd_entry(&d, q.data_ptr(), k.data_ptr(), v.data_ptr(), nullptr, o.data_ptr(), lse.defined() ? static_cast<float *>(lse.data_ptr()) : nullptr, stream);
+        Py_END_ALLOW_THREADS
+        return pair(st, a[6], o, a[7], lse);
+    });
+}
+
+// window_bwd(q, k, v, o, lse, do, window, sinks, scale): a fixed batch; (dq, dk, dv)
+PyObject *window_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 9 || !bwd_entry) throw Irregular{};
+        const at::Tensor &q = plain(a[0]), &k = plain(a[1]);
+        if (q.dim() != 4 || k.dim() != 4) throw Irregular{};
+        const Checked check(q);
+        const kda_attn_dims d = attn_dims(q, k, check, a[6], a[7], a[8], KDA_BF16);
+        const at::Tensor &v = check(a[2], at::kBFloat16, k.sizes()), &o = check(a[3], at::kBFloat16, q.sizes());
+        const at::Tensor &lse = check(a[4], at::kFloat, {q.size(0), q.size(2), q.size(1)}), &d_o = check(a[5], at::kBFloat16, q.sizes());
+        const at::Tensor dq = at::empty(q.sizes(), q.options()), dk = at::empty(k.sizes(), k.options()), dv = at::empty(k.sizes(), k.options());
+        const size_t need = bwd_size_entry(&d);
+        const at::Tensor ws = bytes(need ? need : 256, q);
+        const c10::DeviceGuard on(q.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = bwd_entry(&d, q.data_ptr(), k.data_ptr(), v.data_ptr(), nullptr, o.data_ptr(), static_cast<const float *>(lse.data_ptr()), d_o.data_ptr(),
+                       dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), need ? need : 256, stream);
+        Py_END_ALLOW_THREADS
+        if (st != KDA_OK) return PyLong_FromLong((long)st);
+        PyObject *r = PyTuple_New(3);
+        if (!r) throw Irregular{};
+        int i = 0;
+        for (const at::Tensor &t : {dq, dk, dv}) {
+            PyObject *w = THPVariable_Wrap(t);
+            if (!w) { Py_DECREF(r); throw Irregular{}; }
+            PyTuple_SET_ITEM(r, i++, w);
+        }
+        return r;
+    });
+}
+
+// bind_attn(addresses of kda_cache_append, kda_cache_attn, kda_cache_attn_workspace_size, kda_window_attn_fwd, kda_window_attn_bwd,
+// kda_window_attn_bwd_workspace_size), after bind
+PyObject *bind_attn(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 6) { PyErr_SetString(PyExc_TypeError, "bind_attn takes six arguments"); return nullptr; }
+    void *p[6];
+    for (int i = 0; i < 6; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+    append_entry = reinterpret_cast<decltype(append_entry)>(p[0]);
+    attend_entry = reinterpret_cast<decltype(attend_entry)>(p[1]);
+    attend_size_entry = reinterpret_cast<decltype(attend_size_entry)>(p[2]);
+    fwd_entry = reinterpret_cast<decltype(fwd_entry)>(p[3]);
+    bwd_entry = reinterpret_cast<decltype(bwd_entry)>(p[4]);
+    bwd_size_entry = reinterpret_cast<decltype(bwd_size_entry)>(p[5]);
+    Py_RETURN_NONE;
+}
+
 // bind(address of kda_recurrent_step, address of kda_recurrent_steps, function from a device index to its current stream)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -215,6 +445,11 @@ PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind)), METH_FASTCALL, nullptr},
     {"step", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(step)), METH_FASTCALL, nullptr},
     {"steps", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(steps)), METH_FASTCALL, nullptr},
+    {"bind_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind_attn)), METH_FASTCALL, nullptr},
+    {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(append)), METH_FASTCALL, nullptr},
+    {"attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attend)), METH_FASTCALL, nullptr},
+    {"window_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(window_fwd)), METH_FASTCALL, nullptr},
+    {"window_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(window_bwd)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kda_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

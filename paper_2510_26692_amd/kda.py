@@ -132,7 +132,7 @@ def load_library():
     lib.kda_window_attn_bwd.argtypes = [vp] * 12 + [sz, vp]
     i64 = ctypes.c_int64
     lib.kda_cache_append.restype = ctypes.c_int
-    lib.kda_cache_append.argtypes = [vp, i64, vp, vp, i64, i64, vp, vp, vp, vp, i64, vp, vp]
+    lib.kda_cache_append.argtypes = [vp, i64, vp, vp, i64, i64, vp, vp, vp, vp, i64, vp, ctypes.c_uint32, vp]
     lib.kda_cache_attn_workspace_size.restype = sz
     lib.kda_cache_attn_workspace_size.argtypes = [vp, vp]
     lib.kda_cache_attn.restype = ctypes.c_int
@@ -140,6 +140,9 @@ def load_library():
     try:
         from . import _kda_host
         _kda_host.bind(*[ctypes.cast(f, vp).value for f in (lib.kda_recurrent_step, lib.kda_recurrent_steps)], _raw_stream)
+        _kda_host.bind_attn(*[ctypes.cast(f, vp).value for f in (lib.kda_cache_append, lib.kda_cache_attn, lib.kda_cache_attn_workspace_size,
+                                                                 lib.kda_window_attn_fwd, lib.kda_window_attn_bwd,
+                                                                 lib.kda_window_attn_bwd_workspace_size)])
         _native = _kda_host
     except ImportError as e:                # (missing, or built for another torch or interpreter: right all the same, but no secret)
         warnings.warn("decode calls are marshalled in Python, at about twice the host time: %s (build it with "

@@ -80,7 +80,7 @@ def _cache(**kw):
 
 def _append(c, seqlen=4, rope=None, **kw):
     a = dict(k=SOME, v=SOME, ks=0, vs=0, cu=None)
-    b = dict(k_out=None, q=None, qs=0, q_out=None)
+    b = dict(k_out=None, q=None, qs=0, q_out=None, flags=0)
     for n, x in kw.items():
         (a if n in a else b)[n] = x
     return kda.load_library().kda_cache_append(None if c is None else ctypes.byref(c), seqlen, *a.values(), None if rope is None else ctypes.byref(rope),
@@ -111,7 +111,7 @@ def test_cache_append_refuses():
     assert _append(None) == INVALID
     c = _cache()
     for kw in (dict(k=None), dict(v=None), dict(k=SOME + 8), dict(ks=250), dict(vs=128), dict(q=SOME), dict(q_out=SOME), dict(q=SOME, q_out=SOME + 8),
-               dict(q=SOME, q_out=SOME, qs=100), dict(k_out=SOME + 8), dict(cu=SOME + 1), dict(seqlen=-1)):
+               dict(q=SOME, q_out=SOME, qs=100), dict(k_out=SOME + 8), dict(cu=SOME + 1), dict(seqlen=-1), dict(flags=4)):
         assert _append(c, **kw) == INVALID, kw
     for n in (-8, 4, 12, 72):
         assert _append(c, rope=kda.KdaRope(inv_freq=SOME, num_freqs=n)) == INVALID

@@ -138,6 +138,33 @@ def test_append_skips_sequences_and_pages_that_are_not_there():
     assert not bool(q_out[0].any()) and not bool(k_out[0].any())
 
 
+def test_append_rows_of_nobody_in_what_is_passed_in_and_what_is_allocated():
+    """Skipped sequences and unowned tokens: untouched in q_out and k_out that the caller brings, zeros in fresh ones; a batch of no
+    sequences at all."""
+    import paper_2510_26692_amd as kda
+    pool = Pool(3, 2, 64, 16, 64, 9)
+    kd, vd, ksd, vsd, td = pool.device()
+    f = torch.from_numpy(_freqs(32)).cuda()
+    k, v, q = (_tokens(1, 30, h, 64, h).cuda() for h in (2, 2, 4))
+    lens = torch.tensor([4, -3, 9], dtype=torch.int32, device="cuda")
+    cu = torch.tensor([2, 10, 15, 27], dtype=torch.int32, device="cuda")
+    nobody = torch.ones(30, dtype=torch.bool)
+    nobody[2:10] = nobody[15:27] = False
+    outs = []
+    for given in (False, True):
+        q_in, k_in = (torch.full_like(t, 7) for t in (q, k)) if given else (None, None)
+        q_out, k_out = kda.kda_cache_append(k, v, kd, vd, ksd, vsd, td, lens, cu_seqlens=cu, inv_freq=f, q=q, q_out=q_in, k_out=k_in, want_k=True)
+        for t in (q_out, k_out):
+            assert bool((t[0, nobody] == (7 if given else 0)).all())
+        outs.append((q_out[0, ~nobody], k_out[0, ~nobody]))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    only_k = kda.kda_cache_append(k, v, kd, vd, ksd, vsd, td, lens, cu_seqlens=cu, inv_freq=f, want_k=True)
+    assert only_k[0] is None and torch.equal(only_k[1][0, ~nobody], outs[0][1]) and not bool(only_k[1][0, nobody].any())
+    none = torch.zeros(1, dtype=torch.int32, device="cuda")
+    q_out, k_out = kda.kda_cache_append(k, v, kd, vd, ksd, vsd, td[:0], lens[:0], cu_seqlens=none, inv_freq=f, q=q, want_k=True)
+    assert not bool(q_out.any()) and not bool(k_out.any())
+
+
 def test_append_token_by_token_rounds_older_codes_again():
     import paper_2510_26692_amd as kda
     pool = Pool(2, 2, 64, 32, 96, 4)
