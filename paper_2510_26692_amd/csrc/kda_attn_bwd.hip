@@ -159,12 +159,17 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
         }
     return false;
 }
+// The walk with care is a call at d 128, where in line it takes registers from the loop that always runs (dK / dV: 78 spilled without it,
+// 261 with it); at d 64 there are enough, and the call's stack costs more (us in line / called, d 64: 8 x 4096 x 32 heads 2290 / 2370,
+// 2 x 200 x 4 heads, forward and backward, 28.0 / 29.5; d 128: 4 x 4096 x 16 heads 1090 / 1041).
 template <int D> __device__ __noinline__ void dq_tile_again(const Shape s, const Back g, const uint32_t lds) { dq_tile<D, true>(s, g, lds); }
-template <int D> __global__ __launch_bounds__(kThreads, 2) void kda_attn_dq_kernel(const Shape s, const Back g)
+template <int D> __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kda_attn_dq_kernel(const Shape s, const Back g)
 {
     extern __shared__ __align__(16) uint8_t lds_raw[];
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds_raw;
-    if (dq_tile<D, false>(s, g, lds)) dq_tile_again<D>(s, g, lds);
+    if (!dq_tile<D, false>(s, g, lds)) return;
+    if constexpr (D == 128) dq_tile_again<D>(s, g, lds);
+    else dq_tile<D, true>(s, g, lds);
 }
 
 // dK and dV of 128 keys, or (the first workgroups) the sinks' part of a sequence's first 64, each half of the waves on every other tile of
@@ -342,6 +347,7 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dkv_tile(const S
                         dv[db] = mfma(rd.transposed(dt, db, 2 * b + ks), pb[ks], dv[db]);
                         dk[db] = mfma(rd.transposed(qt, db, 2 * b + ks), ds[ks], dk[db]);
                     }
+                reads_ahead<8, 2, D / 4, D / 8>();
             }
         }
     }
@@ -380,7 +386,9 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void kda_attn_dkv_ker
 {
     extern __shared__ __align__(16) uint8_t lds_raw[];
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds_raw;
-    if (dkv_tile<D, false>(s, g, lds)) dkv_tile_again<D>(s, g, lds);
+    if (!dkv_tile<D, false>(s, g, lds)) return;
+    if constexpr (D == 128) dkv_tile_again<D>(s, g, lds);
+    else dkv_tile<D, true>(s, g, lds);
 }
 
 // Sums of the parts: a thread has four channels of a token and key head.
@@ -444,13 +452,16 @@ int64_t rows_of(const Shape &s) { return s.cu ? s.tokens : s.tokens * s.num_seqs
 Plan plan_of(const Shape &s, int dim)
 {
     Plan p{};
-    // workgroups of the dK / dV walk: eight for each place (two a compute unit), so that the last ones to run are a small part
+    // Workgroups of the dK / dV walk: causal walks differ in length up to the whole sequence, and eight for each place (two a compute unit)
+    // let the short ones fill in behind the long; walks of a window are alike, and two for each place are enough.  us with 512 / 1024 / 2048:
+    // 4 x 4096 x 16 heads causal 1280 / 1150 / 1040, 32768 x 16 heads d 64, window 256 358 / 354 / 444.
+    const int64_t want = s.window ? 1024 : 2048;
     p.splits = 1;
-    while (p.splits < s.group && (s.group % p.splits || (int64_t)s.slots * s.heads_kv * p.splits < 2048)) ++p.splits;
+    while (p.splits < s.group && (s.group % p.splits || (int64_t)s.slots * s.heads_kv * p.splits < want)) ++p.splits;
     if (s.sinks) {
         // as many tiles as the window's walk of another workgroup, and 8 at least
-        const int64_t want = (s.window + kCols) / kTile;
-        p.sink_tiles = (int32_t)(want < 8 ? 8 : want > (1 << 20) ? 1 << 20 : want);
+        const int64_t tiles = (s.window + kCols) / kTile;
+        p.sink_tiles = (int32_t)(tiles < 8 ? 8 : tiles > (1 << 20) ? 1 << 20 : tiles);
         const int64_t per = (int64_t)kTile * p.sink_tiles, parts = (s.tokens + per - 1) / per;
         p.sink_parts = s.cu ? 0 : (int32_t)parts;
         p.sink_slots = (int32_t)(s.cu ? s.tokens / per + s.num_seqs : parts * s.num_seqs);

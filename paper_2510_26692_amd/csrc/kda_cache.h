@@ -26,9 +26,11 @@ struct Append {
     int64_t k_stride, v_stride, q_stride;
     int32_t n_freq;                  // half the rotated channels
     int32_t interleaved;
-    int32_t slots;                   // pages that the call may touch: every workgroup has one of them for a head
+    int32_t slots;                   // pages that the call may touch: a workgroup has one of them for some heads
     int32_t slots_per_seq;           // 0: packed
     int32_t page_blocks;             // workgroups of pages; those behind them turn queries
+    int32_t whole;                   // a slot is a sequence: its workgroups have all pages that its new tokens touch
+    int32_t page_heads;              // heads of a page that a workgroup has
     int32_t q_heads;                 // query heads a thread turns
     int32_t zero_q, zero_k;          // rows that no sequence writes become zeros
 };
@@ -37,9 +39,9 @@ struct Attend {
     const uint16_t *q;
     void *o;
     float *part, *stats;             // [N][Hk][splits][rows][D] and [..][2]: numerators' sums, maximum (in powers of two) and sum of the softmax
-    int64_t q_stride, window;
+    int64_t q_stride;
     float scale;
-    int32_t tokens, sinks, rows, row_tiles, splits, out_bf16;
+    int32_t tokens, window, sinks, rows, row_tiles, splits, out_bf16;
 };
 
 // Number of the page that holds logical page p of sequence n, or -1.

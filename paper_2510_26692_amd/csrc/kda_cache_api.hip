@@ -71,14 +71,15 @@ kda_status check(const kda_cache *d, bool buffers, const kda_cache_query *q, cac
     if (!(q->scale >= 1e-30f && q->scale <= 1e30f)) return fail(KDA_ERR_INVALID_ARG, "scale must be positive, in [1e-30, 1e30]");
     if (q->out_dtype != KDA_F32 && q->out_dtype != KDA_BF16) return fail(KDA_ERR_INVALID_ARG, "out_dtype %d is not a kda_dtype", (int)q->out_dtype);
     a = {};
-    a.window = q->window;
-    a.sinks = q->window ? q->sinks : 0;
+    // a window that no two tokens are apart by is none
+    a.window = q->window > 0x7fffffffLL ? 0 : (int32_t)q->window;
+    a.sinks = a.window ? q->sinks : 0;
     a.scale = q->scale;
     a.tokens = q->tokens;
     a.out_bf16 = q->out_dtype == KDA_BF16;
     if (const kda_status st = stride_of(q->q_stride, (int64_t)d->heads_q * d->dim, "q", a.q_stride); st != KDA_OK) return st;
     a.rows = q->tokens * c.group;
-    a.row_tiles = a.rows <= 32 ? 1 : (a.rows + 63) / 64;
+    a.row_tiles = (a.rows + 31) / 32;
     const int64_t pairs = (int64_t)c.num_seqs * c.heads_kv, held = (int64_t)d->max_pages * d->page_size;
     const int64_t most = q->max_kv_len && q->max_kv_len < held ? q->max_kv_len : held;
     a.splits = pairs && a.rows ? cache_attn_splits(c, pairs * a.row_tiles, most, a.window, a.sinks, a.tokens) : 1;

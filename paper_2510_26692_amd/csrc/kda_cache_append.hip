@@ -37,21 +37,30 @@ struct Piece {
         shift = interleaved || !on ? 0 : (second ? -1 : 1) * (a.n_freq / 8);
         first = interleaved ? 4 * c : 8 * c - (second ? a.n_freq : 0);
     }
-    // revolutions of pair e at position pos, less the nearest whole number: exact to 2^-20 of a revolution at 2^31
-    __device__ __forceinline__ double turns(const Append &a, int e, int64_t pos) const
+    // revolutions a position of pair e (0: not rotated)
+    __device__ __forceinline__ double frequency(const Append &a, int e) const
     {
-        const double t = on ? (double)pos * ((double)a.inv_freq[first + e] * 0.15915494309189535) : 0.0;
-        return t - __builtin_rint(t);
+        return on ? (double)a.inv_freq[first + (interleaved ? e & 3 : e)] * 0.15915494309189535 : 0.0;
+    }
+    // The pairs that this lane computes angles of: its four, or half of the eight that it shares with the other half's lane.
+    __device__ __forceinline__ void own_frequencies(const Append &a, bool wanted, double (&f)[4]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = wanted ? frequency(a, second ? 4 + e : e) : 0.0;
     }
 };
-// cos and sin of 2 pi r, |r| <= 1/2, in 64 bits: Taylor's series about the nearest quarter, 16 terms (2^-54 at pi / 4).
+// revolutions at a position, less the nearest whole number: exact to 2^-20 of a revolution at 2^31
+__device__ __forceinline__ double turns(double frequency, int64_t pos)
+{
+    const double t = (double)pos * frequency;
+    return t - __builtin_rint(t);
+}
+// cos and sin of 2 pi r, |r| <= 1/2: Taylor's series about the nearest quarter, to x^14 and x^13 (2^-46 at pi / 4: one code in 2^40 would differ).
 struct Angle { double c, s; };
 __device__ __forceinline__ Angle angle64(double r)
 {
     const double q = __builtin_rint(4.0 * r), x = (r - 0.25 * q) * 6.283185307179586, y = x * x;
-    double c = 4.779477332387385e-14, s = -7.647163731819816e-13;                            // 1/16!, -1/15!
-    c = fma(c, y, -1.1470745597729725e-11);
-    s = fma(s, y, 1.6059043836821613e-10);
+    double c = -1.1470745597729725e-11, s = 1.6059043836821613e-10;                          // -1/14!, 1/13!
     c = fma(c, y, 2.08767569878681e-09);
     s = fma(s, y, -2.505210838544172e-08);
     c = fma(c, y, -2.755731922398589e-07);
@@ -70,6 +79,28 @@ __device__ __forceinline__ Angle angle64(double r)
     return {k == 1 || k == 2 ? -cc : cc, k & 2 ? -ss : ss};
 }
 __device__ __forceinline__ Angle operator*(const Angle &a, const Angle &b) { return {fma(a.c, b.c, -a.s * b.s), fma(a.c, b.s, a.s * b.c)}; }
+
+__device__ __forceinline__ double from_lane(double v, int byte)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_ds_bpermute(byte, (uint32_t)b), hi = __builtin_amdgcn_ds_bpermute(byte, (uint32_t)(b >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// The angles of a lane's pairs at a position.  (64-bit operations take about three times the others' time: four angles a lane, the rest
+// from the lane that has them.  Every lane takes part.)
+__device__ __forceinline__ void angles(const Piece &t, const double (&freq)[4], int64_t pos, double (&cs)[8], double (&sn)[8])
+{
+    const int from = ((int)(threadIdx.x & 63) + t.shift) * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const Angle z = angle64(turns(freq[e], pos));
+        const double oc = from_lane(z.c, from), os = from_lane(z.s, from);
+        cs[e] = t.second ? oc : z.c;
+        sn[e] = t.second ? os : z.s;
+        cs[4 + e] = t.second ? z.c : oc;
+        sn[4 + e] = t.second ? z.s : os;
+    }
+}
 
 __device__ __forceinline__ void unpack8(const u32x4 &w, float (&x)[8])
 {
@@ -136,79 +167,229 @@ __device__ __forceinline__ float scale_for(float top)
     return __uint_as_float((uint32_t)e << 23);
 }
 
-template <int D, int kThreads, int kIters>
-__global__ __launch_bounds__(kThreads) void kda_cache_append_kernel(const Cache c, const Append a)
+// Queries: a token's angles, then its heads.
+template <int D, int kThreads> __device__ __forceinline__ void turn_queries(const Cache &c, const Append &a, uint32_t block)
 {
     constexpr int kPieces = D / 8, kRows = kThreads / kPieces;           // pieces of a row, rows at a time
     const int tid = threadIdx.x, piece = tid % kPieces, row0 = tid / kPieces;
-    if ((int)blockIdx.x >= a.page_blocks) {
-        // ---- queries: a token's angles, then its heads ----
-        const int parts = (c.heads_q + a.q_heads - 1) / a.q_heads;
-        const int64_t item = ((int64_t)blockIdx.x - a.page_blocks) * kRows + row0;
-        const int64_t token = item / parts;
-        const int h0 = (int)(item - token * parts) * a.q_heads;
-        int64_t pos = -1;
-        if (token < a.tokens) {
-            if (a.slots_per_seq) {
-                const int n = (int)(token / a.per_seq);
-                const int64_t len = c.lens[n];
-                if (len >= 0) pos = len + token - n * a.per_seq;
-            } else if (token >= cu_at(a, 0) && c.num_seqs && token < cu_at(a, c.num_seqs)) {
-                int lo = 0, hi = c.num_seqs - 1;
-                while (lo < hi) {
-                    const int mid = (lo + hi + 1) >> 1;
-                    if (cu_at(a, mid) <= token) lo = mid; else hi = mid - 1;
-                }
-                const int64_t len = c.lens[lo];
-                if (len >= 0) pos = len + token - cu_at(a, lo);
+    const int parts = (c.heads_q + a.q_heads - 1) / a.q_heads;
+    Piece t;                                                 // (its loads ahead of those that wait for one another)
+    t.init(a, piece);
+    double freq[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) freq[e] = a.q ? t.frequency(a, e) : 0.0;
+    const int64_t item = (int64_t)block * kRows + row0;
+    const int64_t token = item / parts;
+    const int h0 = (int)(item - token * parts) * a.q_heads;
+    int64_t pos = -1;
+    if (token < a.tokens) {
+        if (a.slots_per_seq) {
+            const int n = (int)(token / a.per_seq);
+            const int64_t len = c.lens[n];
+            if (len >= 0) pos = len + token - n * a.per_seq;
+        } else if (token >= cu_at(a, 0) && c.num_seqs && token < cu_at(a, c.num_seqs)) {
+            int lo = 0, hi = c.num_seqs - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (cu_at(a, mid) <= token) lo = mid; else hi = mid - 1;
             }
+            const int64_t len = c.lens[lo];
+            if (len >= 0) pos = len + token - cu_at(a, lo);
         }
-        if (pos < 0 && token < a.tokens && (a.zero_q || a.zero_k)) {
-            const u32x4 zero = {0, 0, 0, 0};
-            if (a.zero_q)
-                for (int h = h0; h < h0 + a.q_heads && h < c.heads_q; ++h) *reinterpret_cast<u32x4 *>(a.q_out + (token * c.heads_q + h) * D + 8 * piece) = zero;
-            if (a.zero_k && h0 == 0)
-                for (int h = 0; h < c.heads_kv; ++h) *reinterpret_cast<u32x4 *>(a.k_out + (token * c.heads_kv + h) * D + 8 * piece) = zero;
-        }
-        if (!a.q) return;
-        Piece t;
-        t.init(a, piece);
-        float cs[8], sn[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float r = (float)t.turns(a, t.interleaved ? e & 3 : e, pos);
-            cs[e] = __builtin_amdgcn_cosf(r);                // (of 2 pi r)
-            sn[e] = __builtin_amdgcn_sinf(r);
-        }
-        const bool in = pos >= 0;
-        const uint16_t *from = a.q + (in ? token : 0) * a.q_stride + 8 * piece;
-        uint16_t *to = a.q_out + (in ? token : 0) * (int64_t)c.heads_q * D + 8 * piece;
-        // (no lane leaves early: the pieces of a row exchange their halves)
-        const int last = c.heads_q - 1;
-        for (int h = h0; h < h0 + a.q_heads; h += 4) {
-            u32x4 w[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (u < a.q_heads) w[u] = *reinterpret_cast<const u32x4 *>(from + (int64_t)(h + u < last ? h + u : last) * D);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (u >= a.q_heads) break;                   // (the same for every lane)
-                float x[8];
-                turn(t, cs, sn, w[u], x);
-                if (in && h + u <= last) *reinterpret_cast<u32x4 *>(to + (int64_t)(h + u) * D) = pack8(x);
-            }
-        }
-        return;
     }
+    if (pos < 0 && token < a.tokens && (a.zero_q || a.zero_k)) {
+        const u32x4 zero = {0, 0, 0, 0};
+        if (a.zero_q)
+            for (int h = h0; h < h0 + a.q_heads && h < c.heads_q; ++h) *reinterpret_cast<u32x4 *>(a.q_out + (token * c.heads_q + h) * D + 8 * piece) = zero;
+        if (a.zero_k && h0 == 0)
+            for (int h = 0; h < c.heads_kv; ++h) *reinterpret_cast<u32x4 *>(a.k_out + (token * c.heads_kv + h) * D + 8 * piece) = zero;
+    }
+    if (!a.q) return;
+    const bool in = pos >= 0;
+    const uint16_t *from = a.q + (in ? token : 0) * a.q_stride + 8 * piece;
+    uint16_t *to = a.q_out + (in ? token : 0) * (int64_t)c.heads_q * D + 8 * piece;
+    // (no lane leaves early: the pieces of a row exchange their halves.  The loads of the first heads go ahead of the angles.)
+    const int last = c.heads_q - 1;
+    u32x4 w[4];
+    auto fetch = [&](int h) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (u < a.q_heads) w[u] = *reinterpret_cast<const u32x4 *>(from + (int64_t)min(h + u, last) * D);
+    };
+    fetch(h0);
+    float cs[8], sn[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float r = (float)turns(freq[e], pos);
+        cs[e] = __builtin_amdgcn_cosf(r);                    // (of 2 pi r)
+        sn[e] = __builtin_amdgcn_sinf(r);
+    }
+    for (int h = h0; h < h0 + a.q_heads; h += 4) {
+        u32x4 y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] = w[u];
+        if (h + 4 < h0 + a.q_heads) fetch(h + 4);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (u >= a.q_heads) break;                       // (the same for every lane)
+            float x[8];
+            turn(t, cs, sn, y[u], x);
+            if (in && h + u <= last) *reinterpret_cast<u32x4 *>(to + (int64_t)(h + u) * D) = pack8(x);
+        }
+    }
+}
 
-    // ---- one page of one sequence and head ----
-    const bool values = blockIdx.x & 1;
-    const int head = (int)((blockIdx.x >> 1) % c.heads_kv), slot = (int)((blockIdx.x >> 1) / c.heads_kv);
+// One page of one sequence, keys or values, `heads` heads of it one after the other.
+//
+// Angles are held in 64 bits, so that the codes are those of the exact rotation (in 32 bits one in 2^21 was another): computed for the
+// lane's first row and for the distance to its next, then multiplied, 4 operations a pair instead of 30, down the rows of one head and up
+// those of the next.  16 prompts (67 000 tokens, 8 heads, pages of 64), 0.55 GB: 354 us with a workgroup a head, 160 so; a plain copy of as
+// many bytes takes 106.  256 sequences x 4 tokens: 20 us with a workgroup a page, head and 4 rows, 11 so.
+template <int D, int kThreads, int kIters>
+__device__ __forceinline__ void append_page(const Cache &c, const Append &a, const Piece &t, const double (&freq)[4], bool turned, bool values, int head0, int n,
+                                            int64_t logical, int64_t len, int64_t count, int64_t first_row)
+{
+    constexpr int kPieces = D / 8, kRows = kThreads / kPieces;
+    const int tid = threadIdx.x, piece = tid % kPieces, row0 = tid / kPieces;
+    const int64_t page0 = logical << c.page_log2;
+    const int64_t begin = page0 > len ? page0 : len, end = page0 + c.page_size < len + count ? page0 + c.page_size : len + count;
+    if (begin >= end) return;
+    const int rows = (int)(end - begin), older = (int)(begin - page0);
+
+    const int64_t row = first_row + begin - len;
+    const int64_t stride = values ? a.v_stride : a.k_stride;
+    const uint16_t *from = (values ? a.v : a.k) + (row + row0) * stride + (int64_t)head0 * D + 8 * piece;
+    // a head's new rows, 16 bytes a lane
+    auto fetch = [&](int j, u32x4 (&w)[kIters]) {
+#pragma unroll
+        for (int i = 0; i < kIters; ++i) {
+            w[i] = u32x4{0, 0, 0, 0};
+            if (i * kRows + row0 < rows) w[i] = *reinterpret_cast<const u32x4 *>(from + i * kRows * stride + (int64_t)j * D);
+        }
+    };
+    u32x4 w[kIters];
+    fetch(0, w);
+    const int32_t page = page_at(c, n, logical);
+    if (page < 0 && (values || !a.k_out)) return;
+    float *scale_at = (values ? c.v_scale : c.k_scale) + (int64_t)page * c.heads_kv + head0;
+    uint8_t *codes = (values ? c.v : c.k) + ((int64_t)page * c.heads_kv + head0) * c.page_size * D + 8 * piece;
+    const bool has_older = page >= 0 && older;
+    float scale_next = has_older ? scale_at[0] : 0.f;
+
+    double cs[8], sn[8], nc[8], ns[8];
+    if (turned) {
+        angles(t, freq, begin + row0, cs, sn);
+        if (kIters > 1 && rows > kRows) angles(t, freq, kRows, nc, ns);
+    }
+    [[maybe_unused]] __shared__ float tops[2][kThreads / 64];
+    if constexpr (kThreads > 64) __syncthreads();            // (of the page before)
+    for (int j = 0; j < a.page_heads; ++j) {
+        const float scale_old = scale_next;
+        float x[kIters][8], top = 0.f;
+        if (turned) {
+            const bool up = j & 1;
+            auto one = [&](int i, bool more) {
+                turn(t, cs, sn, w[i], x[i]);
+                if (more) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const Angle z = Angle{cs[e], sn[e]} * Angle{nc[e], up ? -ns[e] : ns[e]};
+                        cs[e] = z.c;
+                        sn[e] = z.s;
+                    }
+                }
+            };
+            // (the conditions are the same for every lane)
+            if (!up) {
+#pragma unroll
+                for (int i = 0; i < kIters; ++i)
+                    if (i * kRows < rows) one(i, (i + 1) * kRows < rows && i + 1 < kIters);
+            } else {
+#pragma unroll
+                for (int i = kIters - 1; i >= 0; --i)
+                    if (i * kRows < rows) one(i, i > 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kIters; ++i)
+                if (i * kRows < rows) unpack8(w[i], x[i]);
+        }
+        if (!values && a.k_out) {
+            uint16_t *to = a.k_out + ((row + row0) * c.heads_kv + head0 + j) * D + 8 * piece;
+#pragma unroll
+            for (int i = 0; i < kIters; ++i)
+                if (i * kRows + row0 < rows) *reinterpret_cast<u32x4 *>(to + (int64_t)i * kRows * c.heads_kv * D) = pack8(x[i]);
+        }
+        if (j + 1 < a.page_heads) {
+            fetch(j + 1, w);
+            scale_next = has_older ? scale_at[j + 1] : 0.f;
+        }
+        if (page < 0) continue;
+#pragma unroll
+        for (int i = 0; i < kIters; ++i)
+            if (i * kRows < rows) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = fabsf(x[i][e]);
+                    top = fmaxf(top, y < __builtin_huge_valf() ? y : 0.f);
+                }
+            }
+#pragma unroll
+        for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+        if constexpr (kThreads > 64) {
+            if ((tid & 63) == 0) tops[j & 1][tid >> 6] = top;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kThreads / 64; ++i) top = fmaxf(top, tops[j & 1][i]);
+        }
+        const float scale = fmaxf(scale_old, scale_for(top)), inv = 1.f / scale;
+        uint8_t *to = codes + (int64_t)j * c.page_size * D;
+        if (scale > scale_old && older) {
+            const float again = scale_old * inv;
+            for (int r = row0; r < older; r += kRows) {
+                u32x2 *at = reinterpret_cast<u32x2 *>(to + r * D);
+                const u32x2 y = *at;
+                float z[8];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], true);
+                    z[4 * i] = lo[0];
+                    z[4 * i + 1] = lo[1];
+                    z[4 * i + 2] = hi[0];
+                    z[4 * i + 3] = hi[1];
+                }
+                *at = codes8(z, again);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kIters; ++i)
+            if (i * kRows + row0 < rows) *reinterpret_cast<u32x2 *>(to + (older + i * kRows + row0) * D) = codes8(x[i], inv);
+        if (tid == 0) scale_at[j] = scale;
+    }
+}
+
+// The pages of a workgroup: its slot's, for some heads.
+template <int D, int kThreads, int kIters>
+__device__ __forceinline__ void append_pages(const Cache &c, const Append &a, uint32_t block)
+{
+    constexpr int kPieces = D / 8;
+    const int piece = threadIdx.x % kPieces;
+    const bool values = block & 1;
+    const int groups = c.heads_kv / a.page_heads, head0 = (int)((block >> 1) % groups) * a.page_heads, slot = (int)((block >> 1) / groups);
+    const bool turned = !values && a.n_freq;
+    Piece t;                                                 // (its loads ahead of those that wait for one another)
+    t.init(a, piece);
+    double freq[4];
+    t.own_frequencies(a, turned, freq);
     int n, index;
     int64_t first_row, count;                                // of the sequence's new tokens
     if (a.slots_per_seq) {
-        n = slot / a.slots_per_seq;
-        index = slot - n * a.slots_per_seq;
+        n = slot;                                            // all pages that the sequence's new tokens touch, or a slot a page
+        index = 0;
+        if (!a.whole) {
+            n = slot / a.slots_per_seq;
+            index = slot - n * a.slots_per_seq;
+        }
         first_row = n * a.per_seq;
         count = a.per_seq;
     } else {
@@ -225,112 +406,24 @@ __global__ __launch_bounds__(kThreads) void kda_cache_append_kernel(const Cache 
     }
     const int64_t len = c.lens[n];
     if (len < 0 || count <= 0 || index < 0) return;
-    const int64_t logical = (len >> c.page_log2) + index, page0 = logical << c.page_log2;
-    const int64_t begin = page0 > len ? page0 : len, end = page0 + c.page_size < len + count ? page0 + c.page_size : len + count;
-    if (begin >= end) return;
-    const int rows = (int)(end - begin), older = (int)(begin - page0);
-    const int32_t page = page_at(c, n, logical);
-    if (page < 0 && (values || !a.k_out)) return;
-
-    // (the rows' new tokens, 16 bytes a lane)
-    const int64_t row = first_row + begin - len;
-    const uint16_t *from = values ? a.v + row * a.v_stride : a.k + row * a.k_stride;
-    const int64_t stride = values ? a.v_stride : a.k_stride;
-    u32x4 w[kIters];
-#pragma unroll
-    for (int i = 0; i < kIters; ++i) {
-        const int r = i * kRows + row0;
-        w[i] = u32x4{0, 0, 0, 0};
-        if (r < rows) w[i] = *reinterpret_cast<const u32x4 *>(from + r * stride + (int64_t)head * D + 8 * piece);
-    }
-    float *scale_at = (values ? c.v_scale : c.k_scale) + (int64_t)page * c.heads_kv + head;
-    const float scale_old = page >= 0 && older ? *scale_at : 0.f;
-    float x[kIters][8], top = 0.f;
-    if (!values && a.n_freq) {
-        // Angles in 64 bits, so that the codes are those of the exact rotation (in 32 bits one in 2^21 was another): computed for the first
-        // row and for the distance to the next, then multiplied, 4 operations a pair instead of 30.
-        Piece t;
-        t.init(a, piece);
-        double cs[8], sn[8];
-        Angle next[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int f = t.interleaved ? e & 3 : e;
-            const Angle z = angle64(t.turns(a, f, begin + row0));
-            cs[e] = z.c;
-            sn[e] = z.s;
-            if (kIters > 1) next[e] = angle64(t.turns(a, f, kRows));
-        }
-#pragma unroll
-        for (int i = 0; i < kIters; ++i) {
-            if (i * kRows >= rows) break;                    // (the same for every lane)
-            const int r = i * kRows + row0;
-            turn(t, cs, sn, w[i], x[i]);
-            if (a.k_out && r < rows) *reinterpret_cast<u32x4 *>(a.k_out + ((row + r) * c.heads_kv + head) * D + 8 * piece) = pack8(x[i]);
-            if (i + 1 < kIters) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const Angle z = Angle{cs[e], sn[e]} * next[e];
-                    cs[e] = z.c;
-                    sn[e] = z.s;
-                }
-            }
-        }
+    const int64_t logical = (len >> c.page_log2) + index;
+    if constexpr (kIters == 1) {
+        const int pages = a.whole ? (int)(((len + count - 1) >> c.page_log2) - logical) + 1 : 1;
+        for (int p = 0; p < pages; ++p)
+            append_page<D, kThreads, kIters>(c, a, t, freq, turned, values, head0, n, logical + p, len, count, first_row);
     } else {
-#pragma unroll
-        for (int i = 0; i < kIters; ++i) {
-            if (i * kRows >= rows) break;
-            const int r = i * kRows + row0;
-            unpack8(w[i], x[i]);
-            if (!values && a.k_out && r < rows) *reinterpret_cast<u32x4 *>(a.k_out + ((row + r) * c.heads_kv + head) * D + 8 * piece) = w[i];
-        }
+        append_page<D, kThreads, kIters>(c, a, t, freq, turned, values, head0, n, logical, len, count, first_row);
     }
-    if (page < 0) return;
-#pragma unroll
-    for (int i = 0; i < kIters; ++i) {
-        if (i * kRows >= rows) break;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float y = fabsf(x[i][e]);
-            top = fmaxf(top, y < __builtin_huge_valf() ? y : 0.f);
-        }
-    }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    if constexpr (kThreads > 64) {
-        __shared__ float tops[kThreads / 64];
-        if ((tid & 63) == 0) tops[tid >> 6] = top;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kThreads / 64; ++i) top = fmaxf(top, tops[i]);
-    }
-    const float scale = fmaxf(scale_old, scale_for(top)), inv = 1.f / scale;
-    uint8_t *codes = (values ? c.v : c.k) + ((int64_t)page * c.heads_kv + head) * c.page_size * D + 8 * piece;
-    if (scale > scale_old && older) {
-        const float again = scale_old * inv;
-        for (int r = row0; r < older; r += kRows) {
-            u32x2 *at = reinterpret_cast<u32x2 *>(codes + r * D);
-            const u32x2 y = *at;
-            float z[8];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], true);
-                z[4 * i] = lo[0];
-                z[4 * i + 1] = lo[1];
-                z[4 * i + 2] = hi[0];
-                z[4 * i + 3] = hi[1];
-            }
-            *at = codes8(z, again);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kIters; ++i) {
-        const int r = i * kRows + row0;
-        if (i * kRows >= rows) break;
-        if (r < rows) *reinterpret_cast<u32x2 *>(codes + (int64_t)(older + r) * D) = codes8(x[i], inv);
-    }
-    if (tid == 0) *scale_at = scale;
 }
+
+// Pages, and behind them queries.
+template <int D, int kThreads, int kIters>
+__global__ __launch_bounds__(kThreads, kIters == 1 ? 3 : 2) void kda_cache_append_kernel(const Cache c, const Append a)
+{
+    if (blockIdx.x < (uint32_t)a.page_blocks) append_pages<D, kThreads, kIters>(c, a, blockIdx.x);
+    else turn_queries<D, kThreads>(c, a, blockIdx.x - a.page_blocks);
+}
+template <int D> __global__ __launch_bounds__(256) void kda_cache_queries_kernel(const Cache c, const Append a) { turn_queries<D, 256>(c, a, blockIdx.x); }
 
 }  // namespace cache
 
@@ -340,30 +433,47 @@ template <int D, int kThreads, int kIters>
 static hipError_t launch_append(const Cache &c, Append a, hipStream_t st)
 {
     constexpr int kRows = kThreads / (D / 8);
+    // Heads that share a lane's angles: as many as leave 1024 workgroups.
+    a.page_heads = c.heads_kv;
+    while (a.page_heads > 1 && (c.heads_kv % a.page_heads || (int64_t)a.slots * (c.heads_kv / a.page_heads) < 1024)) --a.page_heads;
+    a.page_blocks = a.slots * (c.heads_kv / a.page_heads) * 2;
     int64_t q_blocks = 0;
     if (a.q || a.zero_k) {
         // several heads a thread share its angles once there are threads enough: 2^17 of them
         a.q_heads = 1;
-        while (a.q_heads < 8 && a.tokens * c.heads_q * (D / 8) / a.q_heads > 1 << 17) a.q_heads *= 2;
+        while (a.q_heads < 16 && a.tokens * c.heads_q * (D / 8) / a.q_heads > 1 << 17) a.q_heads *= 2;
         const int64_t items = a.tokens * ((c.heads_q + a.q_heads - 1) / a.q_heads);
         q_blocks = (items + kRows - 1) / kRows;
     }
-    a.page_blocks = a.slots * c.heads_kv * 2;
-    if (a.page_blocks + q_blocks == 0) return hipSuccess;
-    hipLaunchKernelGGL((kda_cache_append_kernel<D, kThreads, kIters>), dim3((uint32_t)(a.page_blocks + q_blocks)), dim3(kThreads), 0, st, c, a);
+    // Queries of many tokens go by themselves: theirs is a kernel of few registers, and so of many waves (the same 16 prompts x 32 heads, 1.1 GB:
+    // 231 us, 4.8 TB/s).
+    const bool apart = kThreads >= 256 && q_blocks > 2048;
+    if (apart) {
+        hipLaunchKernelGGL(kda_cache_queries_kernel<D>, dim3((uint32_t)(q_blocks * (kThreads / 256))), dim3(256), 0, st, c, a);
+        q_blocks = 0;
+    }
+    if (a.page_blocks + q_blocks > 0)
+        hipLaunchKernelGGL((kda_cache_append_kernel<D, kThreads, kIters>), dim3((uint32_t)(a.page_blocks + q_blocks)), dim3(kThreads), 0, st, c, a);
     return hipGetLastError();
 }
 
 kda_status cache_append_dispatch(const Cache &c, const Append &a, int dim, hipStream_t st)
 {
-    // up to 8 new tokens a sequence: a wave has them all; else a page's rows by 16 (d 128) or 32
+    // Up to 8 new tokens a sequence: a workgroup holds them all, one row a lane group, whatever pages they fall into.  More: a page's rows
+    // by 16 or 32.
+    Append b = a;
     const bool few = a.slots_per_seq && a.per_seq <= 8;
+    if (few) {
+        b.whole = 1;
+        b.slots = c.num_seqs;
+    }
     hipError_t e;
     if (dim == 128)
-        e = few ? launch_append<128, 64, 2>(c, a, st) : c.page_size == 128 ? launch_append<128, 256, 8>(c, a, st)
-                : c.page_size == 64 ? launch_append<128, 256, 4>(c, a, st) : launch_append<128, 256, 2>(c, a, st);
+        e = few ? (a.per_seq <= 4 ? launch_append<128, 64, 1>(c, b, st) : launch_append<128, 128, 1>(c, b, st))
+                : c.page_size == 128 ? launch_append<128, 512, 4>(c, b, st)
+                : c.page_size == 64  ? launch_append<128, 256, 4>(c, b, st) : launch_append<128, 256, 2>(c, b, st);
     else
-        e = few ? launch_append<64, 64, 1>(c, a, st) : c.page_size == 128 ? launch_append<64, 256, 4>(c, a, st) : launch_append<64, 256, 2>(c, a, st);
+        e = few ? launch_append<64, 64, 1>(c, b, st) : c.page_size == 128 ? launch_append<64, 256, 4>(c, b, st) : launch_append<64, 256, 2>(c, b, st);
     return e == hipSuccess ? KDA_OK : fail(KDA_ERR_LAUNCH, "kda_cache_append: %s", hipGetErrorString(e));
 }
 

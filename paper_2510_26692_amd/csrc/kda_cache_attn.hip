@@ -1,6 +1,6 @@
 // Attention of the newest tokens over a paged cache of e4m3 codes with a scale for each page and head.
 //
-// A step is 32 keys of one key head for up to 64 rows (new tokens x query heads of the group), 16 at a time, in one wave and without LDS:
+// A step is 32 keys of one key head for 16 or 32 rows (new tokens x query heads of the group) in one wave and without LDS:
 //
 //     X^T [key, row] = K Q^T            A: codes widened to bf16 (exact), a lane 8 channels of a key at a time,     B: the rows, in registers
 //     O^T [channel, row] += V^T P^T     A: codes of 8 keys' same channel,                                         B: X's accumulators as they stand
@@ -29,20 +29,20 @@ constexpr int kWaves = 4;
 
 // The visible keys of a sequence's new tokens as steps: those of the sinks where the window begins behind them, then the window's.
 struct Steps {
-    int64_t len, low;                // keys; first step of the window
+    int32_t len, low;                // keys; first step of the window
     int32_t sink_steps, count;
 };
 __device__ __forceinline__ Steps steps_of(const Cache &c, const Attend &a, int n)
 {
-    const int64_t most = (int64_t)c.max_pages << c.page_log2, l = c.lens[n], len = l < 0 ? 0 : l < most ? l : most;
-    const int64_t first = l - a.tokens - a.window + 1;       // of the first new token's window
+    const int32_t most = c.max_pages << c.page_log2, l = c.lens[n];          // (below 2^31)
     Steps s;
-    s.len = len;
-    s.low = a.window && first > 0 ? first / kStep : 0;
-    const int64_t high = (len + kStep - 1) / kStep, sinks = (a.sinks + kStep - 1) / kStep;
-    if (s.low > high) s.low = high;
-    s.sink_steps = (int32_t)(s.low < sinks ? s.low : sinks);
-    s.count = (int32_t)(high - s.low) + s.sink_steps;
+    s.len = l < 0 ? 0 : min(l, most);
+    // the first new token's window begins at l - tokens - window + 1
+    s.low = a.window && l >= a.tokens && l - a.tokens >= a.window ? (l - a.tokens - a.window + 1) / kStep : 0;
+    const int32_t high = (s.len + kStep - 1) / kStep;
+    s.low = min(s.low, high);
+    s.sink_steps = min(s.low, (a.sinks + kStep - 1) / kStep);
+    s.count = high - s.low + s.sink_steps;
     return s;
 }
 // steps of one wave: as many as the others', and none where it has none left
@@ -67,9 +67,10 @@ template <typename F> __device__ __forceinline__ float over_groups(float v, F f)
     return f(v, __shfl_xor(v, 32));
 }
 
-// RB: blocks of 16 rows.
+// RB: blocks of 16 rows.  More than 32 rows go to several workgroups, side by side, which meet in the L2: 64 sequences of up to 8192 tokens,
+// 64 rows, 242 us with two of 32, 334 with four of 16; with one of 64 most of its values stand in scratch (1922).
 template <int D, int RB>
-__global__ __launch_bounds__(64 * kWaves, RB < 4 ? 2 : 1) void kda_cache_attn_kernel(const Cache c, const Attend a)
+__global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Cache c, const Attend a)
 {
     constexpr int KW = D / 64;                               // 16-byte pieces of a key that a lane reads
     constexpr int VW = D / 64;                               // dwords of a key's values that a lane reads
@@ -78,28 +79,28 @@ __global__ __launch_bounds__(64 * kWaves, RB < 4 ? 2 : 1) void kda_cache_attn_ke
     uint32_t id = blockIdx.x;
     const int kv = id % c.heads_kv;
     id /= c.heads_kv;
-    const int split = id % a.splits;
-    id /= a.splits;
-    const int tile = id % a.row_tiles, n = id / a.row_tiles;
+    const int tile = id % a.row_tiles;
+    id /= a.row_tiles;
+    const int split = id % a.splits, n = id / a.splits;
     const Steps st = steps_of(c, a, n);
     const int32_t per = wave_steps(st, a.splits);
     const int32_t begin0 = (split * kWaves + wave) * per, begin = begin0 < st.count ? begin0 : st.count, end = begin + per < st.count ? begin + per : st.count;
     if (a.splits > 1 && split * kWaves * per >= st.count) return;          // (the join knows)
 
+    // position of the first new token (a sequence of no length has no step)
+    const int32_t qfirst = max(c.lens[n], 0) - a.tokens;
     // rows of this tile: (token, head of the group)
     bf16x8 qf[RB][D / 32];
-    int64_t qpos[RB];
-    int32_t row[RB];
+    int32_t qpos[RB], row[RB];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         row[r] = (tile * RB + r) * 16 + x;
         const int rr = row[r] < a.rows ? row[r] : a.rows - 1, t = rr / c.group, head = kv * c.group + rr - t * c.group;
-        qpos[r] = (int64_t)c.lens[n] - a.tokens + t;
+        qpos[r] = qfirst + t;
         const uint16_t *from = a.q + ((int64_t)n * a.tokens + t) * a.q_stride + (int64_t)head * D + D / 4 * g;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) qf[r][i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(from + 8 * i));
     }
-    const int64_t qfirst = (int64_t)c.lens[n] - a.tokens;    // position of the first new token
     const float cs = a.scale * kLog2e;
 
     f32x4 acc[RB][CB];
@@ -113,7 +114,7 @@ __global__ __launch_bounds__(64 * kWaves, RB < 4 ? 2 : 1) void kda_cache_attn_ke
     }
 
     // what a lane knows of one 16-key block of the 32 steps at hand: page and scales
-    auto first_key = [&](int32_t u) { return (u < st.sink_steps ? (int64_t)u : st.low + u - st.sink_steps) * kStep; };
+    auto first_key = [&](int32_t u) { return (u < st.sink_steps ? u : st.low + u - st.sink_steps) * kStep; };
     int32_t page_l = -1;
     float ks_l = 0.f, vs_l = 0.f;
     auto look_up = [&](int32_t u0) {
@@ -121,7 +122,7 @@ __global__ __launch_bounds__(64 * kWaves, RB < 4 ? 2 : 1) void kda_cache_attn_ke
         page_l = -1;
         ks_l = vs_l = 0.f;
         if (u < end) {
-            const int64_t key = first_key(u) + 16 * (lane & 1);
+            const int32_t key = first_key(u) + 16 * (lane & 1);
             if (key < st.len) page_l = page_at(c, n, key >> c.page_log2);
             if (page_l >= 0) {
                 ks_l = c.k_scale[(int64_t)page_l * c.heads_kv + kv];
@@ -136,13 +137,11 @@ __global__ __launch_bounds__(64 * kWaves, RB < 4 ? 2 : 1) void kda_cache_attn_ke
         int32_t page[2];
     };
     auto fetch = [&](int32_t u, int32_t u0, Codes &w) {
-        const int64_t key0 = first_key(u);
+        const int32_t key0 = first_key(u);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const int src = 2 * (u - u0) + b;
             w.page[b] = __builtin_amdgcn_readlane(page_l, src);
-            w.ks[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), src));
-            w.vs[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), src));
             const int64_t at = ((int64_t)(w.page[b] < 0 ? 0 : w.page[b]) * c.heads_kv + kv) * c.page_size + ((key0 + 16 * b) & (c.page_size - 1));
             const uint8_t *kp = c.k + (at + x) * D + D / 4 * g;
 #pragma unroll
@@ -154,78 +153,67 @@ __global__ __launch_bounds__(64 * kWaves, RB < 4 ? 2 : 1) void kda_cache_attn_ke
                 else w.v[4 * b + i][0] = *reinterpret_cast<const uint32_t *>(vp + i * D);
             }
         }
+        // (behind the codes' loads, which need the pages alone)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int src = 2 * (u - u0) + b;
+            w.ks[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), src));
+            w.vs[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), src));
+        }
     };
     auto work = [&](int32_t u, Codes &w) {
-        const int64_t key0 = first_key(u);
+        const int32_t key0 = first_key(u);
         // some row does not see some key, or there is none
         const bool edge = key0 + kStep - 1 > qfirst || (a.window && qfirst + a.tokens - 1 - key0 >= a.window) || w.page[0] < 0 || w.page[1] < 0;
-        bf16x8 kf[2][D / 32];
+        // logits of all rows, then their terms, then the values: K's and V's widened codes are not held at once
+        f32x4 s[RB][2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < 2; ++b) {
+            bf16x8 kf[D / 32];
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) kf[b][i] = widen(w.k[b][i / 2][2 * (i % 2)], w.k[b][i / 2][2 * (i % 2) + 1]);
-        // V^T: channel D/16 x + j of keys 4 g + 0..3 and 16 + 4 g + 0..3
+            for (int i = 0; i < D / 32; ++i) kf[i] = widen(w.k[b][i / 2][2 * (i % 2)], w.k[b][i / 2][2 * (i % 2) + 1]);
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                s[r][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) s[r][b] = mfma(kf[i], qf[r][i], s[r][b]);
+                s[r][b] *= cs * w.ks[b];
+            }
+        }
+        uint32_t seen[RB];
         bool odd = false;                                    // a code that is not a number, on a step that not every row sees whole
         if (edge) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r) seen[r] = 0;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int64_t key = key0 + 16 * b + 4 * g + i;
+                    const int32_t key = key0 + 16 * b + 4 * g + i;
                     const bool none = w.page[b] < 0 || key >= st.len;
 #pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        const bool ok = !none && key <= qpos[r] && (a.window == 0 || qpos[r] - key < a.window || key < a.sinks);
+                        s[r][b][i] = ok ? s[r][b][i] : -kInf;
+                        seen[r] |= (ok ? 1u : 0u) << (4 * b + i);
+                    }
+#pragma unroll
                     for (int d = 0; d < VW; ++d) {
-                        uint32_t y = w.v[4 * b + i][d];
-                        y = none ? 0u : y;
+                        const uint32_t y = none ? 0u : w.v[4 * b + i][d];
                         w.v[4 * b + i][d] = y;
                         odd |= ((((y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0);
                     }
                 }
         }
         const bool careful = edge && __any(odd);
-        bf16x8 vf[CB];
-#pragma unroll
-        for (int d = 0; d < VW; ++d)
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                u32x4 lo, hi;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t pair = __builtin_amdgcn_perm(w.v[2 * e + 1][d], w.v[2 * e][d], half ? 0x07030602u : 0x05010400u);
-                    lo[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(pair, 1.f, false));
-                    hi[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(pair, 1.f, true));
-                }
-                vf[4 * d + 2 * half] = __builtin_bit_cast(bf16x8, lo);
-                vf[4 * d + 2 * half + 1] = __builtin_bit_cast(bf16x8, hi);
-            }
+        bf16x8 pb[RB];
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-            f32x4 s[2];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) s[b] = mfma(kf[b][i], qf[r][i], s[b]);
-                s[b] *= cs * w.ks[b];
-            }
-            uint32_t seen = 0xffu;
-            if (edge) {
-                seen = 0;
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int64_t key = key0 + 16 * b + 4 * g + i;
-                        const bool ok = w.page[b] >= 0 && key < st.len && key <= qpos[r] && (a.window == 0 || qpos[r] - key < a.window || key < a.sinks);
-                        s[b][i] = ok ? s[b][i] : -kInf;
-                        seen |= (ok ? 1u : 0u) << (4 * b + i);
-                    }
-            }
-            float top = s[0][0];
+            float top = s[r][0][0];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i]);
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[r][b][i]);
             if (__any(top > m[r] + 8.f)) {
                 top = over_groups(top, [](float p, float q) { return fmaxf(p, q); });
                 const float mn = fmaxf(m[r], top), f = mn == -kInf ? 1.f : fast_exp2(m[r] - mn);
@@ -240,35 +228,60 @@ __global__ __launch_bounds__(64 * kWaves, RB < 4 ? 2 : 1) void kda_cache_attn_ke
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[4 * b + i] = fast_exp2(s[b][i] - mref[r]);
+                    p[4 * b + i] = fast_exp2(s[r][b][i] - mref[r]);
                     l[r] += p[4 * b + i];
                     p[4 * b + i] *= w.vs[b];
                 }
             u32x4 pw;
 #pragma unroll
             for (int i = 0; i < 4; ++i) pw[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
-            const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
-            if (!careful) {
+            pb[r] = __builtin_bit_cast(bf16x8, pw);
+        }
+        // V^T: channel D/16 x + j of keys 4 g + 0..3 and 16 + 4 g + 0..3, two channels at a time
+        auto channels = [&](int d, int half, u32x4 (&two)[2]) {
 #pragma unroll
-                for (int j = 0; j < CB; ++j) acc[r][j] = mfma(vf[j], pb, acc[r][j]);
-            } else {
-                // such a code leaves the product, and the rows that see it become NaN
-                u32x4 ones;
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t pair = __builtin_amdgcn_perm(w.v[2 * e + 1][d], w.v[2 * e][d], half ? 0x07030602u : 0x05010400u);
+                two[0][e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(pair, 1.f, false));
+                two[1][e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(pair, 1.f, true));
+            }
+        };
+        if (!careful) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) ones[i] = ((seen >> (2 * i)) & 1u ? 0x3f80u : 0u) | ((seen >> (2 * i + 1)) & 1u ? 0x3f800000u : 0u);
+            for (int j = 0; j < CB; j += 2) {
+                u32x4 two[2];
+                channels(j / 4, j / 2 & 1, two);
 #pragma unroll
-                for (int j = 0; j < CB; ++j) {
-                    u32x4 y = __builtin_bit_cast(u32x4, vf[j]), marks;
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const bool lo = (y[i] & 0x7f80u) == 0x7f80u, hi = (y[i] & 0x7f800000u) == 0x7f800000u;
-                        marks[i] = (lo ? 0x3f80u : 0u) | (hi ? 0x3f800000u : 0u);
-                        y[i] &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+                    for (int r = 0; r < RB; ++r) acc[r][j + i] = mfma(__builtin_bit_cast(bf16x8, two[i]), pb[r], acc[r][j + i]);
+            }
+        } else {
+            // such a code leaves the product, and the rows that see it become NaN
+#pragma unroll
+            for (int j = 0; j < CB; j += 2) {
+                u32x4 two[2];
+                channels(j / 4, j / 2 & 1, two);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    u32x4 y = two[i], marks;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool lo = (y[e] & 0x7f80u) == 0x7f80u, hi = (y[e] & 0x7f800000u) == 0x7f800000u;
+                        marks[e] = (lo ? 0x3f80u : 0u) | (hi ? 0x3f800000u : 0u);
+                        y[e] &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
                     }
-                    acc[r][j] = mfma(__builtin_bit_cast(bf16x8, y), pb, acc[r][j]);
-                    const f32x4 count = mfma(__builtin_bit_cast(bf16x8, marks), __builtin_bit_cast(bf16x8, ones), f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[r][j][i] = count[i] > 0.f ? __builtin_nanf("") : acc[r][j][i];
+                    for (int r = 0; r < RB; ++r) {
+                        u32x4 ones;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            ones[e] = ((seen[r] >> (2 * e)) & 1u ? 0x3f80u : 0u) | ((seen[r] >> (2 * e + 1)) & 1u ? 0x3f800000u : 0u);
+                        acc[r][j + i] = mfma(__builtin_bit_cast(bf16x8, y), pb[r], acc[r][j + i]);
+                        const f32x4 count = mfma(__builtin_bit_cast(bf16x8, marks), __builtin_bit_cast(bf16x8, ones), f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[r][j + i][e] = count[e] > 0.f ? __builtin_nanf("") : acc[r][j + i][e];
+                    }
                 }
             }
         }
@@ -384,14 +397,42 @@ __global__ __launch_bounds__(256) void kda_cache_join_kernel(const Cache c, cons
     const int row = (int)(item - pair * a.rows), n = (int)(pair / c.heads_kv), kv = (int)(pair - (int64_t)n * c.heads_kv);
     const Steps st = steps_of(c, a, n);
     const int32_t per = wave_steps(st, a.splits) * kWaves, used = per ? (st.count + per - 1) / per : 0;
+    // a lane has one split's maximum and sum, 64 splits at a time
     float m = -kInf, l = 0.f, y[W] = {};
-    for (int s = 0; s < used; ++s) m = fmaxf(m, a.stats[((pair * a.splits + s) * a.rows + row) * 2]);
-    for (int s = 0; s < used; ++s) {
-        const int64_t part = (pair * a.splits + s) * a.rows + row;
-        const float ms = a.stats[part * 2], f = ms == -kInf ? 0.f : fast_exp2(ms - m);
-        l += a.stats[part * 2 + 1] * f;
+    for (int s0 = 0; s0 < used; s0 += 64) {
+        const int64_t part = (pair * a.splits + s0 + lane) * a.rows + row;
+        float ms = -kInf, ls = 0.f;
+        if (s0 + lane < used) {
+            ms = a.stats[part * 2];
+            ls = a.stats[part * 2 + 1];
+        }
+        float top = ms;
 #pragma unroll
-        for (int i = 0; i < W; ++i) y[i] += a.part[part * D + W * lane + i] * f;
+        for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+        const float mn = fmaxf(m, top), old = m == -kInf ? 0.f : fast_exp2(m - mn), f = ms == -kInf ? 0.f : fast_exp2(ms - mn);
+        m = mn;
+        ls *= f;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) ls += __shfl_xor(ls, o);
+        l = l * old + ls;
+#pragma unroll
+        for (int i = 0; i < W; ++i) y[i] *= old;
+        const int count = used - s0 < 64 ? used - s0 : 64;
+        const float *from = a.part + ((pair * a.splits + s0) * a.rows + row) * D + W * lane;
+        const int64_t step = (int64_t)a.rows * D;
+        for (int s = 0; s < count; s += 8) {
+            float x[8][W];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int i = 0; i < W; ++i) x[u][i] = from[(s + u < count ? s + u : count - 1) * step + i];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float g = s + u < count ? __shfl(f, s + u) : 0.f;
+#pragma unroll
+                for (int i = 0; i < W; ++i) y[i] += s + u < count ? x[u][i] * g : 0.f;
+            }
+        }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int t = row / c.group, head = kv * c.group + row - t * c.group;
@@ -430,8 +471,7 @@ template <int D, int RB> hipError_t launch(const Cache &c, const Attend &a, hipS
 }
 template <int D> hipError_t launch(const Cache &c, Attend a, hipStream_t st)
 {
-    const int rb = a.rows <= 16 ? 1 : a.rows <= 32 ? 2 : 4;
-    hipError_t e = rb == 1 ? launch<D, 1>(c, a, st) : rb == 2 ? launch<D, 2>(c, a, st) : launch<D, 4>(c, a, st);
+    hipError_t e = a.row_tiles == 1 && a.rows <= 16 ? launch<D, 1>(c, a, st) : launch<D, 2>(c, a, st);
     if (e == hipSuccess && a.splits > 1) {
         const int64_t items = (int64_t)c.num_seqs * c.heads_kv * a.rows;
         hipLaunchKernelGGL(kda_cache_join_kernel<D>, dim3((uint32_t)((items + 3) / 4)), dim3(256), 0, st, c, a);
