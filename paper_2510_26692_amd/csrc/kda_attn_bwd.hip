@@ -37,7 +37,7 @@ __device__ __forceinline__ int first_walk_tiles(const Shape &s, int len)
     return own < all ? own : all;
 }
 
-// dQ of 128 queries.  Returns true, with nothing written, where the walk has to be repeated with care.
+// dQ of 128 queries.  Returns true where the walk has to be repeated with care.
 template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Shape &s, const Back &g, const uint32_t lds)
 {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, x = lane & 31, h = lane >> 5;
@@ -73,7 +73,6 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
     }
     delta += other_half(delta);
     const float lse = g.lse[stat], lse2 = lse == -kInf ? kInf : lse * kLog2e;
-    if (query < at.len) g.stats[stat + (h ? stats_size(s) : 0)] = h ? delta : lse2;
 
     arrived(qf);
     arrived(df);
@@ -95,6 +94,9 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
         lv.issue(lds + (2 * buf + 1) * kT, wave, rows_descriptor(vh + k0 * s.v_stride, at.len - k0, vs_bytes));
     };
 
+    // The sum of a row's dS is zero but for what o's rounding took from d: added to d, it gives the dK / dV walk the d of the unrounded o
+    // (errors of dK 2.5e-3 to 2.8e-3 without, 2.4e-3 with).
+    float rest = 0.f;
     f32x16 acc[D / 32];
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) acc[db] = zeros16();
@@ -129,6 +131,10 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
 #pragma unroll
                 for (int j = 0; j < 16; ++j) e[j] = where_seen(seen_bit(seen.w[b], j), e[j], 0.f);
             }
+            float four[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) four[j] = (e[j] + e[4 + j]) + (e[8 + j] + e[12 + j]);
+            rest += (four[0] + four[1]) + (four[2] + four[3]);
             const bf16x8 ds[2] = {pack8(e), pack8(e + 8)};
             if (kCareful && edge) {
 #pragma unroll
@@ -146,18 +152,26 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
         step(it, std::integral_constant<int, 0>{});
         if (it + 1 < steps) step(it + 1, std::integral_constant<int, 1>{});
     }
-    if (!kCareful && repeat(acc, acc, lds)) return true;
-    if (query >= at.len) return false;
-    uint16_t *out = g.dq + (token * s.heads_q + head) * D;
+    rest += other_half(rest);
+    // (formed again: held through the walk these would take registers from it)
+    int again = tid;
+    asm volatile("" : "+v"(again));
+    const int mine = wq0 + (again & 31);
+    const bool bad = !kCareful && not_finite(acc);
+    if (mine < at.len) {
+        const int64_t place = at.row0 + mine;
+        g.stats[((int64_t)at.batch * (s.heads_q - 1) + head) * s.tokens + place + (again & 32 ? stats_size(s) : 0)] = again & 32 ? delta + rest : lse2;
+        uint16_t *out = g.dq + (place * s.heads_q + head) * D + (again & 32) / 8;
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const u32x2 y = {pack_bf16x2(acc[db][4 * b] * s.scale, acc[db][4 * b + 1] * s.scale),
-                             pack_bf16x2(acc[db][4 * b + 2] * s.scale, acc[db][4 * b + 3] * s.scale)};
-            *reinterpret_cast<u32x2 *>(out + 32 * db + 8 * b + 4 * h) = y;
-        }
-    return false;
+            for (int b = 0; b < 4; ++b) {
+                const u32x2 y = {pack_bf16x2(acc[db][4 * b] * s.scale, acc[db][4 * b + 1] * s.scale),
+                                 pack_bf16x2(acc[db][4 * b + 2] * s.scale, acc[db][4 * b + 3] * s.scale)};
+                *reinterpret_cast<u32x2 *>(out + 32 * db + 8 * b) = y;
+            }
+    }
+    return !kCareful && repeat(bad, lds);
 }
 // The walk with care is a call at d 128, where in line it takes registers from the loop that always runs (dK / dV: 78 spilled without it,
 // 261 with it); at d 64 there are enough, and the call's stack costs more (us in line / called, d 64: 8 x 4096 x 32 heads 2290 / 2370,
@@ -351,35 +365,39 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dkv_tile(const S
             }
         }
     }
-    if (!kCareful && repeat(dk, dv, lds)) return true;
-    if (!sink && key >= at.len) return false;
-    const int64_t row = (token * s.heads_kv + kv) * D;
+    int again = tid;                                         // (as in dq_tile)
+    asm volatile("" : "+v"(again));
+    const bool bad = !kCareful && (not_finite(dk) || not_finite(dv));
+    const int mine = kw0 + (again & 31), half = again & 32;
+    if (sink || mine < at.len) {
+        const int64_t row = ((at.row0 + mine) * s.heads_kv + kv) * D;
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int ch = 32 * db + 8 * b + 4 * h;
-            f32x4 yk, yv;
+            for (int b = 0; b < 4; ++b) {
+                const int ch = 32 * db + 8 * b + half / 8;
+                f32x4 yk, yv;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                yk[j] = dk[db][4 * b + j] * s.scale;
-                yv[j] = dv[db][4 * b + j];
+                for (int j = 0; j < 4; ++j) {
+                    yk[j] = dk[db][4 * b + j] * s.scale;
+                    yv[j] = dv[db][4 * b + j];
+                }
+                if (sink) {
+                    const int64_t w = ((((int64_t)slot * 2 + (wave >> 1)) * g.splits + sub) * s.heads_kv + kv) * kTile * D + (int64_t)mine * D + ch;
+                    *reinterpret_cast<f32x4 *>(g.sink_k + w) = yk;
+                    *reinterpret_cast<f32x4 *>(g.sink_v + w) = yv;
+                } else if (g.direct) {
+                    const u32x2 wk = {pack_bf16x2(yk[0], yk[1]), pack_bf16x2(yk[2], yk[3])}, wv = {pack_bf16x2(yv[0], yv[1]), pack_bf16x2(yv[2], yv[3])};
+                    *reinterpret_cast<u32x2 *>(g.dk + row + ch) = wk;
+                    *reinterpret_cast<u32x2 *>(g.dv + row + ch) = wv;
+                } else {
+                    const int64_t w = (int64_t)sub * part_size(s, D) + row + ch;
+                    *reinterpret_cast<f32x4 *>(g.part_k + w) = yk;
+                    *reinterpret_cast<f32x4 *>(g.part_v + w) = yv;
+                }
             }
-            if (sink) {
-                const int64_t w = ((((int64_t)slot * 2 + (wave >> 1)) * g.splits + sub) * s.heads_kv + kv) * kTile * D + (int64_t)key * D + ch;
-                *reinterpret_cast<f32x4 *>(g.sink_k + w) = yk;
-                *reinterpret_cast<f32x4 *>(g.sink_v + w) = yv;
-            } else if (g.direct) {
-                const u32x2 wk = {pack_bf16x2(yk[0], yk[1]), pack_bf16x2(yk[2], yk[3])}, wv = {pack_bf16x2(yv[0], yv[1]), pack_bf16x2(yv[2], yv[3])};
-                *reinterpret_cast<u32x2 *>(g.dk + row + ch) = wk;
-                *reinterpret_cast<u32x2 *>(g.dv + row + ch) = wv;
-            } else {
-                const int64_t w = (int64_t)sub * part_size(s, D) + row + ch;
-                *reinterpret_cast<f32x4 *>(g.part_k + w) = yk;
-                *reinterpret_cast<f32x4 *>(g.part_v + w) = yv;
-            }
-        }
-    return false;
+    }
+    return !kCareful && repeat(bad, lds);
 }
 template <int D> __device__ __noinline__ void dkv_tile_again(const Shape s, const Back g, const uint32_t lds) { dkv_tile<D, true>(s, g, lds); }
 template <int D> __global__ __launch_bounds__(kThreads, 2) void kda_attn_dkv_kernel(const Shape s, const Back g)

@@ -16,18 +16,16 @@ namespace attn {
 // two: 8 x 4096 x 32 causal 648 / 681, 32768 x 16, window 256: 83 / 100.
 template <int D> constexpr int kFwdKeys = D == 128 ? 32 : 64;
 
-template <int D, bool kOutBf16>
-__global__ __launch_bounds__(kThreads, 3) void kda_attn_fwd_kernel(const Shape s, const uint16_t *q, const uint16_t *k, const uint16_t *v,
-                                                                  void *o, float *lse)
+// o and lse of 128 queries.  Returns true where the walk has to be repeated with care.
+template <int D, bool kOutBf16, bool kCareful>
+__device__ __forceinline__ bool fwd_tile(const Shape &s, const uint16_t *q, const uint16_t *k, const uint16_t *v, void *o, float *lse, const uint32_t lds)
 {
-    extern __shared__ __align__(16) uint8_t lds_raw[];
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds_raw;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, x = lane & 31, h = lane >> 5;
     uint32_t slot, kv, sub;
     split_block(blockIdx.x, s.heads_kv, s.group, slot, kv, sub);
     const int head = kv * s.group + sub;
     const Place at = place_of(s, s.slots - 1 - slot);
-    if (at.first >= at.len || at.first < 0) return;
+    if (at.first >= at.len || at.first < 0) return false;
 
     const int wq0 = at.first + 32 * wave;                                 // the wave's first query
     const int query = wq0 + x, last = min(at.first + kCols - 1, at.len - 1);
@@ -71,111 +69,123 @@ __global__ __launch_bounds__(kThreads, 3) void kda_attn_fwd_kernel(const Shape s
 
     f32x16 acc[D / 32];
     float m, mref, l;
-    auto walk = [&](auto careful) {
-        constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) acc[db] = zeros16();
-        m = -kInf;
-        mref = 0.f;
-        l = 0.f;
-        auto step = [&](int it, auto parity) {
-            constexpr int P = decltype(parity)::value;
-            tile_barrier();
-            if (it + 1 < steps) issue(it + 1, P ^ 1);
-            const int k0 = first_key(it);
-            const uint32_t kt = lds + 2 * P * kT, vt = kt + kT;
-            if (!needed(k0)) return;
-            const bool edge = partial(k0);
-            f32x16 st[kKeys / 32];
+    for (int db = 0; db < D / 32; ++db) acc[db] = zeros16();
+    m = -kInf;
+    mref = 0.f;
+    l = 0.f;
+    auto step = [&](int it, auto parity) {
+        constexpr int P = decltype(parity)::value;
+        tile_barrier();
+        if (it + 1 < steps) issue(it + 1, P ^ 1);
+        const int k0 = first_key(it);
+        const uint32_t kt = lds + 2 * P * kT, vt = kt + kT;
+        if (!needed(k0)) return;
+        const bool edge = partial(k0);
+        f32x16 st[kKeys / 32];
 #pragma unroll
-            for (int b = 0; b < kKeys / 32; ++b) st[b] = zeros16();
+        for (int b = 0; b < kKeys / 32; ++b) st[b] = zeros16();
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i)
+        for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                for (int b = 0; b < kKeys / 32; ++b) st[b] = mfma(rd.rows(kt, b, i), qf[i], st[b]);
-            Seen seen;
-            if (edge) {
-                seen = seen_keys(query, k0, s.window, s.sinks);
-#pragma unroll
-                for (int b = 0; b < kKeys / 32; ++b) {
-                    seen.w[b] >>= 4 * h;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) st[b][j] = where_seen(seen_bit(seen.w[b], j), st[b][j], -kInf);
-                }
-            }
-            float top = st[0][0];
-#pragma unroll
-            for (int b = 0; b < kKeys / 32; ++b)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) top = fmaxf(top, st[b][j]);
-            top = fmaxf(top, other_half(top)) * c;
-            if (__any(top > m + 8.f)) {
-                const float mn = fmaxf(m, top), f = mn == -kInf ? 1.f : fast_exp2(m - mn);
-                m = mn;
-                mref = mn == -kInf ? 0.f : mn;
-                l *= f;
-#pragma unroll
-                for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[db][j] *= f;
-            }
-            bf16x8 p[kKeys / 16];
+            for (int b = 0; b < kKeys / 32; ++b) st[b] = mfma(rd.rows(kt, b, i), qf[i], st[b]);
+        Seen seen;
+        if (edge) {
+            seen = seen_keys(query, k0, s.window, s.sinks);
 #pragma unroll
             for (int b = 0; b < kKeys / 32; ++b) {
-                float e[16];
+                seen.w[b] >>= 4 * h;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    e[j] = fast_exp2(fmaf(st[b][j], c, -mref));
-                    l += e[j];
-                }
-                p[2 * b] = pack8(e);
-                p[2 * b + 1] = pack8(e + 8);
+                for (int j = 0; j < 16; ++j) st[b][j] = where_seen(seen_bit(seen.w[b], j), st[b][j], -kInf);
             }
-            if (kCareful && edge) {
-#pragma unroll
-                for (int db = 0; db < D / 32; ++db) careful_product<D, kKeys / 16>(acc[db], rd, vt, db, 0, p, seen.w);
-            } else {
-#pragma unroll
-                for (int ks = 0; ks < kKeys / 16; ++ks)
-#pragma unroll
-                    for (int db = 0; db < D / 32; ++db) acc[db] = mfma(rd.transposed(vt, db, ks), p[ks], acc[db]);
-            }
-        };
-        int it = 0;
-        for (; it + 1 < steps; it += 2) {
-            step(it, std::integral_constant<int, 0>{});
-            step(it + 1, std::integral_constant<int, 1>{});
         }
-        if (it < steps) step(it, std::integral_constant<int, 0>{});
+        float top = st[0][0];
+#pragma unroll
+        for (int b = 0; b < kKeys / 32; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, st[b][j]);
+        top = fmaxf(top, other_half(top)) * c;
+        if (__any(top > m + 8.f)) {
+            const float mn = fmaxf(m, top), f = mn == -kInf ? 1.f : fast_exp2(m - mn);
+            m = mn;
+            mref = mn == -kInf ? 0.f : mn;
+            l *= f;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[db][j] *= f;
+        }
+        bf16x8 p[kKeys / 16];
+#pragma unroll
+        for (int b = 0; b < kKeys / 32; ++b) {
+            float e[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                e[j] = fast_exp2(fmaf(st[b][j], c, -mref));
+                l += e[j];
+            }
+            p[2 * b] = pack8(e);
+            p[2 * b + 1] = pack8(e + 8);
+        }
+        if (kCareful && edge) {
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) careful_product<D, kKeys / 16>(acc[db], rd, vt, db, 0, p, seen.w);
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < kKeys / 16; ++ks)
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db) acc[db] = mfma(rd.transposed(vt, db, ks), p[ks], acc[db]);
+        }
     };
-    walk(std::false_type{});
-    if (repeat(acc, acc, lds)) {
-        issue(0, 0);
-        walk(std::true_type{});
+    int it = 0;
+    for (; it + 1 < steps; it += 2) {
+        step(it, std::integral_constant<int, 0>{});
+        step(it + 1, std::integral_constant<int, 1>{});
     }
+    if (it < steps) step(it, std::integral_constant<int, 0>{});
 
     l += other_half(l);
-    if (query >= at.len) return;
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : __builtin_nanf("");
-    const int64_t token = at.row0 + query;
-    if (lse && h == 0) lse[((int64_t)at.batch * s.heads_q + head) * s.tokens + token - (int64_t)at.batch * s.tokens] = l == 0.f ? -kInf : (mref + __log2f(l)) * 0.6931471805599453f;
-    const int64_t out = (token * s.heads_q + head) * D;
+    // (formed again: held through the walk these would take registers from it)
+    int again = tid;
+    asm volatile("" : "+v"(again));
+    const bool bad = !kCareful && not_finite(acc);
+    const int mine = wq0 + (again & 31), half = again & 32;
+    if (mine < at.len) {
+        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : __builtin_nanf("");
+        const int64_t token = at.row0 + mine;
+        if (lse && !half) lse[((int64_t)at.batch * (s.heads_q - 1) + head) * s.tokens + token] = l == 0.f ? -kInf : (mref + __log2f(l)) * 0.6931471805599453f;
+        const int64_t out = (token * s.heads_q + head) * D + half / 8;
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            float e[4];
+            for (int b = 0; b < 4; ++b) {
+                float e[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = acc[db][4 * b + j] * inv;
-            const int64_t w = out + 32 * db + 8 * b + 4 * h;
-            if constexpr (kOutBf16) {
-                const u32x2 y = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3])};
-                *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(o) + w) = y;
-            } else {
-                const f32x4 y = {e[0], e[1], e[2], e[3]};
-                *reinterpret_cast<f32x4 *>(static_cast<float *>(o) + w) = y;
+                for (int j = 0; j < 4; ++j) e[j] = acc[db][4 * b + j] * inv;
+                const int64_t w = out + 32 * db + 8 * b;
+                if constexpr (kOutBf16) {
+                    const u32x2 y = {pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3])};
+                    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(o) + w) = y;
+                } else {
+                    const f32x4 y = {e[0], e[1], e[2], e[3]};
+                    *reinterpret_cast<f32x4 *>(static_cast<float *>(o) + w) = y;
+                }
             }
-        }
+    }
+    return !kCareful && repeat(bad, lds);
+}
+template <int D, bool kOutBf16>
+__device__ __noinline__ void fwd_tile_again(const Shape s, const uint16_t *q, const uint16_t *k, const uint16_t *v, void *o, float *lse, const uint32_t lds)
+{
+    fwd_tile<D, kOutBf16, true>(s, q, k, v, o, lse, lds);
+}
+template <int D, bool kOutBf16>
+__global__ __launch_bounds__(kThreads, 3) void kda_attn_fwd_kernel(const Shape s, const uint16_t *q, const uint16_t *k, const uint16_t *v, void *o, float *lse)
+{
+    extern __shared__ __align__(16) uint8_t lds_raw[];
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds_raw;
+    if (!fwd_tile<D, kOutBf16, false>(s, q, k, v, o, lse, lds)) return;
+    fwd_tile_again<D, kOutBf16>(s, q, k, v, o, lse, lds);
 }
 
 }  // namespace attn

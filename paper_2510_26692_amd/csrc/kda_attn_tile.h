@@ -299,18 +299,23 @@ __device__ __forceinline__ void careful_product(f32x16 &y, const TileReader<D> &
     for (int j = 0; j < 16; ++j) y[j] = count[j] > 0.f ? __builtin_nanf("") : y[j];
 }
 
-// Whether any sum of the workgroup is not finite (0 times an infinity or NaN is NaN): the walk is then repeated with care.  LDS is
-// free when this is called, and when it returns.
-template <int N> __device__ __forceinline__ bool repeat(const f32x16 (&a)[N], const f32x16 (&b)[N], uint32_t lds)
+// Whether a sum of the lane is not finite: 0 times an infinity or NaN is NaN.
+template <int N> __device__ __forceinline__ bool not_finite(const f32x16 (&a)[N])
 {
-    float sum = 0.f;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sum += &a == &b ? a[i][j] * 0.f : (a[i][j] + b[i][j]) * 0.f;
+        for (int j = 0; j < 16; ++j) sum[j & 3] = fmaf(a[i][j], 0.f, sum[j & 3]);
+    return !((sum[0] + sum[1]) + (sum[2] + sum[3]) == 0.f);
+}
+// Whether that is so anywhere in the workgroup: its walk is then repeated with care, and what it has stored stored again.  LDS is free when this
+// is called, and when it returns.
+__device__ __forceinline__ bool repeat(bool bad, uint32_t lds)
+{
     typedef __attribute__((address_space(3))) uint32_t *lds_u1;
     typedef __attribute__((address_space(3))) u32x4 *lds_w4;
-    const uint32_t any = __any(!(sum == 0.f));
+    const uint32_t any = __any(bad);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) *reinterpret_cast<lds_u1>(lds + (threadIdx.x >> 4)) = any;
     __syncthreads();
