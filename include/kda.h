@@ -397,7 +397,7 @@ kda_status kda_clear_unowned_rows(const int32_t *cu_seqlens, int32_t num_seqs, i
  */
 typedef struct {
     int32_t   batch;       /* B                                                                        */
-    int64_t   seqlen;      /* T per batch row, or total packed tokens (as in kda_dims)                  */
+    int64_t   seqlen;      /* T per batch row, or total packed tokens (as in kda_dims), at most 2^30    */
     int32_t   heads_q, heads_kv;
     int32_t   dim;         /* head dimension of q, k and v: 64 or 128                                   */
     int32_t   num_seqs;    /* N: == batch, or the sequences of a packed batch                           */
@@ -417,7 +417,7 @@ typedef struct {
  *   o          [B,T,heads_q,dim]   out_dtype; rows of tokens owned by no sequence are left untouched
  *   lse        [B,heads_q,T]       fp32: log sum_j exp(scale q_i . k_j) over the keys that i sees, or NULL
  * Products on the bf16 matrix cores with fp32 accumulation, softmax statistics in fp32, its terms rounded to bf16 ahead of the
- * product with v.  Values that are not finite reach the outputs of the queries that see them and no others: a query that sees a
+ * product with v.  o must not alias an input.  Values that are not finite reach the outputs of the queries that see them and no others: a query that sees a
  * value of v that is not finite gets NaN or an infinity there, in every channel concerned, one that sees a key that is not
  * finite, or is not finite itself, NaN.  (Such a tile is worked through twice.)  No workspace.
  */
@@ -458,7 +458,7 @@ typedef struct {
     int32_t  dim;                  /* 64 or 128                                                               */
     int32_t  page_size;            /* 16, 32, 64 or 128                                                       */
     int64_t  num_pages;
-    int32_t  max_pages;            /* columns of block_table; max_pages * page_size below 2^31                */
+    int32_t  max_pages;            /* columns of block_table; max_pages * page_size at most 2^30              */
     void    *k, *v;
     float   *k_scale, *v_scale;
     const int32_t *block_table, *kv_lens;
@@ -481,7 +481,8 @@ typedef struct {
  *   k, v           [..,heads_kv,dim]   bf16, [num_seqs,seqlen] or packed rows; strides in elements from a token to the next as in kda_attn_dims
  *   rope           rotation of k (and q), or NULL: as they are
  *   k_out          [..,heads_kv,dim]   bf16: the rotated keys, for a prefill that follows, or NULL
- *   q, q_out       [..,heads_q,dim]    bf16: queries to be rotated at their tokens' positions, and where to; NULL both or neither
+ *   q, q_out       [..,heads_q,dim]    bf16: queries to be rotated at their tokens' positions, and where to; NULL both or neither.  k_out may
+ *                  be k and q_out q, where those are contiguous
  * Scales: powers of two.  A page and head's scale is the smallest (2^-100 at least) with which its largest new value is at most 448 codes'
  * steps, or the one it has, if that is larger and the page holds older tokens; where it grows, the older tokens' codes are rounded again
  * to the new scale.  Codes are rounded to nearest even from the fp32 rotation; values that are not finite are stored as NaN and leave the

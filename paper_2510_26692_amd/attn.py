@@ -62,14 +62,16 @@ def _native(name, *args):
 
 
 def _token_stride(t, name):
-    """Elements from a token of t [B,T,H,d] to the next: heads and channels contiguous, tokens evenly spaced over the whole batch."""
+    """Elements from a token of t [B,T,H,d] to the next: heads and channels contiguous, tokens evenly spaced over the whole batch.
+    0: contiguous."""
     B, T, H, d = t.shape
     sb, st, sh, sd = t.stride()
     if t.numel() == 0 or t.is_contiguous():
         return 0
-    if (d > 1 and sd != 1) or (H > 1 and sh != d) or (B > 1 and T > 1 and sb != T * st):
+    step = st if T > 1 else sb if B > 1 else H * d
+    if (d > 1 and sd != 1) or (H > 1 and sh != d) or (B > 1 and T > 1 and sb != T * st) or step < H * d:
         raise ValueError("%s: heads and channels must be contiguous, and tokens evenly spaced" % name)
-    return st if T > 1 else sb if B > 1 else 0
+    return step
 
 
 def _device(*tensors):

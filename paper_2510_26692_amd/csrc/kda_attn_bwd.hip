@@ -7,6 +7,7 @@
 // of every sum is fixed.  A key head's gradients sum over its group's query heads inside a workgroup; where that leaves too few
 // workgroups, over parts of the group, whose fp32 sums a last kernel adds.  The sinks' keys are seen by every later query: what lies beyond
 // their window is walked by workgroups of its own, in parts.
+#include <algorithm>
 #include <type_traits>
 
 #include "kda_attn_tile.h"
@@ -410,12 +411,9 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void kda_attn_dkv_ker
 }
 
 // Sums of the parts: a thread has four channels of a token and key head.
-template <int D>
-__global__ __launch_bounds__(256) void kda_attn_join_kernel(const Shape s, const Back g, int64_t tokens)
+template <int D> __device__ __forceinline__ void join_four(const Shape &s, const Back &g, int64_t i)
 {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     const int64_t token = i / ((int64_t)D * s.heads_kv);
-    if (token >= tokens) return;
     int64_t index = token, first_slot = 0, len = s.tokens;
     if (s.cu) {
         int lo = 0, hi = s.num_seqs - 1;
@@ -451,6 +449,12 @@ __global__ __launch_bounds__(256) void kda_attn_join_kernel(const Shape s, const
     const u32x2 wk = {pack_bf16x2(yk[0], yk[1]), pack_bf16x2(yk[2], yk[3])}, wv = {pack_bf16x2(yv[0], yv[1]), pack_bf16x2(yv[2], yv[3])};
     *reinterpret_cast<u32x2 *>(g.dk + i) = wk;
     *reinterpret_cast<u32x2 *>(g.dv + i) = wv;
+}
+template <int D>
+__global__ __launch_bounds__(256) void kda_attn_join_kernel(const Shape s, const Back g, int64_t tokens)
+{
+    const int64_t all = tokens * s.heads_kv * D, step = (int64_t)gridDim.x * 1024;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < all; i += step) join_four<D>(s, g, i);
 }
 
 }  // namespace attn
@@ -505,7 +509,7 @@ template <int D> hipError_t launch_bwd(const Shape &s, Back g, const Plan &p, hi
     hipLaunchKernelGGL(kda_attn_dkv_kernel<D>, dim3(((uint32_t)s.slots + p.sink_slots) * per_slot), dim3(kThreads), kLdsStats, st, s, g);
     if (!p.direct) {
         const int64_t tokens = rows_of(s), threads = tokens * s.heads_kv * (D / 4);
-        hipLaunchKernelGGL(kda_attn_join_kernel<D>, dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, st, s, g, tokens);
+        hipLaunchKernelGGL(kda_attn_join_kernel<D>, dim3((uint32_t)std::min<int64_t>((threads + 255) / 256, 1 << 20)), dim3(256), 0, st, s, g, tokens);
     }
     return hipGetLastError();
 }

@@ -32,6 +32,7 @@ kda_status check(const kda_cache *d, bool buffers, cache::Cache &c)
     if (d->heads_q > 65535) return fail(KDA_ERR_UNSUPPORTED, "heads_q > 65535");
     if (d->heads_q && (d->heads_kv == 0 || d->heads_q % d->heads_kv))
         return fail(KDA_ERR_INVALID_ARG, "heads_q (%d) must be a multiple of heads_kv (%d)", d->heads_q, d->heads_kv);
+    if ((int64_t)d->max_pages * d->page_size > 1 << 30) return fail(KDA_ERR_UNSUPPORTED, "more than 2^30 tokens a sequence (max_pages %d)", d->max_pages);
     if (d->num_pages > 0x7fffffffLL) return fail(KDA_ERR_INVALID_ARG, "num_pages exceeds the int32 range of block_table");
     c = {};
     c.num_pages = d->num_pages;
@@ -83,7 +84,8 @@ kda_status check(const kda_cache *d, bool buffers, const kda_cache_query *q, cac
     const int64_t pairs = (int64_t)c.num_seqs * c.heads_kv, held = (int64_t)d->max_pages * d->page_size;
     const int64_t most = q->max_kv_len && q->max_kv_len < held ? q->max_kv_len : held;
     a.splits = pairs && a.rows ? cache_attn_splits(c, pairs * a.row_tiles, most, a.window, a.sinks, a.tokens) : 1;
-    if (pairs * a.row_tiles * a.splits > 0x7fffffffLL || held > 0x7fffffffLL) return fail(KDA_ERR_UNSUPPORTED, "more than 2^31 workgroups or cached tokens");
+    // (a launch has fewer than 2^32 threads: 256 a workgroup, and 64 a row of the join)
+    if (pairs * a.row_tiles * a.splits > 0xffffff || pairs * a.rows > 0x3ffffff) return fail(KDA_ERR_UNSUPPORTED, "more than 2^24 workgroups");
     return KDA_OK;
 }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -137,7 +139,9 @@ extern "C" kda_status kda_cache_append(const kda_cache *cache, int64_t seqlen, c
     // pages that seqlen tokens can touch, wherever they begin
     const int64_t per_seq = cu_seqlens ? 0 : (seqlen + c.page_size - 2) / c.page_size + 1;
     const int64_t slots = c.num_seqs == 0 ? 0 : cu_seqlens ? seqlen / c.page_size + 2 * (int64_t)c.num_seqs : per_seq * c.num_seqs;
-    if (slots * c.heads_kv * 2 + a.tokens * c.heads_q > 0x7fffffffLL) return fail(KDA_ERR_UNSUPPORTED, "more than 2^31 pages and heads, or rows of q");
+    // (a launch has fewer than 2^32 threads: up to 512 a page and head, and dim / 8 a row of q)
+    if (slots * c.heads_kv * 2 > 0x3fffff || a.tokens * c.heads_q > 0x7ffffff || a.tokens * c.heads_kv > 0x7ffffff)
+        return fail(KDA_ERR_UNSUPPORTED, "more than 2^22 pages and heads, or 2^27 rows of k or q");
     a.slots = (int32_t)slots;
     a.slots_per_seq = (int32_t)per_seq;
     return cache_append_dispatch(c, a, cache->dim, static_cast<hipStream_t>(hip_stream));

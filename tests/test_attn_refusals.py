@@ -31,7 +31,8 @@ BAD_DIMS = [(dict(batch=-1), INVALID), (dict(seqlen=-1), INVALID), (dict(heads_q
             (dict(heads_kv=0), INVALID), (dict(heads_q=65536, heads_kv=65536), UNSUPPORTED), (dict(window=-1), INVALID), (dict(sinks=-1), INVALID),
             (dict(sinks=65), UNSUPPORTED), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
             (dict(scale=float("inf")), INVALID), (dict(num_seqs=3), INVALID), (dict(q_stride=511), INVALID), (dict(q_stride=504), INVALID),
-            (dict(k_stride=260), INVALID), (dict(v_stride=1 << 25), INVALID), (dict(batch=1, num_seqs=1, seqlen=1 << 40), UNSUPPORTED)]
+            (dict(k_stride=260), INVALID), (dict(v_stride=1 << 25), INVALID), (dict(batch=1, num_seqs=1, seqlen=1 << 40), UNSUPPORTED),
+            (dict(batch=1 << 20, num_seqs=1 << 20, seqlen=4096), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("change,status", BAD_DIMS)
@@ -116,7 +117,8 @@ def test_cache_append_refuses():
     for n in (-8, 4, 12, 72):
         assert _append(c, rope=kda.KdaRope(inv_freq=SOME, num_freqs=n)) == INVALID
     assert _append(c, rope=kda.KdaRope(inv_freq=None, num_freqs=64)) == INVALID
-    assert _append(c, seqlen=1 << 40) == UNSUPPORTED
+    assert _append(c, seqlen=1 << 40) == UNSUPPORTED and _append(_cache(num_seqs=1 << 27)) == UNSUPPORTED
+    assert _append(_cache(num_seqs=1 << 22, heads_q=128), q=SOME, q_out=SOME) == UNSUPPORTED
     assert _append(c, seqlen=0, k=None, v=None) == 0 and _append(_cache(num_seqs=0)) == 0
 
 
@@ -133,7 +135,7 @@ def test_cache_attn_refuses():
     need = kda.load_library().kda_cache_attn_workspace_size(ctypes.byref(long), ctypes.byref(query))
     assert need > 0
     assert _attn(long, ws=None) == WORKSPACE and _attn(long, ws=SOME + 16) == WORKSPACE and _attn(long, ws_bytes=need - 1) == WORKSPACE
-    assert _attn(_cache(max_pages=1 << 30)) == UNSUPPORTED
+    assert _attn(_cache(max_pages=1 << 30)) == UNSUPPORTED and _attn(_cache(num_seqs=1 << 24)) == UNSUPPORTED
     assert _attn(c, tokens=0) == 0 and _attn(_cache(num_seqs=0)) == 0
 
 
@@ -152,8 +154,10 @@ def test_token_strides_the_binding_takes():
     x = torch.zeros(2, 5, 12, 64)
     assert _token_stride(x, "x") == 0
     assert _token_stride(x[:, :, 4:6], "x") == 12 * 64                # a slice of one projection's output
-    assert _token_stride(x[:1, :1, 4:6], "x") == 0                    # one token: no distance to another
+    assert _token_stride(x[:1, :1, 4:6], "x") in (0, 2 * 64)          # one token: no distance to another
     assert _token_stride(x[:, :1, :2], "x") == 5 * 12 * 64            # one token of each row
-    for bad in (x[:, :, ::2], x[..., ::2], x.transpose(1, 2), x[:, :4, :2]):
+    one = torch.zeros(1, 1, 12, 64)
+    for bad in (x[:, :, ::2], x[..., ::2], x.transpose(1, 2), x[:, :4, :2], one.expand(1, 5, 12, 64), one.expand(3, 1, 12, 64), one.expand(3, 5, 12, 64),
+                x[:, :, :1].expand(2, 5, 3, 64)):
         with pytest.raises(ValueError, match="evenly spaced"):
             _token_stride(bad, "x")

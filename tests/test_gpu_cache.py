@@ -165,6 +165,53 @@ def test_append_rows_of_nobody_in_what_is_passed_in_and_what_is_allocated():
     assert not bool(q_out.any()) and not bool(k_out.any())
 
 
+def test_append_turns_keys_and_queries_in_place():
+    import paper_2510_26692_amd as kda
+    for T, inter in ((3, False), (70, True)):
+        pool = Pool(2, 2, 128, 32, 200, 9)
+        k, v, q = (_tokens(2, T, h, 128, h).cuda() for h in (2, 2, 4))
+        lens = torch.tensor([4, 100], dtype=torch.int32, device="cuda")
+        f = torch.from_numpy(_freqs(64)).cuda()
+        outs = []
+        for place in (False, True):
+            kd, vd, ksd, vsd, td = pool.device()
+            ki, qi = k.clone(), q.clone()
+            qo, ko = kda.kda_cache_append(ki, v, kd, vd, ksd, vsd, td, lens, inv_freq=f, interleaved=inter, q=qi, q_out=qi if place else None,
+                                          k_out=ki if place else None, want_k=True)
+            assert (qo is qi and ko is ki) if place else bool((qi == q).all() and (ki == k).all())
+            outs.append([qo, ko, kd.view(torch.uint8), vd.view(torch.uint8), ksd, vsd])
+        assert all(torch.equal(x, y) for x, y in zip(*outs))
+
+
+def test_cache_calls_on_two_streams_at_once():
+    import paper_2510_26692_amd as kda
+    f = torch.from_numpy(_freqs(64)).cuda()
+    jobs = []
+    for i in range(2):
+        pool = Pool(3, 2, 128, 64, 3000, 20 + i)
+        k, v, q = (_tokens(3, 2, h, 128, 30 + 3 * i + h).cuda() for h in (2, 2, 8))
+        jobs.append((pool, k, v, q, torch.tensor([2900, 64, 1000 + i], dtype=torch.int32, device="cuda")))
+
+    def run(job, times):
+        pool, k, v, q, lens = job
+        dev = pool.device()
+        torch.cuda.synchronize()
+        outs = []
+        for _ in range(times):
+            qo, _ = kda.kda_cache_append(k, v, *dev, lens, inv_freq=f, q=q)
+            outs.append(kda.kda_cache_attn(qo, *dev, lens + 2))
+        return outs
+
+    want = [run(j, 1)[0] for j in jobs]
+    torch.cuda.synchronize()
+    got = []
+    for j, s in zip(jobs, [torch.cuda.Stream(), torch.cuda.Stream()]):
+        with torch.cuda.stream(s):
+            got.append(run(j, 4))
+    torch.cuda.synchronize()
+    assert all(torch.equal(w, o) for w, outs in zip(want, got) for o in outs)
+
+
 def test_append_token_by_token_rounds_older_codes_again():
     import paper_2510_26692_amd as kda
     pool = Pool(2, 2, 64, 32, 96, 4)

@@ -68,6 +68,20 @@ def test_fp32_kernels_use_no_scratch_beyond_a_few_dwords_of_the_gradients_kernel
         assert r["Occupancy [waves/SIMD]"] >= 2 and r["VGPRs Spill"] <= (8 if "Li128E" in name else 0), (name, r)
 
 
+def test_softmax_attention_kernels_keep_their_waves(resources):
+    # (stack: of the call that repeats a walk with care, which is not in the loop; what the loops themselves spill is nothing)
+    fwd, dq, dkv = (_kernels(resources, "kda_attn_%s_kernel" % n) for n in ("fwd", "dq", "dkv"))
+    assert len(fwd) == 4 and len(dq) == 2 and len(dkv) == 2
+    for name, r in fwd.items():
+        assert r["Occupancy [waves/SIMD]"] >= 3 and r["VGPRs Spill"] == 0, (name, r)
+    for name, r in (dq | dkv).items():
+        assert r["Occupancy [waves/SIMD]"] >= 2 and ("Li128E" not in name or r["VGPRs Spill"] == 0), (name, r)
+    attend, append = _kernels(resources, "kda_cache_attn_kernel"), _kernels(resources, "kda_cache_append_kernel")
+    assert len(attend) == 4 and len(append) == 8
+    for name, r in (attend | append).items():
+        assert r["Occupancy [waves/SIMD]"] >= 2 and r["VGPRs Spill"] <= (4 if "Li128ELi2E" in name else 0), (name, r)
+
+
 _OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"
 
 
