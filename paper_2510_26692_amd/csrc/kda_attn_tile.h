@@ -167,26 +167,24 @@ __device__ __forceinline__ void tile_barrier()
 typedef __attribute__((address_space(3))) const u32x4 *lds_u4;
 typedef __attribute__((address_space(3))) s16x4 *lds_s4;
 template <int D> struct TileReader {
-    uint32_t row_base, row_x, tr_base[2], tr_x[2];
+    uint32_t row_at, tr_at[2];       // byte of the lane's row and first chunk; the chunk's number is changed by an exclusive or of bits above
     __device__ __forceinline__ void init(int lane)
     {
         const int x = lane & 31, h = lane >> 5, i = lane & 15, g = (lane >> 4) & 1;
-        row_base = x * 2 * D;
-        row_x = (swizzle<D>(x) ^ h) * 16;
+        row_at = x * 2 * D + (swizzle<D>(x) ^ h) * 16;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int row = 8 * u + 4 * h + (i >> 2);
-            tr_base[u] = row * 2 * D + 8 * (i & 1);
-            tr_x[u] = ((2 * g + ((i >> 1) & 1)) ^ swizzle<D>(row)) * 16;
+            tr_at[u] = row * 2 * D + ((2 * g + ((i >> 1) & 1)) ^ swizzle<D>(row)) * 16 + 8 * (i & 1);
         }
     }
-    // The permuted addresses cost an operation or two each; kept across a walk they take 16 registers, which the dK / dV kernel
-    // does not have (the compiler then spills them): what this touches has to be formed again.
-    __device__ __forceinline__ void forget() { asm volatile("" : "+v"(row_x), "+v"(tr_x[0]), "+v"(tr_x[1])); }
+    // The permuted addresses cost an operation each; kept across a walk they take 16 registers, which the dK / dV kernel does not have (the
+    // compiler then spills them): what this touches has to be formed again.
+    __device__ __forceinline__ void forget() { asm volatile("" : "+v"(row_at), "+v"(tr_at[0]), "+v"(tr_at[1])); }
     // row 32 block + x, channels 16 s + 8 h ..
     __device__ __forceinline__ bf16x8 rows(uint32_t tile, int block, int s) const
     {
-        return __builtin_bit_cast(bf16x8, *reinterpret_cast<lds_u4>((row_base + (row_x ^ (32 * s))) + (tile + block * 32 * 2 * D)));
+        return __builtin_bit_cast(bf16x8, *reinterpret_cast<lds_u4>((row_at ^ (32 * s)) + (tile + block * 32 * 2 * D)));
     }
     // channel 32 db + x, rows 16 ks + {4 h + 0..3, 8 + 4 h + 0..3}
     __device__ __forceinline__ bf16x8 transposed(uint32_t tile, int db, int ks) const
@@ -194,7 +192,7 @@ template <int D> struct TileReader {
         s16x4 r[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-            r[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s4>((tr_base[u] + (tr_x[u] ^ (64 * db))) + (tile + ks * 16 * 2 * D)));
+            r[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s4>((tr_at[u] ^ (64 * db)) + (tile + ks * 16 * 2 * D)));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(r[0], r[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
