@@ -118,6 +118,7 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
         }
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
+            rd.forget();
             f32x16 st = zeros16(), dp = zeros16();
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
@@ -180,8 +181,7 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
 template <int D> __device__ __noinline__ void dq_tile_again(const Shape s, const Back g, const uint32_t lds) { dq_tile<D, true>(s, g, lds); }
 template <int D> __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kda_attn_dq_kernel(const Shape s, const Back g)
 {
-    extern __shared__ __align__(16) uint8_t lds_raw[];
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds_raw;
+    constexpr uint32_t lds = kLds;
     if (!dq_tile<D, false>(s, g, lds)) return;
     if constexpr (D == 128) dq_tile_again<D>(s, g, lds);
     else dq_tile<D, true>(s, g, lds);
@@ -403,8 +403,7 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dkv_tile(const S
 template <int D> __device__ __noinline__ void dkv_tile_again(const Shape s, const Back g, const uint32_t lds) { dkv_tile<D, true>(s, g, lds); }
 template <int D> __global__ __launch_bounds__(kThreads, 2) void kda_attn_dkv_kernel(const Shape s, const Back g)
 {
-    extern __shared__ __align__(16) uint8_t lds_raw[];
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds_raw;
+    constexpr uint32_t lds = kLds;
     if (!dkv_tile<D, false>(s, g, lds)) return;
     if constexpr (D == 128) dkv_tile_again<D>(s, g, lds);
     else dkv_tile<D, true>(s, g, lds);

@@ -182,8 +182,7 @@ __device__ __noinline__ void fwd_tile_again(const Shape s, const uint16_t *q, co
 template <int D, bool kOutBf16>
 __global__ __launch_bounds__(kThreads, 3) void kda_attn_fwd_kernel(const Shape s, const uint16_t *q, const uint16_t *k, const uint16_t *v, void *o, float *lse)
 {
-    extern __shared__ __align__(16) uint8_t lds_raw[];
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds_raw;
+    constexpr uint32_t lds = kLds;
     if (!fwd_tile<D, kOutBf16, false>(s, q, k, v, o, lse, lds)) return;
     fwd_tile_again<D, kOutBf16>(s, q, k, v, o, lse, lds);
 }

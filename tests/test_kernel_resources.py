@@ -82,6 +82,12 @@ def test_softmax_attention_kernels_keep_their_waves(resources):
         assert r["Occupancy [waves/SIMD]"] >= 2 and r["VGPRs Spill"] <= (4 if "Li128ELi2E" in name else 0), (name, r)
 
 
+def test_softmax_attention_kernels_have_no_lds_but_the_launch_s(resources):
+    # (their tiles begin at byte 0)
+    for name, r in _kernels(resources, "kda_attn_").items():
+        assert "join" in name or r["LDS Size [bytes/block]"] == 0, (name, r)
+
+
 _OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"
 
 
