@@ -45,7 +45,7 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
     uint32_t slot, kv, sub;
     split_block(blockIdx.x, s.heads_kv, s.group, slot, kv, sub);
     const int head = kv * s.group + sub;
-    const Place at = place_of(s, s.slots - 1 - slot);
+    const Place at = place_of(s, s.slots - 1 - slot, s.window != 0);
     if (at.first >= at.len || at.first < 0) return false;
 
     const int wq0 = at.first + 32 * wave;
@@ -235,7 +235,7 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dkv_tile(const S
         tile0 = from * kTile / kRows;
         tiles = n * kTile / kRows;
     } else {
-        at = place_of(s, slot);
+        at = place_of(s, slot, false);
         if (at.first >= at.len || at.first < 0) return false;
         const int last = s.window ? min(at.first + kCols + s.window - 2, at.len - 1) : at.len - 1;
         tile0 = at.first / kRows;
@@ -473,10 +473,10 @@ int64_t rows_of(const Shape &s) { return s.cu ? s.tokens : s.tokens * s.num_seqs
 Plan plan_of(const Shape &s, int dim)
 {
     Plan p{};
-    // Workgroups of the dK / dV walk: causal walks differ in length up to the whole sequence, and eight for each place (two a compute unit)
-    // let the short ones fill in behind the long; walks of a window are alike, and two for each place are enough.  us with 512 / 1024 / 2048:
-    // 4 x 4096 x 16 heads causal 1280 / 1150 / 1040, 32768 x 16 heads d 64, window 256 358 / 354 / 444.
-    const int64_t want = s.window ? 1024 : 2048;
+    // Workgroups of the dK / dV walk: two for each place (two a compute unit), so that the second fills in behind walks that end early; more
+    // cost their fp32 sums.  Backward pass in us with 512 / 1024 / 2048: 4 x 4096 x 16 heads over 4 causal 1104 / 962 / 985, 32768 x 16 heads
+    // over 4, d 64, window 256 342 / 338 / 424.
+    const int64_t want = 1024;
     p.splits = 1;
     while (p.splits < s.group && (s.group % p.splits || (int64_t)s.slots * s.heads_kv * p.splits < want)) ++p.splits;
     if (s.sinks) {

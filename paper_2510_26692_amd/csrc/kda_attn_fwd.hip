@@ -24,7 +24,7 @@ __device__ __forceinline__ bool fwd_tile(const Shape &s, const uint16_t *q, cons
     uint32_t slot, kv, sub;
     split_block(blockIdx.x, s.heads_kv, s.group, slot, kv, sub);
     const int head = kv * s.group + sub;
-    const Place at = place_of(s, s.slots - 1 - slot);
+    const Place at = place_of(s, s.slots - 1 - slot, s.window != 0);
     if (at.first >= at.len || at.first < 0) return false;
 
     const int wq0 = at.first + 32 * wave;                                 // the wave's first query

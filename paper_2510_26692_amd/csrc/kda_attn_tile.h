@@ -55,11 +55,14 @@ __device__ __forceinline__ int64_t cu_at(const Shape &s, int n)
     const int64_t v = s.cu[n];
     return v < 0 ? 0 : v < s.tokens ? v : s.tokens;
 }
-__device__ __forceinline__ Place place_of(const Shape &s, int slot)
+// by_rows orders the tiles of a fixed batch row after row, where neighbours' windows overlap (forward at 8 x 2048 tokens, 32 heads over 8,
+// window 1024: 250 us, 256 in the other order); else tile after tile, so that no row's longest walks are begun late (forward at 4 x 4096 x 16
+// heads causal 290 us, 300 in the other order; the whole backward pass 978 and 995, with a window 905 and 950).
+__device__ __forceinline__ Place place_of(const Shape &s, int slot, bool by_rows)
 {
     if (s.tiles) {
-        const int b = slot / s.tiles;
-        return {(int64_t)b * s.tokens, (int32_t)s.tokens, (slot - b * s.tiles) * kCols, b};
+        const int b = by_rows ? slot / s.tiles : slot % s.num_seqs, t = by_rows ? slot - b * s.tiles : slot / s.num_seqs;
+        return {(int64_t)b * s.tokens, (int32_t)s.tokens, t * kCols, b};
     }
     int lo = 0, hi = s.num_seqs - 1;                         // the last sequence whose base is not beyond the slot
     while (lo < hi) {
