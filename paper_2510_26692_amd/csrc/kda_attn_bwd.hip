@@ -102,10 +102,13 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) acc[db] = zeros16();
     issue(0, 0);
-    auto step = [&](int it, auto parity) {
+    auto step = [&](int it, auto parity, auto sums_only) {
         constexpr int P = decltype(parity)::value;
-        tile_barrier();
-        if (it + 1 < steps) issue(it + 1, P ^ 1);
+        constexpr bool kSumsOnly = decltype(sums_only)::value;
+        if constexpr (!kSumsOnly) {
+            tile_barrier();
+            if (it + 1 < steps) issue(it + 1, P ^ 1);
+        }
         const int k0 = first_key(it);
         const uint32_t kt = lds + 2 * P * kT, vt = kt + kT;
         if (k0 > wlast || (s.window && k0 + kTile - 1 <= wq0 - s.window && k0 >= s.sinks)) return;
@@ -137,6 +140,7 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
 #pragma unroll
             for (int j = 0; j < 4; ++j) four[j] = (e[j] + e[4 + j]) + (e[8 + j] + e[12 + j]);
             rest += (four[0] + four[1]) + (four[2] + four[3]);
+            if constexpr (kSumsOnly) continue;
             const bf16x8 ds[2] = {pack8(e), pack8(e + 8)};
             if (kCareful && edge) {
 #pragma unroll
@@ -150,9 +154,23 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
             }
         }
     };
+    using First = std::integral_constant<int, 0>;
+    using Second = std::integral_constant<int, 1>;
+    // In a row that sees few keys d is as large as do . v, and o's rounding in it as large as that of dS.  Where the two buffers hold all
+    // the keys there are, d is summed from P and do . v first (dQ at 2 x 200 tokens: 2.7e-3 off without, 2.4e-3 with, for 0.4 us; longer
+    // walks have few such rows).
+    if (steps <= 2) {
+        if (steps == 2) issue(1, 1);
+        tile_barrier();
+        delta = 0.f;
+        step(0, First{}, std::true_type{});
+        if (steps == 2) step(1, Second{}, std::true_type{});
+        delta = rest + other_half(rest);
+        rest = 0.f;
+    }
     for (int it = 0; it < steps; it += 2) {
-        step(it, std::integral_constant<int, 0>{});
-        if (it + 1 < steps) step(it + 1, std::integral_constant<int, 1>{});
+        step(it, First{}, std::false_type{});
+        if (it + 1 < steps) step(it + 1, Second{}, std::false_type{});
     }
     rest += other_half(rest);
     // (formed again: held through the walk these would take registers from it)
