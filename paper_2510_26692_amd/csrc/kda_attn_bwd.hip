@@ -7,6 +7,10 @@
 // of every sum is fixed.  A key head's gradients sum over its group's query heads inside a workgroup; where that leaves too few
 // workgroups, over parts of the group, whose fp32 sums a last kernel adds.  The sinks' keys are seen by every later query: what lies beyond
 // their window is walked by workgroups of its own, in parts.
+//
+// What bounds it is the matrix cores: 16 384 tokens x 16 heads of 128 causal in 3 400 us, 809 TFLOP/s for the 5 products that a gradient
+// needs and 1 132 for the 7 done; 4 x 4 096 x 16 heads over 4 in 960 us (716 and 1 002), 50 of them for the sums of the parts.  A window of
+// 1024 costs a fifth more a visible pair: every walk has two partly seen ends.
 #include <algorithm>
 #include <type_traits>
 

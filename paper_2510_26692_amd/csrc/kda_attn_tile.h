@@ -1,7 +1,7 @@
 // Tiles shared by the softmax-attention kernels (kda_attn_fwd.hip, kda_attn_bwd.hip).
 //
-// A wave owns 32 columns (queries, or in the dK / dV kernel keys) whose operands stay in registers, and walks tiles of 64 rows
-// (keys, or queries) that the workgroup's four waves bring into LDS.  Every product is a 32x32x16 bf16 MFMA with the walked rows as
+// A wave owns 32 columns (queries, or in the dK / dV kernel keys) whose operands stay in registers, and walks tiles of 32 or 64
+// rows (keys, or queries) that the workgroup's four waves bring into LDS.  Every product is a 32x32x16 bf16 MFMA with the walked rows as
 // the A operand:
 //
 //     X [row, column]    = sum_d  R[row, d] C[column, d]       A: rows of the LDS tile,            B: the wave's columns

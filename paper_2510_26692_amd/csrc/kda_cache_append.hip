@@ -243,8 +243,8 @@ template <int D, int kThreads> __device__ __forceinline__ void turn_queries(cons
 //
 // Angles are held in 64 bits, so that the codes are those of the exact rotation (in 32 bits one in 2^21 was another): computed for the
 // lane's first row and for the distance to its next, then multiplied, 4 operations a pair instead of 30, down the rows of one head and up
-// those of the next.  16 prompts (67 000 tokens, 8 heads, pages of 64), 0.55 GB: 354 us with a workgroup a head, 160 so; a plain copy of as
-// many bytes takes 106.  256 sequences x 4 tokens: 20 us with a workgroup a page, head and 4 rows, 11 so.
+// those of the next.  16 prompts (67 000 tokens, 8 key heads and 32 query heads, pages of 64; 1.8 GB): 604 us with an angle formed for each
+// head, 363 so, 5.0 TB/s (a plain copy: 5.2).  256 sequences x 4 tokens: 20 us with a workgroup a page, head and 4 rows, 11 so.
 template <int D, int kThreads, int kIters>
 __device__ __forceinline__ void append_page(const Cache &c, const Append &a, const Piece &t, const double (&freq)[4], bool turned, bool values, int head0, int n,
                                             int64_t logical, int64_t len, int64_t count, int64_t first_row)
@@ -423,7 +423,6 @@ __global__ __launch_bounds__(kThreads, kIters == 1 ? 3 : 2) void kda_cache_appen
     if (blockIdx.x < (uint32_t)a.page_blocks) append_pages<D, kThreads, kIters>(c, a, blockIdx.x);
     else turn_queries<D, kThreads>(c, a, blockIdx.x - a.page_blocks);
 }
-template <int D> __global__ __launch_bounds__(256) void kda_cache_queries_kernel(const Cache c, const Append a) { turn_queries<D, 256>(c, a, blockIdx.x); }
 
 }  // namespace cache
 
@@ -433,24 +432,21 @@ template <int D, int kThreads, int kIters>
 static hipError_t launch_append(const Cache &c, Append a, hipStream_t st)
 {
     constexpr int kRows = kThreads / (D / 8);
-    // Heads that share a lane's angles: as many as leave 1024 workgroups.
+    // Heads that share a lane's angles: as many as leave a wave for each SIMD where a workgroup's rows are few, half as many threads where it
+    // has a page.  us with half the threads / these / twice: 256 x 4 tokens, 8 heads 14.1 / 11.4 / 12.9; one prompt of 2048 tokens and 32
+    // query heads 17.5 / 16.6 / 18.1, four 40.8 / 40.6 / 43.1.
+    constexpr int kEnough = kIters == 1 ? 1 << 16 : 1 << 15;
     a.page_heads = c.heads_kv;
-    while (a.page_heads > 1 && (c.heads_kv % a.page_heads || (int64_t)a.slots * (c.heads_kv / a.page_heads) < 1024)) --a.page_heads;
+    while (a.page_heads > 1 && (c.heads_kv % a.page_heads || (int64_t)a.slots * (c.heads_kv / a.page_heads) * kThreads < kEnough)) --a.page_heads;
     a.page_blocks = a.slots * (c.heads_kv / a.page_heads) * 2;
     int64_t q_blocks = 0;
     if (a.q || a.zero_k) {
-        // several heads a thread share its angles once there are threads enough: 2^17 of them
+        // several heads a thread share its angles once there are threads enough: 2^17 of them (one prompt of 512 tokens 8.2 us, 8.5 with 2^14;
+        // of 2048 16.6 and 20.5; with a head a thread 10 and 29)
         a.q_heads = 1;
         while (a.q_heads < 16 && a.tokens * c.heads_q * (D / 8) / a.q_heads > 1 << 17) a.q_heads *= 2;
         const int64_t items = a.tokens * ((c.heads_q + a.q_heads - 1) / a.q_heads);
         q_blocks = (items + kRows - 1) / kRows;
-    }
-    // Queries of many tokens go by themselves: theirs is a kernel of few registers, and so of many waves (the same 16 prompts x 32 heads, 1.1 GB:
-    // 231 us, 4.8 TB/s).
-    const bool apart = kThreads >= 256 && q_blocks > 2048;
-    if (apart) {
-        hipLaunchKernelGGL(kda_cache_queries_kernel<D>, dim3((uint32_t)(q_blocks * (kThreads / 256))), dim3(256), 0, st, c, a);
-        q_blocks = 0;
     }
     if (a.page_blocks + q_blocks > 0)
         hipLaunchKernelGGL((kda_cache_append_kernel<D, kThreads, kIters>), dim3((uint32_t)(a.page_blocks + q_blocks)), dim3(kThreads), 0, st, c, a);
