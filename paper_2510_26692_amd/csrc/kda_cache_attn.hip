@@ -28,6 +28,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr float kInf = __builtin_huge_valf();
 constexpr int kStep = 32;            // keys of a step
 constexpr int kWaves = 4;
+constexpr int kJoinAlone = 32;       // parts of a row that one wave joins
 
 // The visible keys of a sequence's new tokens as steps: those of the sinks where the window begins behind them, then the window's.
 struct Steps {
@@ -387,24 +388,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Ca
     }
 }
 
-// The splits' parts of a row, one wave a row: D / 64 channels a lane.
-template <int D>
+// The splits' parts of a row, D / 64 channels a lane.  kPer waves have a row between them: one wave reads 8 parts at a time, and what a long
+// sequence of few heads is split into would keep it waiting (the call for one of 131 072 tokens and 2 key heads, 256 parts: 37.7 us with one
+// wave a row, 22.2 with four; 8 192 tokens and 8 heads, 32 parts, 11.2 and 11.1).
+template <int D, int kPer>
 __global__ __launch_bounds__(256) void kda_cache_join_kernel(const Cache c, const Attend a)
 {
-    constexpr int W = D / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);       // (sequence, key head, row)
-    if (item >= (int64_t)c.num_seqs * c.heads_kv * a.rows) return;
+    constexpr int W = D / 64, kAhead = kPer > 1 ? 16 : 8;
+    __shared__ float joined[kPer > 1 ? kPer : 1][D + 2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t item = kPer > 1 ? blockIdx.x : (int64_t)blockIdx.x * kWaves + wave;         // (sequence, key head, row)
+    if (item >= (int64_t)c.num_seqs * c.heads_kv * a.rows) return;                             // (whole workgroups, where they share a row)
     const int64_t pair = item / a.rows;
     const int row = (int)(item - pair * a.rows), n = (int)(pair / c.heads_kv), kv = (int)(pair - (int64_t)n * c.heads_kv);
     const Steps st = steps_of(c, a, n);
     const int32_t per = wave_steps(st, a.splits) * kWaves, used = per ? (st.count + per - 1) / per : 0;
+    const int32_t mine = (used + kPer - 1) / kPer, begin = kPer > 1 ? wave * mine : 0, end = min(begin + mine, used);
     // a lane has one split's maximum and sum, 64 splits at a time
     float m = -kInf, l = 0.f, y[W] = {};
-    for (int s0 = 0; s0 < used; s0 += 64) {
+    for (int s0 = begin; s0 < end; s0 += 64) {
         const int64_t part = (pair * a.splits + s0 + lane) * a.rows + row;
         float ms = -kInf, ls = 0.f;
-        if (s0 + lane < used) {
+        if (s0 + lane < end) {
             ms = a.stats[part * 2];
             ls = a.stats[part * 2 + 1];
         }
@@ -419,21 +424,44 @@ __global__ __launch_bounds__(256) void kda_cache_join_kernel(const Cache c, cons
         l = l * old + ls;
 #pragma unroll
         for (int i = 0; i < W; ++i) y[i] *= old;
-        const int count = used - s0 < 64 ? used - s0 : 64;
+        const int count = end - s0 < 64 ? end - s0 : 64;
         const float *from = a.part + ((pair * a.splits + s0) * a.rows + row) * D + W * lane;
         const int64_t step = (int64_t)a.rows * D;
-        for (int s = 0; s < count; s += 8) {
-            float x[8][W];
+        for (int s = 0; s < count; s += kAhead) {
+            float x[kAhead][W];
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
+            for (int u = 0; u < kAhead; ++u)
 #pragma unroll
                 for (int i = 0; i < W; ++i) x[u][i] = from[(s + u < count ? s + u : count - 1) * step + i];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < kAhead; ++u) {
                 const float g = s + u < count ? __shfl(f, s + u) : 0.f;
 #pragma unroll
                 for (int i = 0; i < W; ++i) y[i] += s + u < count ? x[u][i] * g : 0.f;
             }
+        }
+    }
+    if constexpr (kPer > 1) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) joined[wave][W * lane + i] = y[i];
+        if (lane == 0) {
+            joined[wave][D] = m;
+            joined[wave][D + 1] = l;
+        }
+        __syncthreads();
+        if (wave) return;
+        float top = -kInf;
+#pragma unroll
+        for (int w = 0; w < kPer; ++w) top = fmaxf(top, joined[w][D]);
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) y[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kPer; ++w) {
+            const float f = joined[w][D] == -kInf ? 0.f : fast_exp2(joined[w][D] - top);
+            l += joined[w][D + 1] * f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) y[i] += joined[w][W * lane + i] * f;
         }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -454,7 +482,10 @@ using namespace kda::cache;
 
 namespace kda {
 
-// Workgroups of a sequence and head's keys: enough for two on every compute unit, each of its waves with two steps at least.
+// Workgroups of a sequence and head's keys: enough for two on every compute unit, each of its waves with two steps at least.  us with one /
+// two / four on every compute unit: 8 sequences of 4 096 tokens x 8 heads 17.7 / 17.5 / 20.4, 16 of 8 192 x 4 new tokens 31.1 / 25.4 / 24.5,
+// 32 of 4 096 36.4 / 37.8 / 39.0; with one / two / four steps at least: one sequence of 500 9.4 / 10.2 / 8.4, of 2 000 9.6 / 9.9 / 11.2, of
+// 8 192 12.8 / 11.2 / 11.7.
 int32_t cache_attn_splits(const Cache &c, int64_t pairs, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
 {
     int64_t keys = most_keys;
@@ -476,7 +507,8 @@ template <int D> hipError_t launch(const Cache &c, Attend a, hipStream_t st)
     hipError_t e = a.row_tiles == 1 && a.rows <= 16 ? launch<D, 1>(c, a, st) : launch<D, 2>(c, a, st);
     if (e == hipSuccess && a.splits > 1) {
         const int64_t items = (int64_t)c.num_seqs * c.heads_kv * a.rows;
-        hipLaunchKernelGGL(kda_cache_join_kernel<D>, dim3((uint32_t)((items + 3) / 4)), dim3(256), 0, st, c, a);
+        if (a.splits > kJoinAlone) hipLaunchKernelGGL((kda_cache_join_kernel<D, kWaves>), dim3((uint32_t)items), dim3(64 * kWaves), 0, st, c, a);
+        else hipLaunchKernelGGL((kda_cache_join_kernel<D, 1>), dim3((uint32_t)((items + kWaves - 1) / kWaves)), dim3(64 * kWaves), 0, st, c, a);
         e = hipGetLastError();
     }
     return e;

@@ -286,6 +286,18 @@ def test_attend(Tq, Hq, Hk, d, page, lens, window, sinks, out_dtype):
     _check_attend(pool, _tokens(len(lens), Tq, Hq, d, 5), lens, window, sinks, out_dtype)
 
 
+@pytest.mark.parametrize("d,Hq,window,sinks", [(128, 4, 0, 0), (64, 3, 20000, 7)])
+def test_attend_parts_of_long_sequences_joined_by_several_waves(d, Hq, window, sinks):
+    """Few heads and many keys: more parts than one wave joins, in sequences that fill them, some of them, one or none."""
+    lens = [33000, 9000, 12, 0]
+    pool = Pool(4, 1, d, 64, 33040, 71, nan_behind=lens)
+    q = _tokens(4, 2, Hq, d, 72)
+    clean = _check_attend(pool, q, lens, window, sinks)
+    pool.k[pool.table[0, 32000 // 64], 0, 32000 % 64, 1] = 0xFF
+    got = _attend(pool, q, lens, window, sinks)
+    assert not bool(torch.isfinite(got[0]).any()) and torch.equal(got[1:], clean[1:])
+
+
 def test_attend_lengths_of_nothing_give_zeros():
     pool = Pool(4, 2, 128, 64, 200, 1)
     o = _attend(pool, _tokens(4, 3, 4, 128, 1), [0, -5, -(2 ** 31), 1])
