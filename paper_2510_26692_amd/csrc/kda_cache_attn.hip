@@ -482,15 +482,16 @@ using namespace kda::cache;
 
 namespace kda {
 
-// Workgroups of a sequence and head's keys: enough for two on every compute unit, each of its waves with two steps at least.  us with one /
-// two / four on every compute unit: 8 sequences of 4 096 tokens x 8 heads 17.7 / 17.5 / 20.4, 16 of 8 192 x 4 new tokens 31.1 / 25.4 / 24.5,
-// 32 of 4 096 36.4 / 37.8 / 39.0; with one / two / four steps at least: one sequence of 500 9.4 / 10.2 / 8.4, of 2 000 9.6 / 9.9 / 11.2, of
-// 8 192 12.8 / 11.2 / 11.7.
+// Workgroups of a sequence and head's keys: enough for two on every compute unit, each of its waves with two steps at least, and one,
+// without a join, where six steps do.  us with one / two / four on every compute unit: 8 sequences of 4 096 tokens x 8 heads 17.7 / 17.5 / 20.4,
+// 16 of 8 192 x 4 new tokens 31.1 / 25.4 / 24.5, 32 of 4 096 36.4 / 37.8 / 39.0; with one / two / four steps at least: one sequence of 2 000
+// 9.6 / 9.9 / 11.2, of 8 192 12.8 / 11.2 / 11.7; with two steps at least / six without a join: of 300 9.8 / 6.9, of 700 10.1 / 9.2.
 int32_t cache_attn_splits(const Cache &c, int64_t pairs, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
 {
     int64_t keys = most_keys;
     if (window && window + tokens + sinks + 2 * kStep < keys) keys = window + tokens + sinks + 2 * kStep;
-    const int64_t steps = (keys + kStep - 1) / kStep, most = (steps + 2 * kWaves - 1) / (2 * kWaves), want = (512 + pairs - 1) / (pairs > 0 ? pairs : 1);
+    const int64_t steps = (keys + kStep - 1) / kStep, most = steps <= 6 * kWaves ? 1 : (steps + 2 * kWaves - 1) / (2 * kWaves),
+                  want = (512 + pairs - 1) / (pairs > 0 ? pairs : 1);
     const int64_t n = want < most ? want : most;
     return (int32_t)(n < 1 ? 1 : n);
 }
