@@ -25,12 +25,13 @@ struct Back {
     const float *lse;
     float *stats;                    // [2][B,Hq,T]: lse log2 e (+inf for a row that sees nothing), and d
     uint16_t *dq, *dk, *dv;
-    float *part_k, *part_v;          // [splits][tokens][Hk][D] fp32 (not where the gradients are written directly)
+    float *part_k, *part_v;          // [splits][tokens][Hk][D] fp32, or with `heads_only` [num_seqs][64][Hk][D]
     float *sink_k, *sink_v;          // [sink_slots][2][splits][Hk][64][D] fp32
     int32_t splits;                  // parts that a group's heads are cut into
     int32_t sink_slots, sink_tiles;  // parts of the sinks' walks: how many, and tiles of 64 queries each
     int32_t sink_parts;              // of a sequence of a fixed batch; 0: packed
-    bool direct;
+    bool direct;                     // nothing to be summed: gradients are written as they are
+    bool heads_only;                 // nothing but the sinks' walks' parts, of each sequence's first 64 keys
 };
 // elements of one part of dK or dV
 __device__ __forceinline__ int64_t part_size(const Shape &s, int d) { return (s.cu ? s.tokens : s.tokens * s.num_seqs) * s.heads_kv * d; }
@@ -237,7 +238,7 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dkv_tile(const S
     if (sink) {
         int32_t part;
         if (g.sink_parts) {
-            at = {(int64_t)(slot / g.sink_parts) * s.tokens, (int32_t)s.tokens, 0, (int32_t)(slot / g.sink_parts)};
+            at = {(int64_t)(slot / g.sink_parts) * s.tokens, (int32_t)s.tokens, 0, (int32_t)(slot / g.sink_parts), (int32_t)(slot / g.sink_parts)};
             part = slot % g.sink_parts;
         } else {
             const int64_t per = (int64_t)kTile * g.sink_tiles;               // (slots as in place_of)
@@ -248,7 +249,7 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dkv_tile(const S
             }
             const int64_t a = cu_at(s, lo), e = cu_at(s, lo + 1), p = (int64_t)slot - (a / per + lo);
             if (p < 0) return false;
-            at = {a, (int32_t)(e - a), 0, 0};
+            at = {a, (int32_t)(e - a), 0, 0, lo};
             part = (int32_t)p;
         }
         if (at.len <= 0) return false;
@@ -393,6 +394,7 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dkv_tile(const S
     const bool bad = !kCareful && (not_finite(dk) || not_finite(dv));
     const int mine = kw0 + (again & 31), half = again & 32;
     if (sink || mine < at.len) {
+        const int seq = !sink && g.heads_only && kw0 < kTile ? place_of(s, slot, false).seq : 0;         // (found again, as above)
         const int64_t row = ((at.row0 + mine) * s.heads_kv + kv) * D;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
@@ -409,12 +411,12 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dkv_tile(const S
                     const int64_t w = ((((int64_t)slot * 2 + (wave >> 1)) * g.splits + sub) * s.heads_kv + kv) * kTile * D + (int64_t)mine * D + ch;
                     *reinterpret_cast<f32x4 *>(g.sink_k + w) = yk;
                     *reinterpret_cast<f32x4 *>(g.sink_v + w) = yv;
-                } else if (g.direct) {
+                } else if (g.direct || (g.heads_only && kw0 >= kTile)) {
                     const u32x2 wk = {pack_bf16x2(yk[0], yk[1]), pack_bf16x2(yk[2], yk[3])}, wv = {pack_bf16x2(yv[0], yv[1]), pack_bf16x2(yv[2], yv[3])};
                     *reinterpret_cast<u32x2 *>(g.dk + row + ch) = wk;
                     *reinterpret_cast<u32x2 *>(g.dv + row + ch) = wv;
                 } else {
-                    const int64_t w = (int64_t)sub * part_size(s, D) + row + ch;
+                    const int64_t w = (g.heads_only ? (((int64_t)seq * kTile + mine) * s.heads_kv + kv) * D : (int64_t)sub * part_size(s, D) + row) + ch;
                     *reinterpret_cast<f32x4 *>(g.part_k + w) = yk;
                     *reinterpret_cast<f32x4 *>(g.part_v + w) = yv;
                 }
@@ -431,26 +433,35 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void kda_attn_dkv_ker
     else dkv_tile<D, true>(s, g, lds);
 }
 
-// Sums of the parts: a thread has four channels of a token and key head.
+// Sums of the parts: a thread has four channels of a token and key head.  Places of a sequence's first 64 keys stand one sequence after the
+// other where nothing else is to be summed, else items are tokens.
 template <int D> __device__ __forceinline__ void join_four(const Shape &s, const Back &g, int64_t i)
 {
-    const int64_t token = i / ((int64_t)D * s.heads_kv);
-    int64_t index = token, first_slot = 0, len = s.tokens;
-    if (s.cu) {
+    const int64_t row = i / ((int64_t)D * s.heads_kv), inner = i - row * (int64_t)D * s.heads_kv;
+    int64_t index, first;                                    // in the sequence, and the sequence's first token
+    int64_t len = s.tokens;
+    int seq;
+    if (g.heads_only) {
+        seq = (int)(row / kTile);
+        index = row - (int64_t)seq * kTile;
+        first = s.cu ? cu_at(s, seq) : (int64_t)seq * s.tokens;
+        if (s.cu) len = cu_at(s, seq + 1) - first;
+        if (index >= len) return;
+    } else if (s.cu) {
         int lo = 0, hi = s.num_seqs - 1;
-        if (token < cu_at(s, 0) || token >= cu_at(s, s.num_seqs)) return;        // owned by no sequence
+        if (row < cu_at(s, 0) || row >= cu_at(s, s.num_seqs)) return;            // owned by no sequence
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (cu_at(s, mid) <= token) lo = mid; else hi = mid - 1;
+            if (cu_at(s, mid) <= row) lo = mid; else hi = mid - 1;
         }
-        const int64_t a = cu_at(s, lo);
-        index = token - a;
-        len = cu_at(s, lo + 1) - a;
-        if (g.sink_slots) first_slot = a / ((int64_t)kTile * g.sink_tiles) + lo;
+        seq = lo;
+        first = cu_at(s, lo);
+        index = row - first;
+        len = cu_at(s, lo + 1) - first;
     } else {
-        const int64_t b = token / s.tokens;
-        index = token - b * s.tokens;
-        first_slot = b * g.sink_parts;
+        seq = (int)(row / s.tokens);
+        first = (int64_t)seq * s.tokens;
+        index = row - first;
     }
     f32x4 yk = {0.f, 0.f, 0.f, 0.f}, yv = yk;
     for (int p = 0; p < g.splits; ++p) {
@@ -459,22 +470,25 @@ template <int D> __device__ __forceinline__ void join_four(const Shape &s, const
         yv += *reinterpret_cast<const f32x4 *>(g.part_v + w);
     }
     if (g.sink_slots && index < kTile) {
+        const int64_t first_slot = s.cu ? first / ((int64_t)kTile * g.sink_tiles) + seq : (int64_t)seq * g.sink_parts;
         const int64_t left = (len + kTile - 1) / kTile - first_walk_tiles(s, (int)len), parts = (left + g.sink_tiles - 1) / g.sink_tiles;
-        const int64_t inner = i - token * (int64_t)D * s.heads_kv, kv = inner / D, ch = inner - kv * D;
+        const int64_t kv = inner / D, step = (int64_t)s.heads_kv * kTile * D;
+        const int64_t w = (first_slot * 2 * g.splits * s.heads_kv + kv) * kTile * D + index * D + (inner - kv * D);
+#pragma unroll 8
         for (int64_t p = 0; p < parts * 2 * g.splits; ++p) {
-            const int64_t w = ((first_slot * 2 * g.splits + p) * s.heads_kv + kv) * kTile * D + index * D + ch;
-            yk += *reinterpret_cast<const f32x4 *>(g.sink_k + w);
-            yv += *reinterpret_cast<const f32x4 *>(g.sink_v + w);
+            yk += *reinterpret_cast<const f32x4 *>(g.sink_k + w + p * step);
+            yv += *reinterpret_cast<const f32x4 *>(g.sink_v + w + p * step);
         }
     }
+    const int64_t out = (first + index) * (int64_t)D * s.heads_kv + inner;
     const u32x2 wk = {pack_bf16x2(yk[0], yk[1]), pack_bf16x2(yk[2], yk[3])}, wv = {pack_bf16x2(yv[0], yv[1]), pack_bf16x2(yv[2], yv[3])};
-    *reinterpret_cast<u32x2 *>(g.dk + i) = wk;
-    *reinterpret_cast<u32x2 *>(g.dv + i) = wv;
+    *reinterpret_cast<u32x2 *>(g.dk + out) = wk;
+    *reinterpret_cast<u32x2 *>(g.dv + out) = wv;
 }
 template <int D>
-__global__ __launch_bounds__(256) void kda_attn_join_kernel(const Shape s, const Back g, int64_t tokens)
+__global__ __launch_bounds__(256) void kda_attn_join_kernel(const Shape s, const Back g, int64_t rows)
 {
-    const int64_t all = tokens * s.heads_kv * D, step = (int64_t)gridDim.x * 1024;
+    const int64_t all = rows * s.heads_kv * D, step = (int64_t)gridDim.x * 1024;
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < all; i += step) join_four<D>(s, g, i);
 }
 
@@ -486,8 +500,9 @@ using namespace attn;
 namespace {
 struct Plan {
     int32_t splits, sink_slots, sink_tiles, sink_parts;
-    bool direct;
-    size_t part, sink_k, sink_v, part_k, part_v, total;
+    bool direct, heads_only;
+    int64_t part_rows;
+    size_t sink_k, sink_v, part_k, part_v, total;
 };
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 int64_t rows_of(const Shape &s) { return s.cu ? s.tokens : s.tokens * s.num_seqs; }
@@ -510,8 +525,10 @@ Plan plan_of(const Shape &s, int dim)
         p.sink_slots = (int32_t)(s.cu ? s.tokens / per + s.num_seqs : parts * s.num_seqs);
     }
     p.direct = p.splits == 1 && !s.sinks;
+    p.heads_only = p.splits == 1 && s.sinks && (int64_t)s.num_seqs * kTile <= rows_of(s);          // (many short sequences have fewer tokens)
+    p.part_rows = p.direct ? 0 : p.heads_only ? (int64_t)s.num_seqs * kTile : rows_of(s);
     size_t at = up256((size_t)rows_of(s) * s.heads_q * 4 * 2);
-    const size_t part = p.direct ? 0 : up256((size_t)p.splits * rows_of(s) * s.heads_kv * dim * 4);
+    const size_t part = up256((size_t)p.splits * p.part_rows * s.heads_kv * dim * 4);
     const size_t sink = up256((size_t)p.sink_slots * 2 * p.splits * s.heads_kv * kTile * dim * 4);
     p.part_k = at;
     p.part_v = at += part;
@@ -529,8 +546,8 @@ template <int D> hipError_t launch_bwd(const Shape &s, Back g, const Plan &p, hi
     const uint32_t per_slot = (uint32_t)s.heads_kv * p.splits;
     hipLaunchKernelGGL(kda_attn_dkv_kernel<D>, dim3(((uint32_t)s.slots + p.sink_slots) * per_slot), dim3(kThreads), kLdsStats, st, s, g);
     if (!p.direct) {
-        const int64_t tokens = rows_of(s), threads = tokens * s.heads_kv * (D / 4);
-        hipLaunchKernelGGL(kda_attn_join_kernel<D>, dim3((uint32_t)std::min<int64_t>((threads + 255) / 256, 1 << 20)), dim3(256), 0, st, s, g, tokens);
+        const int64_t threads = p.part_rows * s.heads_kv * (D / 4);
+        hipLaunchKernelGGL(kda_attn_join_kernel<D>, dim3((uint32_t)std::min<int64_t>((threads + 255) / 256, 1 << 20)), dim3(256), 0, st, s, g, p.part_rows);
     }
     return hipGetLastError();
 }
@@ -546,7 +563,7 @@ kda_status attn_bwd_dispatch(const Shape &s, int dim, const void *q, const void 
     auto in = [](const void *x) { return static_cast<const uint16_t *>(x); };
     auto at = [&](size_t off) { return reinterpret_cast<float *>(w + off); };
     const Back g = {in(q), in(k), in(v), in(o), in(d_o), lse, at(0), static_cast<uint16_t *>(dq), static_cast<uint16_t *>(dk), static_cast<uint16_t *>(dv),
-                    at(p.part_k), at(p.part_v), at(p.sink_k), at(p.sink_v), p.splits, p.sink_slots, p.sink_tiles, p.sink_parts, p.direct};
+                    at(p.part_k), at(p.part_v), at(p.sink_k), at(p.sink_v), p.splits, p.sink_slots, p.sink_tiles, p.sink_parts, p.direct, p.heads_only};
     const hipError_t e = dim == 128 ? launch_bwd<128>(s, g, p, st) : launch_bwd<64>(s, g, p, st);
     return e == hipSuccess ? KDA_OK : fail(KDA_ERR_LAUNCH, "kda_window_attn_bwd: %s", hipGetErrorString(e));
 }

@@ -49,6 +49,7 @@ struct Place {
     int32_t len;                     // its tokens
     int32_t first;                   // first token of the tile, relative to row0; len or beyond: nothing to do
     int32_t batch;                   // row of the batch (0: packed)
+    int32_t seq;                     // which sequence
 };
 __device__ __forceinline__ int64_t cu_at(const Shape &s, int n)
 {
@@ -62,7 +63,7 @@ __device__ __forceinline__ Place place_of(const Shape &s, int slot, bool by_rows
 {
     if (s.tiles) {
         const int b = by_rows ? slot / s.tiles : slot % s.num_seqs, t = by_rows ? slot - b * s.tiles : slot / s.num_seqs;
-        return {(int64_t)b * s.tokens, (int32_t)s.tokens, t * kCols, b};
+        return {(int64_t)b * s.tokens, (int32_t)s.tokens, t * kCols, b, b};
     }
     int lo = 0, hi = s.num_seqs - 1;                         // the last sequence whose base is not beyond the slot
     while (lo < hi) {
@@ -70,7 +71,7 @@ __device__ __forceinline__ Place place_of(const Shape &s, int slot, bool by_rows
         if (cu_at(s, mid) / kCols + mid <= slot) lo = mid; else hi = mid - 1;
     }
     const int64_t a = cu_at(s, lo), e = cu_at(s, lo + 1);
-    return {a, (int32_t)(e - a), (int32_t)(slot - (a / kCols + lo)) * kCols, 0};
+    return {a, (int32_t)(e - a), (int32_t)(slot - (a / kCols + lo)) * kCols, 0, lo};
 }
 
 // What a column of a tile of 64 rows sees, as bits: row 32 b + r of the tile is bit r of w[b].  seen_rows: rows first .. last.

@@ -121,6 +121,15 @@ def test_packed_batch_leaves_rows_of_no_sequence_alone(lens, before, behind, win
         assert torch.equal(fresh[n][:, rows], out[n][:, rows]) and not bool(fresh[n][:, :before].any()) and not bool(fresh[n][:, cu[-1]:].any())
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[1500, 2, 0, 64, 65, 700], [3] * 50 + [600, 63], [127, 1]], ids=["long", "many short", "short"])
+def test_packed_sinks_with_a_key_head_for_every_query_head(lens, d):
+    """Nothing but the sinks' later queries is summed apart from the keys' own walks: few long sequences and many short ones."""
+    cu = np.concatenate([[0], np.cumsum(lens)]).tolist()
+    x = _make(1, cu[-1], 3, 3, d, len(lens))
+    _check_bwd(x, _grads(x, 40, 33, cu)[2], 40, 33, cu)
+
+
 def test_entries_of_cu_seqlens_outside_the_batch_are_clamped():
     import paper_2510_26692_amd as kda
     x = {n: t.cuda() for n, t in _make(1, 200, 2, 1, 64, 5).items()}
