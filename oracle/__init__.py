@@ -13,7 +13,8 @@ the output gate of the same section (head-wise RMSNorm times a sigmoid gate), in
 Eq. (1) (Section 2.2, alpha_t = a_t I): the same recurrence on the decay repeated over the channels.
 `kda_backward` is the reverse-mode derivative of that recurrence, token by token (the paper derives no
 backward algorithm; the chain rule on Eq. (1) is the definition), pinned by finite differences of the
-two forward statements.
+two forward statements.  `softmax_attention` states the softmax-attention entry points (window, sinks, gradients,
+the rotated append to an 8-bit cache and attention over it) in float64.
 """
 import numpy as _np
 
