@@ -477,7 +477,7 @@ typedef struct {
 /*
  * Appends new tokens to the cache: sequence n holds kv_lens[n] tokens before the call (a negative entry skips the sequence), and its
  * new ones take the positions from there on.  kv_lens is not changed: the caller adds to it.
- *   seqlen, cu_seqlens   tokens of each sequence, or with cu_seqlens [num_seqs+1] (as for kda_chunk_fwd) all of a packed batch's
+ *   seqlen, cu_seqlens   tokens of each sequence, at most 2^30, or with cu_seqlens [num_seqs+1] (as for kda_chunk_fwd) all of a packed batch's
  *   k, v           [..,heads_kv,dim]   bf16, [num_seqs,seqlen] or packed rows; strides in elements from a token to the next as in kda_attn_dims
  *   rope           rotation of k (and q), or NULL: as they are
  *   k_out          [..,heads_kv,dim]   bf16: the rotated keys, for a prefill that follows, or NULL

@@ -63,7 +63,7 @@ kda_status check(const kda_attn_dims *d, const int32_t *cu, attn::Shape &s)
     const int64_t tiles = (d->seqlen + attn::kCols - 1) / attn::kCols;
     const int64_t slots = cu ? d->seqlen / attn::kCols + d->num_seqs : tiles * d->batch;
     // (a launch has fewer than 2^32 threads; the dK / dV walk has the sinks' workgroups as well, no more than the others)
-    if (slots * 2 * (d->heads_q > 0 ? d->heads_q : 1) * attn::kThreads > 0xffffffffLL)
+    if (slots > 0x7fffff || slots * 2 * (d->heads_q > 0 ? d->heads_q : 1) * attn::kThreads > 0xffffffffLL)
         return fail(KDA_ERR_UNSUPPORTED, "more than 2^23 tiles of %d tokens and heads", attn::kCols);
     s.slots = (int32_t)slots;
     s.tiles = cu ? 0 : (int32_t)tiles;

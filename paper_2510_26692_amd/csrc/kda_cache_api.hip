@@ -126,6 +126,7 @@ extern "C" kda_status kda_cache_append(const kda_cache *cache, int64_t seqlen, c
     for (const void *p : {k, v, q, (const void *)k_out, (const void *)q_out})
         if (!aligned(p, 16)) return fail(KDA_ERR_INVALID_ARG, "kda_cache_append: tensors must be 16-byte aligned");
     if (cu_seqlens && (seqlen > 0x7fffffffLL || !aligned(cu_seqlens, 4))) return fail(KDA_ERR_INVALID_ARG, "cu_seqlens is misaligned or seqlen exceeds its int32 range");
+    if (seqlen > 1 << 30) return fail(KDA_ERR_UNSUPPORTED, "more than 2^30 new tokens");
     a.k = static_cast<const uint16_t *>(k);
     a.v = static_cast<const uint16_t *>(v);
     a.q = static_cast<const uint16_t *>(q);
@@ -140,7 +141,7 @@ extern "C" kda_status kda_cache_append(const kda_cache *cache, int64_t seqlen, c
     const int64_t per_seq = cu_seqlens ? 0 : (seqlen + c.page_size - 2) / c.page_size + 1;
     const int64_t slots = c.num_seqs == 0 ? 0 : cu_seqlens ? seqlen / c.page_size + 2 * (int64_t)c.num_seqs : per_seq * c.num_seqs;
     // (a launch has fewer than 2^32 threads: up to 512 a page and head, and dim / 8 a row of q)
-    if (slots * c.heads_kv * 2 > 0x3fffff || a.tokens * c.heads_q > 0x7ffffff || a.tokens * c.heads_kv > 0x7ffffff)
+    if (slots > 0x1fffff || slots * c.heads_kv * 2 > 0x3fffff || a.tokens * c.heads_q > 0x7ffffff || a.tokens * c.heads_kv > 0x7ffffff)
         return fail(KDA_ERR_UNSUPPORTED, "more than 2^22 pages and heads, or 2^27 rows of k or q");
     a.slots = (int32_t)slots;
     a.slots_per_seq = (int32_t)per_seq;

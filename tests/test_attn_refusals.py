@@ -32,7 +32,8 @@ BAD_DIMS = [(dict(batch=-1), INVALID), (dict(seqlen=-1), INVALID), (dict(heads_q
             (dict(sinks=65), UNSUPPORTED), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
             (dict(scale=float("inf")), INVALID), (dict(num_seqs=3), INVALID), (dict(q_stride=511), INVALID), (dict(q_stride=504), INVALID),
             (dict(k_stride=260), INVALID), (dict(v_stride=1 << 25), INVALID), (dict(batch=1, num_seqs=1, seqlen=1 << 40), UNSUPPORTED),
-            (dict(batch=1 << 20, num_seqs=1 << 20, seqlen=4096), UNSUPPORTED)]
+            (dict(batch=1 << 20, num_seqs=1 << 20, seqlen=4096), UNSUPPORTED),
+            (dict(batch=1 << 27, num_seqs=1 << 27, seqlen=1 << 30, heads_q=32), UNSUPPORTED)]          # (2^64 threads)
 
 
 @pytest.mark.parametrize("change,status", BAD_DIMS)
@@ -119,6 +120,9 @@ def test_cache_append_refuses():
     assert _append(c, rope=kda.KdaRope(inv_freq=None, num_freqs=64)) == INVALID
     assert _append(c, seqlen=1 << 40) == UNSUPPORTED and _append(_cache(num_seqs=1 << 27)) == UNSUPPORTED
     assert _append(_cache(num_seqs=1 << 22, heads_q=128), q=SOME, q_out=SOME) == UNSUPPORTED
+    for page in (16, 32, 64, 128):                                                 # (2^64 tokens' heads, or pages')
+        for n, hk in ((27, 64), (28, 32), (27, 128), (28, 64), (26, 128), (30, 16)):
+            assert _append(_cache(num_seqs=1 << n, heads_q=hk, heads_kv=hk, page_size=page), seqlen=1 << 36) == UNSUPPORTED
     assert _append(c, seqlen=0, k=None, v=None) == 0 and _append(_cache(num_seqs=0)) == 0
 
 
