@@ -110,10 +110,8 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
     auto step = [&](int it, auto parity, auto sums_only) {
         constexpr int P = decltype(parity)::value;
         constexpr bool kSumsOnly = decltype(sums_only)::value;
-        if constexpr (!kSumsOnly) {
-            tile_barrier();
-            if (it + 1 < steps) issue(it + 1, P ^ 1);
-        }
+        tile_barrier();
+        if (it + 1 < steps) issue(it + 1, P ^ 1);
         const int k0 = first_key(it);
         const uint32_t kt = lds + 2 * P * kT, vt = kt + kT;
         if (k0 > wlast || (s.window && k0 + kTile - 1 <= wq0 - s.window && k0 >= s.sinks)) return;
@@ -161,17 +159,21 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
     };
     using First = std::integral_constant<int, 0>;
     using Second = std::integral_constant<int, 1>;
-    // In a row that sees few keys d is as large as do . v, and o's rounding in it as large as that of dS.  Where the two buffers hold all
-    // the keys there are, d is summed from P and do . v first (dQ at 2 x 200 tokens: 2.7e-3 off without, 2.4e-3 with, for 0.4 us; longer
-    // walks have few such rows).
-    if (steps <= 2) {
-        if (steps == 2) issue(1, 1);
-        tile_barrier();
+    // In a row that sees few keys d is as large as do . v, and o's rounding in it as large as that of dS.  Where all rows see few, in a
+    // short walk or with a small window, d is summed from P and do . v first.  dQ at 2 x 200 tokens: 2.7e-3 off without, 2.4e-3 with, for 0.4 us;
+    // with a window of 16 2.5e-3 and 2.35e-3, 16 384 tokens x 16 heads 202 and 217 us; of 64 2.4e-3 and 2.35e-3, 252 and 280 us.
+    if (steps <= 2 || (s.window && s.window <= kCols)) {
         delta = 0.f;
-        step(0, First{}, std::true_type{});
-        if (steps == 2) step(1, Second{}, std::true_type{});
+        for (int it = 0; it < steps; it += 2) {
+            step(it, First{}, std::true_type{});
+            if (it + 1 < steps) step(it + 1, Second{}, std::true_type{});
+        }
         delta = rest + other_half(rest);
         rest = 0.f;
+        if (steps > 2) {                                     // (else both tiles are there still)
+            tile_barrier();
+            issue(0, 0);
+        }
     }
     for (int it = 0; it < steps; it += 2) {
         step(it, First{}, std::false_type{});

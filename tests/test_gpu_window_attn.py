@@ -244,13 +244,14 @@ def test_a_row_of_a_single_key_has_gradients_of_v_alone(d, T, window):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-def test_rows_of_few_keys_lose_nothing_to_the_rounding_of_o(d):
+@pytest.mark.parametrize("T,window,sinks", [(64, 0, 0), (500, 3, 0), (500, 10, 2)])
+def test_rows_of_few_keys_lose_nothing_to_the_rounding_of_o(d, T, window, sinks):
     """dQ is rounded twice, in dS and at the end.  A rounding to bf16 is uniform in half a step of 2^-8, 2^-8 / sqrt(3) * sqrt(3 / (8 ln 2)) =
-    1.66e-3 of the value in the mean square over an octave; two independent ones 2.35e-3.  A tenth more covers the draw (2048 rows).  With d
-    from the rounded o there would be a third."""
-    x = _make(4, 64, 8, 8, d, 67)
-    got = _np(_grads(x, 0, 0)[2]["dq"])
-    ref = sa.attention_backward(*(_np(x[n]) for n in ("q", "k", "v", "do")))["dq"]
+    1.66e-3 of the value in the mean square over an octave; two independent ones 2.35e-3.  A tenth more covers the draw (2048 rows and more).
+    With d from the rounded o there would be a third."""
+    x = _make(4, T, 8, 8, d, 67)
+    got = _np(_grads(x, window, sinks)[2]["dq"])
+    ref = sa.attention_backward(*(_np(x[n]) for n in ("q", "k", "v", "do")), window, sinks)["dq"]
     assert np.linalg.norm(got - ref) <= 2.6e-3 * np.linalg.norm(ref)
 
 
