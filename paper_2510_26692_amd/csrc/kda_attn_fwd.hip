@@ -16,13 +16,15 @@
 namespace kda {
 namespace attn {
 
-// Keys of a tile: as many as leave registers for three waves a SIMD, whose products and exponentials overlap.  us with 32 keys and three
-// waves / 64 and two: d 128, 65536 tokens x 16 heads, window 1024: 678 / 702, 4 x 4096 x 16 causal 318 / 318; d 64 with 64 keys and three /
-// two: 8 x 4096 x 32 causal 648 / 681, 32768 x 16, window 256: 83 / 100.
-template <int D> constexpr int kFwdKeys = D == 128 ? 32 : 64;
+// Keys of a tile.  At d 64 they are 64, with registers for three waves a SIMD (8 x 4 096 x 32 heads causal 648 us, with two waves 681).  At d 128
+// 64 leave two waves, 32 three, whose products and exponentials overlap better, but whose walks have twice the steps.  us with 32 / 64: 333
+// tokens x 32 heads causal 12.7 / 11.2, 2 000 x 8 53 / 41, 4 x 2 000 x 32 147 / 144, 4 x 4 096 x 16 293 / 295, 16 384 x 16 1 017 / 1 014; with a
+// window, whose walks have ends that only some of the waves need, of 512 at 2 000 x 8 22 / 19, at 8 000 x 16 (1 000 workgroups) 55 / 53, at 16 000 x 16 97 /
+// 100, of 1 024 at 65 536 x 16 628 / 656, of 2 048 1 085 / 1 112.  So 32 are for a window and more workgroups than this.
+constexpr int kMany = 1024;
 
 // o and lse of 128 queries.  Returns true where the walk has to be repeated with care.
-template <int D, bool kOutBf16, bool kCareful>
+template <int D, bool kOutBf16, int kKeys, bool kCareful>
 __device__ __forceinline__ bool fwd_tile(const Shape &s, const uint16_t *q, const uint16_t *k, const uint16_t *v, void *o, float *lse, const uint32_t lds)
 {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, x = lane & 31, h = lane >> 5;
@@ -38,7 +40,6 @@ __device__ __forceinline__ bool fwd_tile(const Shape &s, const uint16_t *q, cons
 
     TileReader<D> rd;
     rd.init(lane);
-    constexpr int kKeys = kFwdKeys<D>;
     TileLoader<D, kKeys> lk, lv;
     const uint32_t ks_bytes = s.k_stride * 2, vs_bytes = s.v_stride * 2;
     lk.init(wave, lane, ks_bytes);
@@ -179,17 +180,17 @@ __device__ __forceinline__ bool fwd_tile(const Shape &s, const uint16_t *q, cons
     }
     return !kCareful && repeat(bad, lds);
 }
-template <int D, bool kOutBf16>
+template <int D, bool kOutBf16, int kKeys>
 __device__ __noinline__ void fwd_tile_again(const Shape s, const uint16_t *q, const uint16_t *k, const uint16_t *v, void *o, float *lse, const uint32_t lds)
 {
-    fwd_tile<D, kOutBf16, true>(s, q, k, v, o, lse, lds);
+    fwd_tile<D, kOutBf16, kKeys, true>(s, q, k, v, o, lse, lds);
 }
-template <int D, bool kOutBf16>
-__global__ __launch_bounds__(kThreads, 3) void kda_attn_fwd_kernel(const Shape s, const uint16_t *q, const uint16_t *k, const uint16_t *v, void *o, float *lse)
+template <int D, bool kOutBf16, int kKeys>
+__global__ __launch_bounds__(kThreads, D == 128 && kKeys == 64 ? 2 : 3) void kda_attn_fwd_kernel(const Shape s, const uint16_t *q, const uint16_t *k, const uint16_t *v, void *o, float *lse)
 {
     constexpr uint32_t lds = kLds;
-    if (!fwd_tile<D, kOutBf16, false>(s, q, k, v, o, lse, lds)) return;
-    fwd_tile_again<D, kOutBf16>(s, q, k, v, o, lse, lds);
+    if (!fwd_tile<D, kOutBf16, kKeys, false>(s, q, k, v, o, lse, lds)) return;
+    fwd_tile_again<D, kOutBf16, kKeys>(s, q, k, v, o, lse, lds);
 }
 
 }  // namespace attn
@@ -200,19 +201,24 @@ using namespace kda::attn;
 
 namespace kda {
 
-template <int D, bool kOutBf16>
+template <int D, bool kOutBf16, int kKeys>
 static hipError_t launch_fwd(const Shape &s, const void *q, const void *k, const void *v, void *o, float *lse, hipStream_t st)
 {
-    constexpr int kLds = 4 * kFwdKeys<D> * D * 2;                  // K and V of the tile in work and of the next
-    hipLaunchKernelGGL((kda_attn_fwd_kernel<D, kOutBf16>), dim3((uint32_t)s.slots * s.heads_q), dim3(kThreads), kLds, st, s,
+    constexpr int kLds = 4 * kKeys * D * 2;                        // K and V of the tile in work and of the next
+    hipLaunchKernelGGL((kda_attn_fwd_kernel<D, kOutBf16, kKeys>), dim3((uint32_t)s.slots * s.heads_q), dim3(kThreads), kLds, st, s,
                        static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k), static_cast<const uint16_t *>(v), o, lse);
     return hipGetLastError();
+}
+template <bool kOutBf16> static hipError_t launch_fwd(const Shape &s, int dim, const void *q, const void *k, const void *v, void *o, float *lse, hipStream_t st)
+{
+    if (dim == 64) return launch_fwd<64, kOutBf16, 64>(s, q, k, v, o, lse, st);
+    if (s.window && (int64_t)s.slots * s.heads_q > kMany) return launch_fwd<128, kOutBf16, 32>(s, q, k, v, o, lse, st);
+    return launch_fwd<128, kOutBf16, 64>(s, q, k, v, o, lse, st);
 }
 
 kda_status attn_fwd_dispatch(const Shape &s, int dim, bool out_bf16, const void *q, const void *k, const void *v, void *o, float *lse, hipStream_t st)
 {
-    const hipError_t e = dim == 128 ? (out_bf16 ? launch_fwd<128, true>(s, q, k, v, o, lse, st) : launch_fwd<128, false>(s, q, k, v, o, lse, st))
-                                    : (out_bf16 ? launch_fwd<64, true>(s, q, k, v, o, lse, st) : launch_fwd<64, false>(s, q, k, v, o, lse, st));
+    const hipError_t e = out_bf16 ? launch_fwd<true>(s, dim, q, k, v, o, lse, st) : launch_fwd<false>(s, dim, q, k, v, o, lse, st);
     return e == hipSuccess ? KDA_OK : fail(KDA_ERR_LAUNCH, "kda_window_attn_fwd: %s", hipGetErrorString(e));
 }
 

@@ -92,6 +92,32 @@ def test_backward(B, T, Hq, Hk, d, window, sinks):
     _check_bwd(x, _grads(x, window, sinks)[2], window, sinks)
 
 
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,window,sinks", [(261, 70, 5), (200, 33, 0), (290, 200, 64), (190, 1, 1)])
+def test_forward_of_many_rows_with_a_window(T, window, sinks, out_dtype):
+    """More workgroups than the device has places for: tiles of 32 keys.  A value that is not finite reaches its own row's queries alone."""
+    import paper_2510_26692_amd as kda
+    x = _make(48, T, 12, 3, 128, T)
+    c = {n: t.cuda() for n, t in x.items()}
+    call = lambda: kda.kda_window_attn_fwd(c["q"], c["k"], c["v"], window=window, sinks=sinks, out_dtype=out_dtype)
+    o, lse = call()
+    _check_fwd(x, o, lse, sa.attention(*(_np(x[n]) for n in "qkv"), window, sinks), out_dtype)
+    c["v"][7, 130, 1, 5] = math.inf
+    bad = ~torch.isfinite(call()[0]).all(-1).cpu()
+    want = torch.zeros_like(bad)
+    want[7, :, 4:8] = torch.from_numpy(sa.visible(np.arange(T), [130], window, sinks))
+    assert torch.equal(bad, want)
+
+
+def test_forward_of_many_packed_sequences_with_a_window():
+    lens = np.random.default_rng(3).integers(0, 90, 120)
+    cu = np.concatenate([[0], np.cumsum(lens)]).tolist()
+    import paper_2510_26692_amd as kda
+    x = _make(1, cu[-1], 10, 2, 128, 11)
+    o, lse = kda.kda_window_attn_fwd(*(x[n].cuda() for n in "qkv"), window=20, sinks=3, cu_seqlens=torch.tensor(cu, dtype=torch.int32, device="cuda"))
+    _check_fwd(x, o, lse, sa.attention(*(_np(x[n]) for n in "qkv"), 20, 3, cu), torch.float32)
+
+
 PACKED = [([5, 0, 300, 128, 1, 129, 700], 3, 6, 50, 3), ([1], 0, 0, 0, 0), ([0, 0, 64], 64, 200, 20, 64), ([256, 384], 0, 0, 0, 0), ([2000, 1, 130], 1, 0, 31, 40)]
 
 

@@ -71,9 +71,10 @@ def test_fp32_kernels_use_no_scratch_beyond_a_few_dwords_of_the_gradients_kernel
 def test_softmax_attention_kernels_keep_their_waves(resources):
     # (stack: of the call that repeats a walk with care, which is not in the loop; what the loops themselves spill is nothing)
     fwd, dq, dkv = (_kernels(resources, "kda_attn_%s_kernel" % n) for n in ("fwd", "dq", "dkv"))
-    assert len(fwd) == 4 and len(dq) == 2 and len(dkv) == 2
-    for name, r in fwd.items():
-        assert r["Occupancy [waves/SIMD]"] >= 3 and r["VGPRs Spill"] == 0, (name, r)
+    assert len(fwd) == 6 and len(dq) == 2 and len(dkv) == 2
+    for name, r in fwd.items():                              # (64 keys of 128 channels a tile: two waves)
+        wide = "Li128E" in name and "Li64E" in name
+        assert r["Occupancy [waves/SIMD]"] >= (2 if wide else 3) and r["VGPRs Spill"] == 0, (name, r)
     for name, r in (dq | dkv).items():
         assert r["Occupancy [waves/SIMD]"] >= 2 and ("Li128E" not in name or r["VGPRs Spill"] == 0), (name, r)
     attend, append = _kernels(resources, "kda_cache_attn_kernel"), _kernels(resources, "kda_cache_append_kernel")
