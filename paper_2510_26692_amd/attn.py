@@ -7,7 +7,7 @@ import ctypes
 import torch
 
 from . import kda as _kda
-from .kda import KdaError, _DTYPE_CODE, _check_dev, _clear_unowned, _out_dtype, _ptr, _stream_ptr, kda_last_error, load_library
+from .kda import KdaError, _DTYPE_CODE, _call, _check_dev, _clear_unowned, _out_dtype, _ptr, kda_last_error, load_library
 
 
 _APPEND_ZERO_Q, _APPEND_ZERO_K = 1, 2    # flags of kda_cache_append
@@ -38,17 +38,6 @@ class KdaCacheQuery(ctypes.Structure):
     """Mirror of ``kda_cache_query``."""
     _fields_ = [("tokens", ctypes.c_int32), ("q_stride", ctypes.c_int64), ("window", ctypes.c_int64), ("sinks", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("max_kv_len", ctypes.c_int64), ("out_dtype", ctypes.c_int)]
-
-
-def _call(dev, entry, *args):
-    """One call of the library on dev's current stream, with dev the current device (launches go to that one)."""
-    if torch.cuda.current_device() == dev.index:
-        st = entry(*args, _stream_ptr(dev))
-    else:
-        with torch.cuda.device(dev):
-            st = entry(*args, _stream_ptr(dev))
-    if st != 0:
-        raise KdaError(st, kda_last_error())
 
 
 def _native(name, *args):

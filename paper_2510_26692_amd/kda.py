@@ -277,6 +277,17 @@ def _stream_ptr(dev):
     return ctypes.c_void_p(_raw_stream(dev.index))
 
 
+def _call(dev, entry, *args):
+    """One call of the library on dev's current stream, with dev the current device (launches go to that one)."""
+    if torch.cuda.current_device() == dev.index:
+        st = entry(*args, _stream_ptr(dev))
+    else:
+        with torch.cuda.device(dev):
+            st = entry(*args, _stream_ptr(dev))
+    if st != 0:
+        raise KdaError(st, kda_last_error())
+
+
 def _result(done):
     """What the native way returned: the tensor, or the status of a call the library refused."""
     if type(done) is int:
@@ -299,10 +310,7 @@ def _clear_unowned(cu_seqlens, tensors):
     n, tokens = len(tensors), tensors[0].shape[1]
     ptrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors])
     rows = (ctypes.c_size_t * n)(*[t.numel() // tokens * t.element_size() for t in tensors])
-    st = load_library().kda_clear_unowned_rows(_ptr(cu_seqlens), cu_seqlens.numel() - 1, tokens, n, ptrs, rows,
-                                               _stream_ptr(cu_seqlens.device))
-    if st != 0:
-        raise KdaError(st, kda_last_error())
+    _call(cu_seqlens.device, load_library().kda_clear_unowned_rows, _ptr(cu_seqlens), cu_seqlens.numel() - 1, tokens, n, ptrs, rows)
 
 
 def _out_dtype(o, out_dtype):
