@@ -143,6 +143,7 @@ PyObject *step(PyObject *, PyObject *const *a, Py_ssize_t n)
         const float scale = number(a[6]);
         const at::Tensor o = output(a[7], a[8], v, check);
         const kda_dims d = decode_dims(N, 1, H, dk, dv, in, code(o.scalar_type()), scale);
+        const c10::DeviceGuard on(q.device());
         void *stream = stream_of(check.device);
         kda_status st;
         Py_BEGIN_ALLOW_THREADS
@@ -196,6 +197,7 @@ PyObject *steps(PyObject *, PyObject *const *a, Py_ssize_t n)
         const at::Tensor o = output(a[8], a[9], v, check);
         const kda_dims d = decode_dims(N, T, H, dk, dv, in, code(o.scalar_type()), scale);
         const uint32_t flags = (form == 1 ? KDA_STEPS_SCALAR_GATE : 0) | (a[8] == Py_None ? KDA_STEPS_ZERO_SKIPPED : 0);
+        const c10::DeviceGuard on(q.device());
         void *stream = stream_of(check.device);
         kda_status st;
         Py_BEGIN_ALLOW_THREADS

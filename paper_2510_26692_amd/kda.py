@@ -350,11 +350,8 @@ def kda_chunk_fwd_check(dims, workspace):
     `workspace` with `dims` reported a failed wait (see kda_chunk_fwd_check in kda.h)."""
     if workspace is None:
         return
-    st = load_library().kda_chunk_fwd_check(ctypes.byref(dims), _ptr(workspace),
-                                            ctypes.c_size_t(workspace.numel() * workspace.element_size()),
-                                            _stream_ptr(workspace.device))
-    if st != 0:
-        raise KdaError(st, kda_last_error())
+    _call(workspace.device, load_library().kda_chunk_fwd_check, ctypes.byref(dims), _ptr(workspace),
+          ctypes.c_size_t(workspace.numel() * workspace.element_size()))
 
 
 def _make_prologue(H, dk, l2norm_eps, a_scale, dt_bias):
@@ -436,16 +433,14 @@ def kda_chunk_fwd(q, k, v, log_alpha, beta, h0=None, cu_seqlens=None, scale=1.0,
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev) if need else None
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     tail = (_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta), _ptr(h0), _ptr(cu_seqlens), _ptr(o),
-            _ptr(hT), _ptr(workspace), ctypes.c_size_t(ws_bytes), _stream_ptr(dev))
+            _ptr(hT), _ptr(workspace), ctypes.c_size_t(ws_bytes))
     if _scalar_gate:
-        st = lib.kda_chunk_fwd_scalar_gate(ctypes.byref(dims), *tail)
+        _call(dev, lib.kda_chunk_fwd_scalar_gate, ctypes.byref(dims), *tail)
     elif _fused is None:
-        st = lib.kda_chunk_fwd(ctypes.byref(dims), *tail)
+        _call(dev, lib.kda_chunk_fwd, ctypes.byref(dims), *tail)
     else:
-        st = lib.kda_chunk_fwd_fused(ctypes.byref(dims), *[None if f is None else ctypes.byref(f) for f in _fused],
-                                     *tail)
-    if st != 0:
-        raise KdaError(st, kda_last_error())
+        _call(dev, lib.kda_chunk_fwd_fused, ctypes.byref(dims), *[None if f is None else ctypes.byref(f) for f in _fused],
+              *tail)
     if clear:                               # (behind the call, whose launch need not wait for this one's)
         _clear_unowned(cu_seqlens, [o])
     if check:
@@ -474,10 +469,8 @@ def kda_chunk_fwd_static_scratch(q, k, v, log_alpha, beta, o, hT=None, h0=None, 
     for name, t in (("hT", hT), ("h0", h0)):
         if t is not None and (t.dtype != torch.float32 or t.shape != (N, H, dk, dv)):
             raise ValueError("%s must be fp32 [N,H,dk,dv]" % name)
-    st = lib.kda_chunk_fwd_static_scratch(ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta),
-                                          _ptr(h0), _ptr(cu_seqlens), _ptr(o), _ptr(hT), _stream_ptr(dev))
-    if st != 0:
-        raise KdaError(st, kda_last_error())
+    _call(dev, lib.kda_chunk_fwd_static_scratch, ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta),
+          _ptr(h0), _ptr(cu_seqlens), _ptr(o), _ptr(hT))
     return o, hT
 
 
@@ -533,12 +526,10 @@ def kda_chunk_bwd(q, k, v, log_alpha, beta, do, dhT=None, h0=None, cu_seqlens=No
         need = kda_chunk_bwd_workspace_size(dims)
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev) if need else None
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    st = lib.kda_chunk_bwd(ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta), _ptr(h0),
-                           _ptr(cu_seqlens), _ptr(do), _ptr(dhT), _ptr(out["dq"]), _ptr(out["dk"]),
-                           _ptr(out["dv"]), _ptr(out["dlog_alpha"]), _ptr(out["dbeta"]), _ptr(out["dh0"]),
-                           _ptr(workspace), ctypes.c_size_t(ws_bytes), _stream_ptr(dev))
-    if st != 0:
-        raise KdaError(st, kda_last_error())
+    _call(dev, lib.kda_chunk_bwd, ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta), _ptr(h0),
+          _ptr(cu_seqlens), _ptr(do), _ptr(dhT), _ptr(out["dq"]), _ptr(out["dk"]),
+          _ptr(out["dv"]), _ptr(out["dlog_alpha"]), _ptr(out["dbeta"]), _ptr(out["dh0"]),
+          _ptr(workspace), ctypes.c_size_t(ws_bytes))
     if clear:                               # (behind the call, as in kda_chunk_fwd)
         _clear_unowned(cu_seqlens, clear)
     return out
@@ -575,10 +566,7 @@ def kda_recurrent_step(q, k, v, log_alpha, beta, S, scale=1.0, o=None, out_dtype
         raise ValueError("o must have shape [N,H,dv]")
     dims = KdaDims(batch=N, seqlen=1, heads=H, dk=dk, dv=dv, chunk=64, num_seqs=N,
                    in_dtype=_DTYPE_CODE[q.dtype], out_dtype=_DTYPE_CODE[odt], scale=float(scale), max_seqlen=0)
-    st = lib.kda_recurrent_step(ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha),
-                                _ptr(beta), _ptr(S), _ptr(o), _stream_ptr(dev))
-    if st != 0:
-        raise KdaError(st, kda_last_error())
+    _call(dev, lib.kda_recurrent_step, ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta), _ptr(S), _ptr(o))
     return o
 
 
@@ -638,9 +626,6 @@ def kda_recurrent_steps_pooled(q, k, v, log_alpha, beta, S_pool, state_indices=N
     dims = KdaDims(batch=N, seqlen=Tq, heads=H, dk=dk, dv=dv, chunk=64, num_seqs=N,
                    in_dtype=_DTYPE_CODE[q.dtype], out_dtype=_DTYPE_CODE[odt], scale=float(scale), max_seqlen=0)
     pro, epi = _fused or (None, None)
-    st = lib.kda_recurrent_steps(ctypes.byref(dims), None if pro is None else ctypes.byref(pro), None if epi is None else ctypes.byref(epi),
-                                 _ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta), _ptr(S_pool), _ptr(state_indices), _ptr(o),
-                                 flags, _stream_ptr(dev))
-    if st != 0:
-        raise KdaError(st, kda_last_error())
+    _call(dev, lib.kda_recurrent_steps, ctypes.byref(dims), None if pro is None else ctypes.byref(pro), None if epi is None else ctypes.byref(epi),
+          _ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta), _ptr(S_pool), _ptr(state_indices), _ptr(o), flags)
     return o

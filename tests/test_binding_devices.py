@@ -10,16 +10,22 @@ from paper_2510_26692_amd import kda as binding
 
 class Elsewhere:
     """As much of a tensor on device 1 as marshalling looks at."""
-    device = torch.device("cuda", 1)
+    device, is_cuda = torch.device("cuda", 1), True
 
-    def __init__(self, *shape):
-        self.shape = torch.Size(shape)
+    def __init__(self, *shape, dtype=torch.bfloat16):
+        self.shape, self.dtype = torch.Size(shape), dtype
 
     def numel(self):
         return self.shape.numel()
 
     def element_size(self):
-        return 2
+        return self.dtype.itemsize
+
+    def is_contiguous(self):
+        return True
+
+    def dim(self):
+        return len(self.shape)
 
     def data_ptr(self):
         return 1 << 20
@@ -59,3 +65,32 @@ def test_rows_of_nobody_are_cleared_on_the_tensors_device(monkeypatch, current):
         binding._clear_unowned(Elsewhere(4), [Elsewhere(1, 50, 2, 64), Elsewhere(1, 50, 8)])
         assert current[0] == index
     assert seen == [(1, 101, 3, 50, [256, 16])] * 2
+
+
+def test_kda_calls_launch_on_the_tensors_device(monkeypatch, current):
+    seen = []
+
+    class Library:
+        def __getattr__(self, name):
+            def entry(*args):
+                seen.append((name, current[0], args[-1].value))
+                return 0
+            return entry
+
+    monkeypatch.setattr(binding, "load_library", Library)
+    monkeypatch.setattr(binding, "_native", None)
+    x, g, f32 = Elsewhere(1, 70, 2, 64), Elsewhere(1, 70, 2), torch.float32
+    state, ws = Elsewhere(1, 2, 64, 64, dtype=f32), Elsewhere(1 << 20, dtype=torch.uint8)
+    grads = {n: Elsewhere(1, 70, 2, 64, dtype=f32) for n in ("dq", "dk", "dv", "dlog_alpha")}
+    grads.update(dbeta=Elsewhere(1, 70, 2, dtype=f32), dh0=state)
+    binding.kda_chunk_fwd(x, x, x, x, g, o=x, hT=state, workspace=ws, check=True)
+    binding.kda_chunk_fwd_scalar_gate(x, x, x, g, g, o=x, hT=state, workspace=ws)
+    binding.kda_chunk_fwd_fused(x, x, x, x, g, o=x, hT=state, workspace=ws)
+    binding.kda_chunk_fwd_static_scratch(x, x, x, x, g, x, hT=state)
+    binding.kda_chunk_bwd(x, x, x, x, g, x, workspace=ws, out=grads)
+    one, four = Elsewhere(1, 2, 64), Elsewhere(1, 4, 2, 64)
+    binding.kda_recurrent_step(one, one, one, one, Elsewhere(1, 2), state, o=one)
+    binding.kda_recurrent_steps_pooled(four, four, four, four, Elsewhere(1, 4, 2), state, o=four)
+    assert [s[0] for s in seen] == ["kda_chunk_fwd", "kda_chunk_fwd_check", "kda_chunk_fwd_scalar_gate", "kda_chunk_fwd_fused",
+                                    "kda_chunk_fwd_static_scratch", "kda_chunk_bwd", "kda_recurrent_step", "kda_recurrent_steps"]
+    assert all(s[1:] == (1, 101) for s in seen) and current[0] == 0
