@@ -3,7 +3,9 @@
 // One pass over the keys with a running maximum m and sum l per query: a tile of 32 or 64 keys gives X^T = K Q^T, P^T = 2^(X^T c - m)
 // (c = scale log2 e, fp32) and O^T = O^T 2^(m_old - m) + V^T P^T, P rounded to bf16 (2^-8 a term at most, the operand type of the
 // matrix cores; l sums the unrounded values).  m is moved only when a maximum passes it by more than 8, i.e. terms grow to 2^8 at most,
-// which costs no precision and leaves most tiles without the 64 multiplications of O.
+// which costs no precision and leaves most tiles without the 64 multiplications of O.  Sums of such terms and values of v next to the largest fp32
+// leave its range where o does not: the walk is then repeated as for values that are not finite, with P times 2^-38 on its way to the product
+// (at most 2^30 terms of at most 2^8: no sum is larger than the largest value).
 //
 // What bounds it is the matrix cores, at the clock that the power limit leaves them, with the exponentials beside them: 16 384 tokens x 16
 // heads of 128 causal in 997 us, 1 103 TFLOP/s (a library product of 8192^3: 1 251); 4 x 4 096 x 16 heads 290 us (948); 65 536 x 16 heads, window 1024, 625 us
@@ -129,6 +131,7 @@ __device__ __forceinline__ bool fwd_tile(const Shape &s, const uint16_t *q, cons
             for (int j = 0; j < 16; ++j) {
                 e[j] = fast_exp2(fmaf(st[b][j], c, -mref));
                 l += e[j];
+                if (kCareful) e[j] *= 0x1p-38f;
             }
             p[2 * b] = pack8(e);
             p[2 * b + 1] = pack8(e + 8);
@@ -157,7 +160,7 @@ __device__ __forceinline__ bool fwd_tile(const Shape &s, const uint16_t *q, cons
     const bool bad = !kCareful && not_finite(acc);
     const int mine = wq0 + (again & 31), half = again & 32;
     if (mine < at.len) {
-        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : __builtin_nanf("");
+        const float inv = (l > 0.f ? 1.f / l : l == 0.f ? 0.f : __builtin_nanf("")) * (kCareful ? 0x1p38f : 1.f);
         const int64_t token = at.row0 + mine;
         if (lse && !half) lse[((int64_t)at.batch * (s.heads_q - 1) + head) * s.tokens + token] = l == 0.f ? -kInf : (mref + __log2f(l)) * 0.6931471805599453f;
         const int64_t out = (token * s.heads_q + head) * D + half / 8;

@@ -270,7 +270,7 @@ template <int lead, int valu, int mfmas> __device__ __forceinline__ void reads_a
 
 // ---- values that are not finite in masked places.  A product takes P = 0 times such a value for NaN.  Where that happened (the
 // accumulators say so in the end), the walk is repeated with this on tiles that some column sees only in part: the value is taken
-// out of the product, and every column that does see it becomes NaN. ----
+// out of the product, and every column that does see it becomes NaN.  (Forward, a sum of finite values may have left fp32 as well.) ----
 __device__ __forceinline__ bf16x8 without_nonfinite(const bf16x8 &v, bf16x8 &marks, bool &any)
 {
     u32x4 w = __builtin_bit_cast(u32x4, v), m;
