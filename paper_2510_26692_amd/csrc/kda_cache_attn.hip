@@ -126,7 +126,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Ca
         ks_l = vs_l = 0.f;
         if (u < end) {
             const int32_t key = first_key(u) + 16 * (lane & 1);
-            if (key < st.len) page_l = page_at(c, n, key >> c.page_log2);
+            // (a block that no row sees may belong to a page that is another sequence's by now, and its scale be anything)
+            const bool hidden = a.window && qfirst - key - 15 >= a.window && key >= a.sinks;
+            if (key < st.len && !hidden) page_l = page_at(c, n, key >> c.page_log2);
             if (page_l >= 0) {
                 ks_l = c.k_scale[(int64_t)page_l * c.heads_kv + kv];
                 vs_l = c.v_scale[(int64_t)page_l * c.heads_kv + kv];
