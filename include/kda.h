@@ -515,8 +515,9 @@ typedef struct {
  * nothing (kv_lens[n] <= 0, a position below zero: a batch of sequences with fewer new tokens is padded in front) gets zeros.
  *   q [num_seqs,tokens,heads_q,dim] bf16      o [num_seqs,tokens,heads_q,dim] out_dtype
  *   workspace   at least kda_cache_attn_workspace_size bytes (0 for some calls), 256-byte aligned
- * Scales may be any finite numbers here.  What is not finite reaches the rows that see it and no others, whatever stands behind the
- * last token of a page.
+ * Scales may be any finite numbers here, so that scale * k_scale is finite and, for full precision, v_scale is 2^-110 at least and within a factor
+ * of 2^100 of the sequence and head's largest: results are finite wherever they are in fp32.  What is not finite reaches the rows that see it and no
+ * others, whatever stands behind the last token of a page or in pages that no row sees.
  */
 size_t kda_cache_attn_workspace_size(const kda_cache *cache, const kda_cache_query *query);
 kda_status kda_cache_attn(const kda_cache *cache, const kda_cache_query *query, const void *q, void *o, void *workspace,

@@ -9,7 +9,9 @@
 // order in which a lane's accumulators hold them, {4 g + 0..3, 16 + 4 g + 0..3} (g = lane / 16), and channels to the first so that a lane
 // reads whole 32-byte pieces of a key.  V is read by rows, 8 channels of 8 keys a lane, and its bytes are regrouped in registers.  Scales
 // multiply the 16 logits and numerators of their page, in fp32, so that they may be any numbers.  Statistics as in the prefill: fp32,
-// the maximum moved when it is passed by more than 8.
+// the maximum moved when it is passed by more than 8.  Terms of up to 2^8 times a scale, summed over up to 2^30 keys, leave fp32 where the
+// result does not: the logits of a page whose values' scale is 2^64 or more count 64 more to the maximum, so that no term times its scale is
+// beyond 2^72.
 //
 // What bounds it is reading the cache, 2 D bytes a key and head: 256 sequences of 4 096 to 8 192 tokens, 8 heads of 128, in 560 us (5.7 TB/s;
 // a plain copy moves 5.2 read and written), 4 sequences of up to 131 072 in 134 us (5.1 TB/s), one of 2 000 in 9.5 us, launches and the
@@ -29,6 +31,8 @@ constexpr float kInf = __builtin_huge_valf();
 constexpr int kStep = 32;            // keys of a step
 constexpr int kWaves = 4;
 constexpr int kJoinAlone = 32;       // parts of a row that one wave joins
+constexpr float kLift = 64.f;        // what logits, in powers of two, count more to the maximum where a scale of their values has these bits
+constexpr uint32_t kLargeScale = 0x5f800000u;                // or more: 2^64
 
 // The visible keys of a sequence's new tokens as steps: those of the sinks where the window begins behind them, then the window's.
 struct Steps {
@@ -211,6 +215,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Ca
                 }
         }
         const bool careful = edge && __any(odd);
+        const bool large = (__float_as_uint(w.vs[0]) & 0x7fffffffu) >= kLargeScale || (__float_as_uint(w.vs[1]) & 0x7fffffffu) >= kLargeScale;
+        const float lift = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(large ? kLift : 0.f)));
         bf16x8 pb[RB];
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
@@ -219,6 +225,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Ca
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, s[r][b][i]);
+            top += lift;
             if (__any(top > m[r] + 8.f)) {
                 top = over_groups(top, [](float p, float q) { return fmaxf(p, q); });
                 const float mn = fmaxf(m[r], top), f = mn == -kInf ? 1.f : fast_exp2(m[r] - mn);
