@@ -269,8 +269,10 @@ def _raw_stream(index):
     return torch.cuda.current_stream(index).cuda_stream
 
 
-# (the same number without a Stream object around it: 0.1 instead of 2 us)
+# (the same number without a Stream object around it: 0.1 instead of 2 us; and torch.cuda.current_device() without its look whether
+# the device is in use yet, which a device tensor answers: 0.2 us)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream_ptr(dev):
@@ -279,7 +281,7 @@ def _stream_ptr(dev):
 
 def _call(dev, entry, *args):
     """One call of the library on dev's current stream, with dev the current device (launches go to that one)."""
-    if torch.cuda.current_device() == dev.index:
+    if _current_device() == dev.index:
         st = entry(*args, _stream_ptr(dev))
     else:
         with torch.cuda.device(dev):

@@ -44,7 +44,7 @@ def current(monkeypatch):
         finally:
             at[0] = before
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: at[0])
+    monkeypatch.setattr(binding, "_current_device", lambda: at[0])
     monkeypatch.setattr(torch.cuda, "device", device)
     monkeypatch.setattr(binding, "_raw_stream", lambda index: 100 + index)
     return at
