@@ -419,7 +419,8 @@ typedef struct {
  * Products on the bf16 matrix cores with fp32 accumulation, softmax statistics in fp32, its terms rounded to bf16 ahead of the
  * product with v.  o must not alias an input.  Values that are not finite reach the outputs of the queries that see them and no others: a query that sees a
  * value of v that is not finite gets NaN or an infinity there, in every channel concerned, one that sees a key that is not
- * finite, or is not finite itself, NaN.  (Such a tile is worked through twice.)  o is finite for any finite values of v, however large; the products
+ * finite, or is not finite itself, NaN; but for a logit of minus infinity, whose term is zero, so that the key is as one that is not seen (a query
+ * with no other logits gets zeros, and lse minus infinity).  (Such a tile is worked through twice.)  o is finite for any finite values of v, however large; the products
  * q . k, ahead of the scale, have to stay within fp32.  No workspace.
  */
 kda_status kda_window_attn_fwd(const kda_attn_dims *dims, const void *q, const void *k, const void *v, const int32_t *cu_seqlens,

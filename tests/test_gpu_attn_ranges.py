@@ -56,3 +56,22 @@ def test_gradients_with_large_values(d, window, sinks):
     x = _large(_make(1, 400, 4, 2, d, 9, 0.5), 1, 124)
     x["do"][:, :, 2:] = (x["do"][:, :, 2:].float() * 2.0 ** -124).to(torch.bfloat16)
     _check_bwd(x, _grads(x, window, sinks)[2], window, sinks)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (60, 4)])
+def test_a_key_of_infinities_is_unseen_by_queries_that_point_away_from_it(d, window, sinks):
+    """Logits of minus infinity are terms of zero; those of plus infinity make their rows NaN."""
+    import paper_2510_26692_amd as kda
+    T = 300
+    x = _make(1, T, 2, 1, d, 13)
+    x["k"][0, :, 0, 5] = 0                                    # (the channel is that key's alone)
+    x["k"][0, 100, 0, 5] = math.inf
+    away = torch.arange(T) % 3 != 0
+    x["q"][0, :, :, 5] = torch.where(away[:, None], -1.0, 1.0).to(torch.bfloat16)
+    o, lse = kda.kda_window_attn_fwd(*(x[n].cuda() for n in "qkv"), window=window, sinks=sinks)
+    hit = torch.from_numpy(sa.visible(np.arange(T), [100], window, sinks)[:, 0]) & ~away
+    assert bool(hit.any()) and bool(torch.isnan(o[0, hit]).all()) and bool(torch.isnan(lse[0, :, hit]).all())
+    x["k"][0, 100, 0, 5] = 2.0 ** 15                         # (a term of e^-2000 and less, next to none)
+    ref = sa.attention(*(_np(x[n]) for n in "qkv"), window, sinks)
+    _check_fwd(x, o[:, ~hit], lse[:, :, ~hit], {n: (t[:, :, ~hit] if n == "lse" else t[:, ~hit]) for n, t in ref.items()}, torch.float32)
