@@ -256,18 +256,6 @@ template <int lead, int per, int reads, int mfmas> __device__ __forceinline__ vo
     __builtin_amdgcn_sched_group_barrier(0x008, mfmas - steps, 0);
 }
 
-// The same with `valu` vector instructions behind every MFMA.
-template <int lead, int valu, int mfmas> __device__ __forceinline__ void reads_among()
-{
-    __builtin_amdgcn_sched_group_barrier(0x100, lead, 0);
-#pragma unroll
-    for (int i = 0; i < mfmas; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, valu, 0);
-        if (i < mfmas - lead) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-}
-
 // ---- values that are not finite in masked places.  A product takes P = 0 times such a value for NaN.  Where that happened (the
 // accumulators say so in the end), the walk is repeated with this on tiles that some column sees only in part: the value is taken
 // out of the product, and every column that does see it becomes NaN.  (Forward, a sum of finite values may have left fp32 as well.) ----

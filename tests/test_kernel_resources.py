@@ -89,6 +89,13 @@ def test_softmax_attention_kernels_have_no_lds_but_the_launch_s(resources):
         assert "join" in name or r["LDS Size [bytes/block]"] == 0, (name, r)
 
 
+def test_softmax_attention_gradients_of_64_channels_spill_next_to_nothing(resources):
+    # (their walk with care is in line)
+    for n, spilled in (("dq", 2), ("dkv", 0)):
+        (r,) = [r for name, r in _kernels(resources, "kda_attn_%s_kernel" % n).items() if "Li64E" in name]
+        assert r["VGPRs Spill"] <= spilled, (n, r)
+
+
 _OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"
 
 
