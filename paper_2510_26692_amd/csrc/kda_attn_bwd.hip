@@ -8,9 +8,9 @@
 // workgroups, over parts of the group, whose fp32 sums a last kernel adds.  The sinks' keys are seen by every later query: what lies beyond
 // their window is walked by workgroups of its own, in parts.
 //
-// What bounds it is the matrix cores: 16 384 tokens x 16 heads of 128 causal in 3 400 us, 809 TFLOP/s for the 5 products that a gradient
-// needs and 1 132 for the 7 done; 4 x 4 096 x 16 heads over 4 in 960 us (716 and 1 002), 50 of them for the sums of the parts.  A window of
-// 1024 costs a fifth more a visible pair: every walk has two partly seen ends.
+// What bounds it is the matrix cores: 16 384 tokens x 16 heads of 128 causal in 3 550 us, 775 TFLOP/s for the 5 products that a gradient
+// needs and 1 084 for the 7 done; 4 x 4 096 x 16 heads over 4 in 985 us (698 and 977), 29 of them for the sums of the parts.  A window of
+// 1024 costs a fifth more a visible pair (65 536 x 16 heads over 2, 2 130 us): every walk has two partly seen ends.
 #include <algorithm>
 #include <type_traits>
 
@@ -200,9 +200,9 @@ template <int D, bool kCareful> __device__ __forceinline__ bool dq_tile(const Sh
     }
     return !kCareful && repeat(bad, lds);
 }
-// The walk with care is a call at d 128, where in line it takes registers from the loop that always runs (dK / dV: 78 spilled without it,
-// 261 with it); at d 64 there are enough, and the call's stack costs more (us in line / called, d 64: 8 x 4096 x 32 heads 2290 / 2370,
-// 2 x 200 x 4 heads, forward and backward, 28.0 / 29.5; d 128: 4 x 4096 x 16 heads 1090 / 1041).
+// The walk with care is a call at d 128, where in line it takes registers from the loop that always runs (spilled in line: dQ 13, dK / dV 94; none
+// as calls); at d 64 there are enough (dQ 2, dK / dV none), and the call's stack costs more.  us in line / called, d 64: 8 x 4096 x 32 heads 2 119 /
+// 2 128, 2 x 200 x 4 heads 20.7 / 20.9; d 128: 4 x 4096 x 16 heads over 4 996 / 985.
 template <int D> __device__ __noinline__ void dq_tile_again(const Shape s, const Back g, const uint32_t lds) { dq_tile<D, true>(s, g, lds); }
 template <int D> __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kda_attn_dq_kernel(const Shape s, const Back g)
 {

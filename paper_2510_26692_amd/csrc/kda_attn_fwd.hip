@@ -7,9 +7,10 @@
 // leave its range where o does not: the walk is then repeated as for values that are not finite, with P times 2^-38 on its way to the product
 // (at most 2^30 terms of at most 2^8: no sum is larger than the largest value).
 //
-// What bounds it is the matrix cores, at the clock that the power limit leaves them, with the exponentials beside them: 16 384 tokens x 16
-// heads of 128 causal in 997 us, 1 103 TFLOP/s (a library product of 8192^3: 1 251); 4 x 4 096 x 16 heads 290 us (948); 65 536 x 16 heads, window 1024, 625 us
-// (880, the edges' tiles counted as they are seen); d 64, 8 x 4 096 x 32 heads 640 us (859: as many exponentials for half the product).
+// What bounds it is the matrix cores, at the clock that the power limit leaves them, with the exponentials beside them.  Medians of 7 stretches of 20 runs behind 60
+// others (a device that comes from rest takes up to 40 % longer at first): 16 384 tokens x 16 heads of 128 causal in 1 040 us, 1 055 TFLOP/s (a library
+// product of 8192^3: 1 251 to 1 304); 4 x 4 096 x 16 heads 275 us (1 000); 65 536 x 16 heads, window 1024, 634 us (860, the visible pairs
+// counted); d 64, 8 x 4 096 x 32 heads 661 us (830: as many exponentials for half the product).
 // A third buffer of tiles, wave priorities and reads ahead of the products were tried and gave nothing.
 #include <type_traits>
 
@@ -19,7 +20,7 @@ namespace kda {
 namespace attn {
 
 // Keys of a tile.  At d 64 they are 64, with registers for three waves a SIMD (8 x 4 096 x 32 heads causal 648 us, with two waves 681).  At d 128
-// 64 leave two waves, 32 three, whose products and exponentials overlap better, but whose walks have twice the steps.  us with 32 / 64: 333
+// 64 leave two waves, 32 three, whose products and exponentials overlap better, but whose walks have twice the steps.  Side by side, us with 32 / 64: 333
 // tokens x 32 heads causal 12.7 / 11.2, 2 000 x 8 53 / 41, 4 x 2 000 x 32 147 / 144, 4 x 4 096 x 16 293 / 295, 16 384 x 16 1 017 / 1 014; with a
 // window, whose walks have ends that only some of the waves need, of 512 at 2 000 x 8 22 / 19, at 8 000 x 16 (1 000 workgroups) 55 / 53, at 16 000 x 16 97 /
 // 100, of 1 024 at 65 536 x 16 628 / 656, of 2 048 1 085 / 1 112.  So 32 are for a window and more workgroups than this.

@@ -6,7 +6,8 @@
 //
 // Scales are powers of two, so that a page that grows costs its older codes only the bits that fall below the smallest step, however
 // often it grows, and every cached value is a bf16 number.  Angles are formed as revolutions in 64 bits, p (f / 2 pi) less its nearest
-// whole number: at position 2^31 they are still good to 1e-6, where a product in 32 bits would be off by whole turns.
+// whole number: at position 2^31 they are still good to 1e-6, where a product in 32 bits would be off by whole turns.  Their sines and cosines are
+// in 64 bits as well for keys, whose codes are those of the exact rotation, and the hardware's of the fp32 revolutions for queries.
 //
 // A workgroup has one page of one sequence and head, keys or values: rows of 8-channel pieces in registers, one pass for the largest
 // value, one for the codes.  Further workgroups turn the queries, a token's angles once for several heads.
@@ -173,7 +174,7 @@ template <int D, int kThreads> __device__ __forceinline__ void turn_queries(cons
     constexpr int kPieces = D / 8, kRows = kThreads / kPieces;           // pieces of a row, rows at a time
     const int tid = threadIdx.x, piece = tid % kPieces, row0 = tid / kPieces;
     const int parts = (c.heads_q + a.q_heads - 1) / a.q_heads;
-    Piece t;                                                 // (its loads ahead of those that wait for one another)
+    Piece t;                                                 // (its loads, one after the other, ahead of the tables')
     t.init(a, piece);
     double freq[8];
 #pragma unroll
@@ -244,7 +245,8 @@ template <int D, int kThreads> __device__ __forceinline__ void turn_queries(cons
 // Angles are held in 64 bits, so that the codes are those of the exact rotation (in 32 bits one in 2^21 was another): computed for the
 // lane's first row and for the distance to its next, then multiplied, 4 operations a pair instead of 30, down the rows of one head and up
 // those of the next.  16 prompts (67 000 tokens, 8 key heads and 32 query heads, pages of 64; 1.8 GB): 604 us with an angle formed for each
-// head, 363 so, 5.0 TB/s (a plain copy: 5.2).  256 sequences x 4 tokens: 20 us with a workgroup a page, head and 4 rows, 11 so.
+// head, 352 so, 5.1 TB/s (a plain copy: 4.8 to 5.2).  256 sequences x 4 tokens: 20 us with a workgroup a page, head and 4 rows, 11 so, and 22
+// where every page's scale grows: its older codes are then read and written again, 8 bytes a lane and one round trip after the other.
 template <int D, int kThreads, int kIters>
 __device__ __forceinline__ void append_page(const Cache &c, const Append &a, const Piece &t, const double (&freq)[4], bool turned, bool values, int head0, int n,
                                             int64_t logical, int64_t len, int64_t count, int64_t first_row)
@@ -377,7 +379,7 @@ __device__ __forceinline__ void append_pages(const Cache &c, const Append &a, ui
     const bool values = block & 1;
     const int groups = c.heads_kv / a.page_heads, head0 = (int)((block >> 1) % groups) * a.page_heads, slot = (int)((block >> 1) / groups);
     const bool turned = !values && a.n_freq;
-    Piece t;                                                 // (its loads ahead of those that wait for one another)
+    Piece t;                                                 // (its loads, one after the other, ahead of the tables')
     t.init(a, piece);
     double freq[4];
     t.own_frequencies(a, turned, freq);

@@ -14,7 +14,7 @@
 // beyond 2^72.
 //
 // What bounds it is reading the cache, 2 D bytes a key and head: 256 sequences of 4 096 to 8 192 tokens, 8 heads of 128, in 560 us (5.7 TB/s;
-// a plain copy moves 5.2 read and written), 4 sequences of up to 131 072 in 134 us (5.1 TB/s), one of 2 000 in 9.5 us, launches and the
+// plain reads of 1 to 4 GiB reach 6.7 to 7.0), 4 sequences of up to 131 072 in 135 us (5.1 TB/s), one of 2 000 in 9.5 us, launches and the
 // latency of two steps.  Every wave has a stretch of its own of a sequence's visible keys; the
 // next step's codes are in flight while one is worked on.  The four waves of a workgroup join through LDS, the workgroups of a
 // sequence and head (as many as fill the device) through the workspace and a second kernel, in a fixed order.
@@ -24,7 +24,6 @@ namespace kda {
 namespace cache {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr float kInf = __builtin_huge_valf();
@@ -75,7 +74,7 @@ template <typename F> __device__ __forceinline__ float over_groups(float v, F f)
 }
 
 // RB: blocks of 16 rows.  More than 32 rows go to several workgroups, side by side, which meet in the L2: 64 sequences of up to 8192 tokens,
-// 64 rows, 242 us with two of 32, 334 with four of 16; with one of 64 most of its values stand in scratch (1922).
+// 64 rows, 225 us with two of 32, 334 with four of 16; with one of 64 most of its values stand in scratch (1922).
 template <int D, int RB>
 __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Cache c, const Attend a)
 {
