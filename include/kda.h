@@ -20,7 +20,8 @@
  *   - Calls are asynchronous on `hip_stream` (a hipStream_t passed as void*,
  *     NULL = default stream): every kernel of a call is launched on that stream,
  *     no host synchronisation happens inside (kda_chunk_fwd_check, which exists to
- *     wait, aside), and a call may be captured into a graph.
+ *     wait, aside), and a call may be captured into a graph.  The current device has to
+ *     be that of the tensors and of the stream (the Python binding sees to it).
  *   - Concurrency: calls may be issued from several host threads and on several
  *     streams at once, each with its own workspace (a workspace belongs to one call
  *     until that call has completed).  The bf16 prefill runs its per-chunk stage and

@@ -245,7 +245,7 @@ template <int D, int kThreads> __device__ __forceinline__ void turn_queries(cons
 // Angles are held in 64 bits, so that the codes are those of the exact rotation (in 32 bits one in 2^21 was another): computed for the
 // lane's first row and for the distance to its next, then multiplied, 4 operations a pair instead of 30, down the rows of one head and up
 // those of the next.  16 prompts (67 000 tokens, 8 key heads and 32 query heads, pages of 64; 1.8 GB): 604 us with an angle formed for each
-// head, 352 so, 5.1 TB/s (a plain copy: 4.8 to 5.2).  256 sequences x 4 tokens: 20 us with a workgroup a page, head and 4 rows, 11 so, and 22
+// head, 352 so, 5.1 TB/s (a plain copy: 4.8 to 5.2).  256 sequences x 4 tokens: 20 us with a workgroup a page, head and 4 rows, 11 so, and 23
 // where every page's scale grows: its older codes are then read and written again, 8 bytes a lane and one round trip after the other.
 template <int D, int kThreads, int kIters>
 __device__ __forceinline__ void append_page(const Cache &c, const Append &a, const Piece &t, const double (&freq)[4], bool turned, bool values, int head0, int n,
