@@ -27,6 +27,9 @@ class Elsewhere:
     def dim(self):
         return len(self.shape)
 
+    def stride(self):
+        return (0,) * len(self.shape)                        # (looked at where a tensor is not contiguous)
+
     def data_ptr(self):
         return 1 << 20
 
@@ -93,4 +96,31 @@ def test_kda_calls_launch_on_the_tensors_device(monkeypatch, current):
     binding.kda_recurrent_steps_pooled(four, four, four, four, Elsewhere(1, 4, 2), state, o=four)
     assert [s[0] for s in seen] == ["kda_chunk_fwd", "kda_chunk_fwd_check", "kda_chunk_fwd_scalar_gate", "kda_chunk_fwd_fused",
                                     "kda_chunk_fwd_static_scratch", "kda_chunk_bwd", "kda_recurrent_step", "kda_recurrent_steps"]
+    assert all(s[1:] == (1, 101) for s in seen) and current[0] == 0
+
+
+def test_packed_attention_calls_launch_everything_on_the_tensors_device(monkeypatch, current):
+    """What the calls allocate themselves is cleared behind them: two launches each, on one device and stream."""
+    from paper_2510_26692_amd import attn
+    seen = []
+
+    class Library:
+        def __getattr__(self, name):
+            def entry(*args):
+                if name.endswith("_size"):
+                    return 1024
+                seen.append((name, current[0], args[-1].value))
+                return 0
+            return entry
+
+    fresh = lambda *shape, dtype, device: Elsewhere(*(shape[0] if isinstance(shape[0], torch.Size) else shape), dtype=dtype)
+    for module in (binding, attn):
+        monkeypatch.setattr(module, "load_library", Library)
+    monkeypatch.setattr(binding, "_native", None)
+    monkeypatch.setattr(torch, "empty", fresh)
+    monkeypatch.setattr(torch, "zeros", fresh)
+    q, k, cu = Elsewhere(1, 70, 4, 64), Elsewhere(1, 70, 2, 64), Elsewhere(4, dtype=torch.int32)
+    o, lse = attn.kda_window_attn_fwd(q, k, k, cu_seqlens=cu, out_dtype=torch.bfloat16)
+    attn.kda_window_attn_bwd(q, k, k, o, lse, q, cu_seqlens=cu)
+    assert [s[0] for s in seen] == ["kda_window_attn_fwd", "kda_clear_unowned_rows", "kda_window_attn_bwd", "kda_clear_unowned_rows"]
     assert all(s[1:] == (1, 101) for s in seen) and current[0] == 0
