@@ -421,7 +421,7 @@ typedef struct {
  * product with v.  o must not alias an input.  Values that are not finite reach the outputs of the queries that see them and no others: a query that sees a
  * value of v that is not finite gets NaN or an infinity there, in every channel concerned, one that sees a key that is not
  * finite, or is not finite itself, NaN; but for a logit of minus infinity, whose term is zero, so that the key is as one that is not seen (a query
- * with no other logits gets zeros, and lse minus infinity).  (Such a tile is worked through twice.)  o is finite for any finite values of v, however large; the products
+ * with no other logits gets zeros, and lse minus infinity).  (Such a tile is worked through twice.)  o is finite for values of v up to 2^127; the products
  * q . k, ahead of the scale, have to stay within fp32.  No workspace.
  */
 kda_status kda_window_attn_fwd(const kda_attn_dims *dims, const void *q, const void *k, const void *v, const int32_t *cu_seqlens,
@@ -518,7 +518,7 @@ typedef struct {
  *   q [num_seqs,tokens,heads_q,dim] bf16      o [num_seqs,tokens,heads_q,dim] out_dtype
  *   workspace   at least kda_cache_attn_workspace_size bytes (0 for some calls), 256-byte aligned
  * Scales may be any finite numbers here, so that scale * k_scale is finite and, for full precision, v_scale is 2^-110 at least and within a factor
- * of 2^100 of the sequence and head's largest: results are finite wherever they are in fp32.  What is not finite reaches the rows that see it and no
+ * of 2^100 of the sequence and head's largest: results are finite for values up to 2^127.  What is not finite reaches the rows that see it and no
  * others, whatever stands behind the last token of a page or in pages that no row sees.
  */
 size_t kda_cache_attn_workspace_size(const kda_cache *cache, const kda_cache_query *query);
