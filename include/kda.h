@@ -525,6 +525,139 @@ size_t kda_cache_attn_workspace_size(const kda_cache *cache, const kda_cache_que
 kda_status kda_cache_attn(const kda_cache *cache, const kda_cache_query *query, const void *q, void *o, void *workspace,
                           size_t workspace_bytes, void *hip_stream);
 
+/*
+ * ---- Draft trees: several tokens of a sequence verified at once, of which any path from the root may be accepted ----
+ *
+ * A sequence has up to 64 drafted tokens.  parents[n][t] is the index of the token that token t follows, below t, or -1 where it follows what
+ * the sequence holds.  Any other entry means that there is no token t (sequences of a batch may have fewer than others), and a token whose
+ * parent is not there is not there either.  depth(t): 0 for a token that follows what the sequence holds, else its parent's and one.
+ * A token's ancestors are its parent and its parent's ancestors.
+ *
+ * A step of a hybrid stack: kda_rotate turns queries and keys by the positions of their depths, kda_cache_append (without rope) puts
+ * token t's key and value at place kv_lens[n] + t of the cache, kda_cache_tree_attn and kda_tree_steps read cache and states without changing
+ * them, and once the accepted path is known kda_cache_keep and kda_tree_commit make its tokens what the sequence holds.
+ */
+
+/*
+ * Position rotation by positions of one to four axes (time, height and width of an image's token; one axis: a text's).
+ *   q [B,T,heads_q,dim]   k [B,T,heads_k,dim]   dtype, 16-byte aligned; k may be NULL (heads_k 0)
+ *   positions [axes,B,T]  int32
+ * Channel pair i, (i, i + num_freqs) or interleaved (2 i, 2 i + 1), turns by the angle positions[axis_of_freq[i]][b][t] * inv_freq[i];
+ * channels from 2 * num_freqs on stay as they are.  inverse: by the angle's negative, which is the gradient of the rotation as well: dq, dk from
+ * the gradients of q_out, k_out.  q_out and k_out are contiguous; q_out may be q and k_out k, where those are contiguous; no other
+ * outputs may overlap inputs or one another.  Angles are reduced in 64 bits, products in fp32, each output rounded once.  What is not finite
+ * reaches its own pair alone.
+ */
+typedef struct {
+    int32_t        batch;
+    int64_t        seqlen;
+    int32_t        heads_q, heads_k;
+    int32_t        dim;                /* 64 or 128                                                               */
+    kda_dtype      dtype;              /* of q, k and what is written                                             */
+    int64_t        q_stride, k_stride; /* elements from a token to the next, as in kda_attn_dims                  */
+    int32_t        axes;               /* 1..4                                                                    */
+    int32_t        num_freqs;          /* a multiple of 8, at most dim / 2                                        */
+    const float   *inv_freq;           /* [num_freqs] fp32, device memory                                         */
+    const uint8_t *axis_of_freq;       /* [num_freqs], HOST memory, read during the call: below axes; NULL: all 0 */
+    int32_t        interleaved, inverse;
+} kda_rotation;
+kda_status kda_rotate(const kda_rotation *rotation, const void *q, const void *k, const int32_t *positions, void *q_out, void *k_out,
+                      void *hip_stream);
+
+/*
+ * Attention of every sequence's drafted tokens over the cache, like kda_cache_attn but for whom a token sees: kv_lens[n] (0 or more; a negative
+ * one skips the sequence, whose rows of o become zeros) counts what the sequence holds without the drafted tokens, whose keys and values
+ * stand at places kv_lens[n] + t.  Token t is at position kv_lens[n] + depth(t), and sees of what is held, of its ancestors and itself
+ * what is at position j with  window == 0  or  its position - j < window  or  j < sinks.  Rows of tokens that are not there are zeros.
+ *   query       tokens 0..64, the rest as for kda_cache_attn; max_kv_len: upper bound of kv_lens[n] + tokens
+ *   parents     [num_seqs,tokens] int32
+ *   workspace   at least kda_cache_tree_attn_workspace_size bytes (0 for some calls), 256-byte aligned
+ * Scales and what is not finite: as for kda_cache_attn.
+ */
+size_t kda_cache_tree_attn_workspace_size(const kda_cache *cache, const kda_cache_query *query);
+kda_status kda_cache_tree_attn(const kda_cache *cache, const kda_cache_query *query, const void *q, const int32_t *parents, void *o,
+                               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * The accepted tokens of a tree become the end of what the sequence holds: the keys and values at places kv_lens[n] + kept[n][i] of the cache move
+ * to kv_lens[n] + i, in all of `layers` caches that lie one behind the other (k, v [layers,num_pages,heads_kv,page_size,dim], k_scale, v_scale
+ * [layers,num_pages,heads_kv]) and share block_table and kv_lens.  kv_lens is not changed: the caller adds to it.
+ *   kept        [num_seqs,max_kept] int32, max_kept up to 64: indices of drafted tokens, increasing.  An entry that is negative or not above the
+ *               one before ends the path.  A sequence with kv_lens[n] < 0 is skipped.
+ * A page and head's scale becomes the largest of those of the tokens that move into it and, where older tokens stand in it, its own; codes
+ * whose scale grows are rounded to it once.  Scales are positive, as kda_cache_append makes them.  What stands behind the kept tokens is left
+ * as it is.  A token without a page, there or where it would go, is dropped.  Pages that are written must belong to one sequence.
+ */
+kda_status kda_cache_keep(const kda_cache *cache, int32_t layers, const int32_t *kept, int32_t max_kept, void *hip_stream);
+
+/*
+ * KDA over a draft tree: token t steps from the state behind its parent, or from the sequence's own, and its output reads the state behind it,
+ *     S_t = (I - beta_t k_t k_t^T) Diag(alpha_t) S_parent(t) + beta_t k_t v_t^T,      o_t = scale * S_t^T q_t.
+ * The states are read once and not changed.  dims as for kda_recurrent_steps_pooled, seqlen 0..64 tokens of every sequence;
+ *   q, k, log_alpha [N,Tq,H,dk]   v [N,Tq,H,dv]   beta [N,Tq,H]   S_pool [P,H,dk,dv] fp32   state_indices [N] int32 or NULL, all as there, but
+ *                  that sequences may read the same state; rows of o of skipped sequences and of tokens that are not there become zeros
+ *   parents        [N,Tq] int32
+ *   o              [N,Tq,H,dv]   out_dtype, either with either in_dtype
+ *   flags          KDA_STEPS_SCALAR_GATE: log_alpha is [N,Tq,H]
+ * All arithmetic is fp32.  No workspace.
+ */
+kda_status kda_tree_steps(const kda_dims *dims, const void *q, const void *k, const void *v, const void *log_alpha, const void *beta,
+                          const float *S_pool, const int32_t *state_indices, const int32_t *parents, void *o, uint32_t flags, void *hip_stream);
+
+/*
+ * Takes the states through the accepted tokens of a tree, in place: sequence n's through tokens kept[n][0], kept[n][1], ... of the k, v,
+ * log_alpha and beta that kda_tree_steps had (dims->seqlen: their tokens a sequence).  kept [N,max_kept] as for kda_cache_keep; an entry of seqlen
+ * or more ends the path too.  A state without an accepted token is not touched.  Two sequences naming the same state race.
+ */
+kda_status kda_tree_commit(const kda_dims *dims, const void *k, const void *v, const void *log_alpha, const void *beta, float *S_pool,
+                           const int32_t *state_indices, const int32_t *kept, int32_t max_kept, uint32_t flags, void *hip_stream);
+
+/*
+ * ---- Pages that several sequences share ----
+ *
+ * block_table as in kda_cache; page_refs [num_pages] int32: how many of its entries name a page.  A page with none is free.
+ * Entries outside [0, num_pages) are no page and not counted.
+ */
+
+/*
+ * Rows of the table become copies of other rows, in place: row n what row source[n] was (source[n] == n or >= num_seqs: it stays), or
+ * empty (-1) where source[n] < 0, which frees what it alone had.  Beams that are carried on, dropped or doubled, prompts that are shared,
+ * and sequences that end.  page_refs follows.  num_seqs at most 8192.
+ */
+kda_status kda_pages_fork(int32_t *block_table, int32_t num_seqs, int32_t max_pages, int32_t *page_refs, int64_t num_pages,
+                          const int32_t *source, void *hip_stream);
+
+/*
+ * Makes every sequence the only owner of the pages that it writes next, when it grows from kv_lens[n] to new_lens[n] tokens (one that does not
+ * grow, or has a negative length, is skipped): entries of the columns kv_lens[n] / page_size up to that of its last token that are no page,
+ * or a page with more than one reference when the call begins, become free pages, the lowest-numbered first, in the order of rows and then
+ * columns; a page that is replaced loses a reference.  Tokens behind the table's columns get no page.
+ *   copies      [num_seqs,2] int32, written: (from, to) for a sequence whose page of column kv_lens[n] / page_size is replaced and holds older
+ *               tokens, for kda_cache_copy_pages; else (-1, -1)
+ *   missing     [1] int32, written: 0, or by how many pages the free ones fall short: then nothing else is changed, and copies are all (-1, -1)
+ * num_seqs at most 8192, num_seqs * max_pages below 2^31.  workspace: kda_pages_reserve_workspace_size bytes, 256-byte aligned.
+ */
+size_t kda_pages_reserve_workspace_size(int32_t num_seqs, int32_t max_pages, int64_t num_pages);
+kda_status kda_pages_reserve(int32_t *block_table, int32_t num_seqs, int32_t max_pages, int32_t page_size, int32_t *page_refs, int64_t num_pages,
+                             const int32_t *kv_lens, const int32_t *new_lens, int32_t *copies, int32_t *missing, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Moves the pages in use to the front of the pool: with U of them, those at U and above take the free places below, the lowest first, in
+ * order.  Table and counts are changed; the pages themselves are the caller's to move:
+ *   moves       [num_pages / 2,2] int32, written: (from, to), and (-1, -1) behind the last
+ * for kda_cache_copy_pages, before anything else writes them.  workspace: 4 * num_pages + 256 bytes, 256-byte aligned.
+ */
+kda_status kda_pages_compact(int32_t *block_table, int32_t num_seqs, int32_t max_pages, int32_t *page_refs, int64_t num_pages, int32_t *moves,
+                             void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Copies pages, codes and scales, in all of `layers` caches that lie one behind the other (as for kda_cache_keep): pairs [num_pairs,2] int32, device
+ * memory, (from, to).  A pair with an entry outside [0, num_pages) is skipped.  No page may be written by two pairs, or written by one and read by
+ * another.  Of `cache`, heads_kv, dim, page_size, num_pages and the four arrays are read.
+ */
+kda_status kda_cache_copy_pages(const kda_cache *cache, int32_t layers, const int32_t *pairs, int64_t num_pairs, void *hip_stream);
+
 /* Static description of a status code (never NULL). */
 const char *kda_status_string(kda_status status);
 

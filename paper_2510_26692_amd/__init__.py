@@ -14,3 +14,5 @@ from .kda import (KdaDims, KdaError, KdaEpilogue, KdaPrologue, kda_chunk_fwd, kd
                   kda_status_string, kda_version, library_path, load_library)
 from .attn import (KdaAttnDims, KdaCache, KdaCacheQuery, KdaRope, kda_cache_append, kda_cache_attn, kda_window_attn_bwd,  # noqa: F401
                    kda_window_attn_bwd_workspace_size, kda_window_attn_fwd)
+from .tree import (KdaRotation, kda_cache_copy_pages, kda_cache_keep, kda_cache_tree_attn, kda_pages_compact, kda_pages_fork,  # noqa: F401
+                   kda_pages_reserve, kda_rotate, kda_tree_commit, kda_tree_steps)

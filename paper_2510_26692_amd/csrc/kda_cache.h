@@ -1,4 +1,4 @@
-// The paged 8-bit cache as its kernels see it (kda_cache_append.hip, kda_cache_attn.hip).
+// The paged 8-bit cache as its kernels see it (kda_cache_append.hip, kda_cache_attn.hip, kda_cache_tree.hip, kda_cache_move.hip).
 #pragma once
 
 #include "kda_common.h"
@@ -42,6 +42,23 @@ struct Attend {
     int64_t q_stride;
     float scale;
     int32_t tokens, window, sinks, rows, row_tiles, splits, out_bf16;
+};
+
+// A call of kda_cache_tree_attn: what kda_cache_attn has, and the trees.
+struct TreeAttend : Attend {
+    const int32_t *parents;          // [N][tokens]
+};
+// A call of kda_cache_copy_pages.
+struct Copies {
+    const int32_t *pairs;
+    int64_t items;                   // pairs x layers x 2 (keys, values) x pieces
+    int64_t page_bytes;              // of a page's codes, all heads
+    int32_t layers, pieces;
+};
+// A call of kda_cache_keep.
+struct Keep {
+    const int32_t *kept;             // [N][most]
+    int32_t most, layers;
 };
 
 // Number of the page that holds logical page p of sequence n, or -1.

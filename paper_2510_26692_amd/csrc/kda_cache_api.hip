@@ -1,10 +1,16 @@
-// C entry points of the paged 8-bit cache: argument checks and what the kernels of kda_cache_append.hip and kda_cache_attn.hip see.
+// C entry points of the paged 8-bit cache: argument checks and what the kernels of kda_cache_append.hip, kda_cache_attn.hip, kda_cache_tree.hip
+// and kda_cache_move.hip see.
 #include "kda_cache.h"
 
 namespace kda {
 
 kda_status cache_append_dispatch(const cache::Cache &, const cache::Append &, int dim, hipStream_t);
 kda_status cache_attn_dispatch(const cache::Cache &, const cache::Attend &, int dim, hipStream_t);
+kda_status cache_tree_dispatch(const cache::Cache &, const cache::TreeAttend &, int dim, hipStream_t);
+int32_t cache_tree_splits(const cache::Cache &, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens);
+int32_t cache_tree_tile_rows(int32_t rows);
+kda_status cache_copy_dispatch(const cache::Cache &, cache::Copies, hipStream_t);
+kda_status cache_keep_dispatch(const cache::Cache &, const cache::Keep &, int dim, hipStream_t);
 int32_t cache_attn_splits(const cache::Cache &, int64_t pairs, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens);
 
 namespace {
@@ -60,14 +66,15 @@ kda_status check(const kda_cache *d, bool buffers, cache::Cache &c)
     return KDA_OK;
 }
 
-kda_status check(const kda_cache *d, bool buffers, const kda_cache_query *q, cache::Cache &c, cache::Attend &a)
+// `tree`: of kda_cache_tree_attn
+kda_status check(const kda_cache *d, bool buffers, const kda_cache_query *q, bool tree, cache::Cache &c, cache::Attend &a)
 {
     if (const kda_status st = check(d, buffers, c); st != KDA_OK) return st;
     if (!q) return fail(KDA_ERR_INVALID_ARG, "query is NULL");
     if (q->tokens < 0 || q->window < 0 || q->sinks < 0 || q->max_kv_len < 0)
         return fail(KDA_ERR_INVALID_ARG, "negative size (tokens %d, window %lld, sinks %d, max_kv_len %lld)", q->tokens, (long long)q->window, q->sinks,
                     (long long)q->max_kv_len);
-    if (q->tokens > 8) return fail(KDA_ERR_UNSUPPORTED, "at most 8 new tokens a sequence, got %d", q->tokens);
+    if (q->tokens > (tree ? 64 : 8)) return fail(KDA_ERR_UNSUPPORTED, "at most %d new tokens a sequence, got %d", tree ? 64 : 8, q->tokens);
     if (q->sinks > 64) return fail(KDA_ERR_UNSUPPORTED, "at most 64 sinks, got %d", q->sinks);
     if (!(q->scale >= 1e-30f && q->scale <= 1e30f)) return fail(KDA_ERR_INVALID_ARG, "scale must be positive, in [1e-30, 1e30]");
     if (q->out_dtype != KDA_F32 && q->out_dtype != KDA_BF16) return fail(KDA_ERR_INVALID_ARG, "out_dtype %d is not a kda_dtype", (int)q->out_dtype);
@@ -80,10 +87,11 @@ kda_status check(const kda_cache *d, bool buffers, const kda_cache_query *q, cac
     a.out_bf16 = q->out_dtype == KDA_BF16;
     if (const kda_status st = stride_of(q->q_stride, (int64_t)d->heads_q * d->dim, "q", a.q_stride); st != KDA_OK) return st;
     a.rows = q->tokens * c.group;
-    a.row_tiles = (a.rows + 31) / 32;
+    const int32_t tile = tree ? cache_tree_tile_rows(a.rows) : 32;
+    a.row_tiles = (a.rows + tile - 1) / tile;
     const int64_t pairs = (int64_t)c.num_seqs * c.heads_kv, held = (int64_t)d->max_pages * d->page_size;
     const int64_t most = q->max_kv_len && q->max_kv_len < held ? q->max_kv_len : held;
-    a.splits = pairs && a.rows ? cache_attn_splits(c, pairs * a.row_tiles, most, a.window, a.sinks, a.tokens) : 1;
+    a.splits = !pairs || !a.rows ? 1 : (tree ? cache_tree_splits : cache_attn_splits)(c, pairs * a.row_tiles, most, a.window, a.sinks, a.tokens);
     // (a launch has fewer than 2^32 threads: 256 a workgroup, and 64 a row of the join)
     if (pairs * a.row_tiles * a.splits > 0xffffff || pairs * a.rows > 0x3ffffff) return fail(KDA_ERR_UNSUPPORTED, "more than 2^24 workgroups");
     return KDA_OK;
@@ -152,7 +160,7 @@ extern "C" size_t kda_cache_attn_workspace_size(const kda_cache *cache, const kd
 {
     cache::Cache c;
     cache::Attend a;
-    if (check(cache, false, query, c, a) != KDA_OK || a.splits <= 1) return 0;
+    if (check(cache, false, query, false, c, a) != KDA_OK || a.splits <= 1) return 0;
     return stats_offset(c, a, cache->dim) + up256((size_t)c.num_seqs * c.heads_kv * a.splits * a.rows * 2 * 4);
 }
 
@@ -161,7 +169,7 @@ extern "C" kda_status kda_cache_attn(const kda_cache *cache, const kda_cache_que
 {
     cache::Cache c;
     cache::Attend a;
-    if (const kda_status st = check(cache, true, query, c, a); st != KDA_OK) return st;
+    if (const kda_status st = check(cache, true, query, false, c, a); st != KDA_OK) return st;
     if (c.num_seqs == 0 || a.rows == 0) return KDA_OK;
     if (!q || !o || !aligned(q, 16) || !aligned(o, 16)) return fail(KDA_ERR_INVALID_ARG, "q or o is NULL or not 16-byte aligned");
     if (a.splits > 1) {
@@ -174,4 +182,78 @@ extern "C" kda_status kda_cache_attn(const kda_cache *cache, const kda_cache_que
     a.q = static_cast<const uint16_t *>(q);
     a.o = o;
     return cache_attn_dispatch(c, a, cache->dim, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" size_t kda_cache_tree_attn_workspace_size(const kda_cache *cache, const kda_cache_query *query)
+{
+    cache::Cache c;
+    cache::Attend a;
+    if (check(cache, false, query, true, c, a) != KDA_OK || a.splits <= 1) return 0;
+    return stats_offset(c, a, cache->dim) + up256((size_t)c.num_seqs * c.heads_kv * a.splits * a.rows * 2 * 4);
+}
+
+extern "C" kda_status kda_cache_tree_attn(const kda_cache *cache, const kda_cache_query *query, const void *q, const int32_t *parents, void *o,
+                                          void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    cache::Cache c;
+    cache::TreeAttend a = {};
+    if (const kda_status st = check(cache, true, query, true, c, a); st != KDA_OK) return st;
+    if (c.num_seqs == 0 || a.rows == 0) return KDA_OK;
+    if (!q || !o || !aligned(q, 16) || !aligned(o, 16)) return fail(KDA_ERR_INVALID_ARG, "q or o is NULL or not 16-byte aligned");
+    if (!parents || !aligned(parents, 4)) return fail(KDA_ERR_INVALID_ARG, "parents is NULL or misaligned");
+    if (a.splits > 1) {
+        const size_t need = kda_cache_tree_attn_workspace_size(cache, query);
+        if (!workspace || !aligned(workspace, 256) || workspace_bytes < need)
+            return fail(KDA_ERR_WORKSPACE, "kda_cache_tree_attn: workspace must be 256-byte aligned and hold %zu bytes, got %zu", need, workspace_bytes);
+        a.part = static_cast<float *>(workspace);
+        a.stats = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + stats_offset(c, a, cache->dim));
+    }
+    a.q = static_cast<const uint16_t *>(q);
+    a.o = o;
+    a.parents = parents;
+    return cache_tree_dispatch(c, a, cache->dim, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" kda_status kda_cache_keep(const kda_cache *cache, int32_t layers, const int32_t *kept, int32_t max_kept, void *hip_stream)
+{
+    cache::Cache c;
+    if (const kda_status st = check(cache, true, c); st != KDA_OK) return st;
+    if (layers < 0 || max_kept < 0) return fail(KDA_ERR_INVALID_ARG, "negative size (layers %d, max_kept %d)", layers, max_kept);
+    if (max_kept > 64) return fail(KDA_ERR_UNSUPPORTED, "at most 64 kept tokens a sequence, got %d", max_kept);
+    if (c.num_seqs == 0 || c.heads_q == 0 || layers == 0 || max_kept == 0 || c.num_pages == 0) return KDA_OK;
+    if (!kept || !aligned(kept, 4)) return fail(KDA_ERR_INVALID_ARG, "kept is NULL or misaligned");
+    // (a launch has fewer than 2^32 threads)
+    if ((int64_t)c.num_seqs * c.heads_kv > 0x7fffff / layers) return fail(KDA_ERR_UNSUPPORTED, "more than 2^23 sequences, layers and heads");
+    cache::Keep a = {};
+    a.kept = kept;
+    a.most = max_kept;
+    a.layers = layers;
+    return cache_keep_dispatch(c, a, cache->dim, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" kda_status kda_cache_copy_pages(const kda_cache *cache, int32_t layers, const int32_t *pairs, int64_t num_pairs, void *hip_stream)
+{
+    cache::Cache c;
+    if (!cache) return fail(KDA_ERR_INVALID_ARG, "cache is NULL");
+    // (a copy knows no sequences and no query heads)
+    kda_cache d = *cache;
+    d.num_seqs = d.max_pages = 0;
+    d.heads_q = d.heads_kv;
+    if (const kda_status st = check(&d, false, c); st != KDA_OK) return st;
+    if (layers < 0 || num_pairs < 0) return fail(KDA_ERR_INVALID_ARG, "negative size (layers %d, num_pairs %lld)", layers, (long long)num_pairs);
+    if (layers == 0 || num_pairs == 0 || c.heads_kv == 0 || c.num_pages == 0) return KDA_OK;
+    if (num_pairs > 0x7fffffffLL || layers > 65535) return fail(KDA_ERR_UNSUPPORTED, "more than 2^31 pairs or 65535 layers");
+    if (!pairs || !d.k || !d.v || !d.k_scale || !d.v_scale) return fail(KDA_ERR_INVALID_ARG, "pairs or a buffer of the cache is NULL");
+    if (!aligned(pairs, 4) || !aligned(d.k, 16) || !aligned(d.v, 16) || !aligned(d.k_scale, 4) || !aligned(d.v_scale, 4))
+        return fail(KDA_ERR_INVALID_ARG, "pairs or a buffer of the cache is misaligned");
+    c.k = static_cast<uint8_t *>(d.k);
+    c.v = static_cast<uint8_t *>(d.v);
+    c.k_scale = d.k_scale;
+    c.v_scale = d.v_scale;
+    cache::Copies a = {};
+    a.pairs = pairs;
+    a.items = num_pairs * layers * 2;
+    a.page_bytes = (int64_t)c.heads_kv * c.page_size * d.dim;
+    a.layers = layers;
+    return cache_copy_dispatch(c, a, static_cast<hipStream_t>(hip_stream));
 }

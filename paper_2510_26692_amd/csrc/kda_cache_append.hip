@@ -12,6 +12,7 @@
 // A workgroup has one page of one sequence and head, keys or values: rows of 8-channel pieces in registers, one pass for the largest
 // value, one for the codes.  Further workgroups turn the queries, a token's angles once for several heads.
 #include "kda_cache.h"
+#include "kda_rotation.h"
 
 namespace kda {
 namespace cache {
@@ -50,12 +51,6 @@ struct Piece {
         for (int e = 0; e < 4; ++e) f[e] = wanted ? frequency(a, second ? 4 + e : e) : 0.0;
     }
 };
-// revolutions at a position, less the nearest whole number: exact to 2^-20 of a revolution at 2^31
-__device__ __forceinline__ double turns(double frequency, int64_t pos)
-{
-    const double t = (double)pos * frequency;
-    return t - __builtin_rint(t);
-}
 // cos and sin of 2 pi r, |r| <= 1/2: Taylor's series about the nearest quarter, to x^14 and x^13 (2^-46 at pi / 4: one code in 2^40 would differ).
 struct Angle { double c, s; };
 __device__ __forceinline__ Angle angle64(double r)

@@ -1,0 +1,398 @@
+// Attention of a draft tree's tokens over the paged cache of e4m3 codes.
+//
+// Rows are (drafted token, query head of the group), 64 or 128 of a key head to a workgroup.  Its four waves bring 64 keys and values
+// at a time into LDS, widened to bf16 (exact) on the way, and walk them as the prefill does:
+//
+//     X^T [key, row] = K Q^T,   P^T = 2^(c X^T - m),   O^T [channel, row] += V^T P^T          (32x32x16 bf16 products, statistics in fp32)
+//
+// with a page's scales on the logits and numerators of its keys, so that they may be any numbers, and 64 more to the maximum for values with a scale of
+// 2^64 or more (kda_cache_attn.hip).  With 128 rows a wave has 32 of them and all keys of a tile, with 64 half of the keys, and two
+// waves' parts meet at the end.  The next tile's codes are on their way into registers while one is worked on, and their pages' numbers a tile
+// ahead of that.
+//
+// A row's token sees what is held (by the window and sinks of its position, len + depth) and its line, a bit for each drafted token; both
+// become one word of bits a tile, made only for tiles that some row sees in part.
+#include <atomic>
+
+#include "kda_attn_tile.h"
+#include "kda_cache.h"
+#include "kda_cache_join.h"
+#include "kda_tree.h"
+
+namespace kda {
+namespace cache {
+
+using attn::bf16x8;
+using attn::f32x16;
+using attn::TileReader;
+using attn::u32x2;
+using attn::u32x4;
+constexpr int kKeys = 64;            // of a tile
+
+// The visible keys of a sequence's tree as tiles: those of the sinks where the window begins behind them, then the window's and the tree's.
+struct Tiles {
+    int32_t held, len, low, sink_tiles, count;
+};
+__device__ __forceinline__ Tiles tiles_of(const Cache &c, const TreeAttend &a, int n)
+{
+    const int32_t most = c.max_pages << c.page_log2, l = c.lens[n];
+    Tiles t = {min(l, 1 << 30), 0, 0, 0, 0};                 // (no table has more)
+    if (l < 0) return t;
+    t.len = t.held < most - a.tokens ? t.held + a.tokens : most;
+    // a token of depth 0 is at position l, and its window begins at l - window + 1
+    t.low = a.window && t.held >= a.window ? (t.held - a.window + 1) / kKeys : 0;
+    const int32_t high = (t.len + kKeys - 1) / kKeys;
+    t.low = min(t.low, high);
+    t.sink_tiles = min(t.low, (a.sinks + kKeys - 1) / kKeys);
+    t.count = high - t.low + t.sink_tiles;
+    return t;
+}
+__device__ __forceinline__ int32_t part_tiles(const Tiles &t, int splits) { return (t.count + splits - 1) / splits; }
+__device__ __forceinline__ int32_t used_parts(const Cache &c, const TreeAttend &a, int n)
+{
+    const Tiles t = tiles_of(c, a, n);
+    const int32_t per = part_tiles(t, a.splits);
+    return per ? (t.count + per - 1) / per : 0;
+}
+
+// sixteen codes as two pieces of eight bf16
+__device__ __forceinline__ void widen16(const u32x4 &w, u32x4 (&o)[2])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        o[i / 2][2 * (i % 2)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, false));
+        o[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, true));
+    }
+}
+__device__ __forceinline__ bool has_nan(const u32x4 &w)
+{
+    uint32_t r = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r |= ((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    return r != 0;
+}
+
+// LDS: K and V of one tile, then of another; then what the waves share
+template <int D> struct Lds {
+    static constexpr int kT = kKeys * D * 2;
+    static constexpr int kScales = 4 * kT;                   // [2][8] fp32: of the tile's four 16-key blocks, keys and values
+    static constexpr int kHave = kScales + 64;               // [2][4] words: the block has a page
+    static constexpr int kOdd = kHave + 32;                  // [2][4] words: of the waves, some code of a value is no number
+    static constexpr int kLine = kOdd + 32;                  // [64] of 64 bits
+    static constexpr int kBytes = kLine + 512;
+};
+
+template <int D, int WR>
+__global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, const TreeAttend a)
+{
+    constexpr int WK = 4 / WR, KB = 2 / WK;                  // waves along the keys; 32-key blocks of a wave
+    constexpr int kT = Lds<D>::kT, kChunks = D / 16, kPieces = kKeys * kChunks / 256;     // 16-code pieces of a key; of a thread, keys or values
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), x = lane & 31, h = lane >> 5;
+    const int wr = wave % WR, wk = wave / WR;
+    uint32_t id = blockIdx.x;
+    const int kv = id % c.heads_kv;
+    id /= c.heads_kv;
+    const int tile = id % a.row_tiles;
+    id /= a.row_tiles;
+    const int split = id % a.splits, n = id / a.splits;
+    const Tiles t = tiles_of(c, a, n);
+    const int32_t per = part_tiles(t, a.splits), begin = min(split * per, t.count), end = min(begin + per, t.count);
+    if (a.splits > 1 && begin >= end) return;                // (the join knows)
+
+    // ---- the trees' lines, and what the window leaves of them ----
+    uint64_t *lines = reinterpret_cast<uint64_t *>(lds + Lds<D>::kLine);
+    if (wave == 0) lines[lane] = tree_line(a.parents + (int64_t)n * a.tokens, a.tokens);
+    __syncthreads();
+    const int row0 = (tile * WR + wr) * 32, row = row0 + x;
+    const bool working = row0 < a.rows;
+    const int rr = min(row, a.rows - 1), tok = rr / c.group, head = kv * c.group + rr - tok * c.group;
+    uint64_t line = lines[tok];
+    const bool there = line != 0;
+    const int32_t depth = __popcll(line) - 1, pos = t.held + depth;
+    if (a.window && a.window < kTreeTokens)
+        for (int j = 0; j < a.tokens; ++j) {
+            const int32_t dj = __popcll(lines[j]) - 1;
+            if (depth - dj >= a.window && t.held + dj >= a.sinks) line &= ~(1ull << j);
+        }
+
+    // ---- the loader: a thread has 16 codes of kPieces keys ----
+    const int key_of = tid / kChunks, chunk = tid % kChunks;
+    auto first_key = [&](int32_t u) { return (u < t.sink_tiles ? u : t.low + u - t.sink_tiles) * kKeys; };
+    // the page of the 16 keys from `key` on, or -1: none, or one that no row sees (which may be another sequence's by now)
+    auto page_of = [&](int32_t key) -> int32_t {
+        const bool hidden = a.window && t.held - key - 15 >= a.window && key >= a.sinks;
+        return key < t.len && !hidden ? page_at(c, n, key >> c.page_log2) : -1;
+    };
+    int32_t pages[kPieces], scale_page = -1;
+    auto look_up = [&](int32_t u) {
+        const int32_t k0 = first_key(u);
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) pages[j] = page_of((k0 + key_of + j * (kKeys / kPieces)) & ~15);
+        if (tid < 8) scale_page = page_of(k0 + 16 * (tid & 3));
+    };
+    u32x4 kc[kPieces], vc[kPieces];
+    float scale = 0.f;
+    bool have = false;
+    auto fetch = [&](int32_t u) {
+        const int32_t k0 = first_key(u);
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            const int32_t key = k0 + key_of + j * (kKeys / kPieces);
+            kc[j] = vc[j] = u32x4{0, 0, 0, 0};
+            if (pages[j] >= 0 && key < t.len) {
+                const int64_t at = (((int64_t)pages[j] * c.heads_kv + kv) * c.page_size + (key & (c.page_size - 1))) * D + 16 * chunk;
+                kc[j] = *reinterpret_cast<const u32x4 *>(c.k + at);
+                vc[j] = *reinterpret_cast<const u32x4 *>(c.v + at);
+            }
+        }
+        if (tid < 8) {
+            have = scale_page >= 0;
+            scale = have ? (tid < 4 ? c.k_scale : c.v_scale)[(int64_t)scale_page * c.heads_kv + kv] : 0.f;
+        }
+    };
+    auto leave = [&](int buf) {
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            const int r = key_of + j * (kKeys / kPieces);
+            u32x4 o[2];
+            widen16(kc[j], o);
+            uint8_t *to = lds + 2 * buf * kT + r * 2 * D;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) *reinterpret_cast<u32x4 *>(to + 16 * ((2 * chunk + e) ^ attn::swizzle<D>(r))) = o[e];
+            odd |= has_nan(vc[j]);
+            widen16(vc[j], o);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) *reinterpret_cast<u32x4 *>(to + kT + 16 * ((2 * chunk + e) ^ attn::swizzle<D>(r))) = o[e];
+        }
+        if (tid < 8) reinterpret_cast<float *>(lds + Lds<D>::kScales)[8 * buf + tid] = scale;
+        if (tid < 4) reinterpret_cast<uint32_t *>(lds + Lds<D>::kHave)[4 * buf + tid] = have;
+        const uint32_t any = __any(odd);
+        if (lane == 0) reinterpret_cast<uint32_t *>(lds + Lds<D>::kOdd)[4 * buf + wave] = any;
+    };
+
+    // ---- the rows ----
+    TileReader<D> rd;
+    rd.init(lane);
+    bf16x8 qf[D / 16];
+    {
+        const uint16_t *from = a.q + ((int64_t)n * a.tokens + tok) * a.q_stride + (int64_t)head * D + 8 * h;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(from + 16 * i));
+    }
+    const float cs = a.scale * kLog2e;
+    f32x16 acc[D / 32];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) acc[db] = attn::zeros16();
+    float m = -kInf, mref = 0.f, l = 0.f;
+
+    auto work = [&](int32_t u, int buf) {
+        const int32_t k0 = first_key(u);
+        const uint32_t kt = 2 * buf * kT, vt = kt + kT;
+        f32x16 st[KB];
+#pragma unroll
+        for (int b = 0; b < KB; ++b) st[b] = attn::zeros16();
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int b = 0; b < KB; ++b) st[b] = attn::mfma(rd.rows(kt, KB * wk + b, i), qf[i], st[b]);
+        const f32x4 *sc = reinterpret_cast<const f32x4 *>(lds + Lds<D>::kScales) + 2 * buf;
+        const f32x4 ks = sc[0], vs = sc[1];
+        const u32x4 hv = *reinterpret_cast<const u32x4 *>(lds + Lds<D>::kHave + 16 * buf);
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) st[b][j] *= cs * ks[2 * (KB * wk + b) + j / 8];
+        // some row does not see some key
+        const bool whole = hv[0] & hv[1] & hv[2] & hv[3];
+        const bool edge = __builtin_amdgcn_readfirstlane(!whole || k0 + kKeys - 1 >= t.held || (a.window && t.held + a.tokens - 1 - k0 >= a.window));
+        uint32_t seen[KB];
+        if (edge) {
+            const int32_t node = t.held - k0;                // the row of the first drafted token
+            const attn::Seen ctx = attn::seen_rows(a.window ? attn::clamp_tile(pos - a.window + 1 - k0) : 0, attn::clamp_tile(node - 1));
+            const attn::Seen sinks = attn::seen_rows(0, attn::clamp_tile(min(a.sinks, t.held) - 1 - k0));
+            uint64_t w = ((uint64_t)(ctx.w[1] | sinks.w[1]) << 32) | (ctx.w[0] | sinks.w[0]);
+            w |= node >= 64 || node <= -64 ? 0ull : node >= 0 ? line << node : line >> -node;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) w &= hv[b] ? ~0ull : ~(0xffffull << (16 * b));
+            w = there ? w : 0ull;
+#pragma unroll
+            for (int b = 0; b < KB; ++b) {
+                seen[b] = (uint32_t)(w >> (32 * (KB * wk + b))) >> (4 * h);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) st[b][j] = attn::where_seen(attn::seen_bit(seen[b], j), st[b][j], -kInf);
+            }
+        }
+        bool large = false;
+#pragma unroll
+        for (int b = 0; b < 2 * KB; ++b) large |= (__float_as_uint(vs[2 * KB * wk + b]) & 0x7fffffffu) >= kLargeScale;
+        float top = st[0][0];
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, st[b][j]);
+        top = fmaxf(top, attn::other_half(top)) + (large ? kLift : 0.f);
+        if (__any(top > m + 8.f)) {
+            const float mn = fmaxf(m, top), f = mn == -kInf ? 1.f : fast_exp2(m - mn);
+            m = mn;
+            mref = mn == -kInf ? 0.f : mn;
+            l *= f;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[db][j] *= f;
+        }
+        bf16x8 p[2 * KB];
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            float e[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                e[j] = fast_exp2(st[b][j] - mref);
+                l += e[j];
+                e[j] *= vs[2 * (KB * wk + b) + j / 8];
+            }
+            p[2 * b] = attn::pack8(e);
+            p[2 * b + 1] = attn::pack8(e + 8);
+        }
+        const u32x4 od = *reinterpret_cast<const u32x4 *>(lds + Lds<D>::kOdd + 16 * buf);
+        if (edge && __builtin_amdgcn_readfirstlane(od[0] | od[1] | od[2] | od[3])) {
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) attn::careful_product<D, 2 * KB>(acc[db], rd, vt, db, 2 * KB * wk, p, seen);
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2 * KB; ++s)
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db) acc[db] = attn::mfma(rd.transposed(vt, db, 2 * KB * wk + s), p[s], acc[db]);
+        }
+    };
+
+    if (begin < end) {
+        look_up(begin);
+        fetch(begin);
+        if (begin + 1 < end) look_up(begin + 1);
+        for (int32_t u = begin; u < end; ++u) {
+            const int buf = (u - begin) & 1;
+            leave(buf);
+            if (u + 1 < end) {
+                fetch(u + 1);
+                if (u + 2 < end) look_up(u + 2);
+            }
+            __syncthreads();
+            if (working) work(u, buf);
+        }
+    }
+    l += attn::other_half(l);
+
+    // ---- two waves' parts of the same rows ----
+    if constexpr (WK == 2) {
+        __syncthreads();
+        f32x4 *at = reinterpret_cast<f32x4 *>(lds) + wr * (D / 32 * 4) * 64 + lane;
+        float *stats = reinterpret_cast<float *>(lds + WR * (D / 32 * 4) * 64 * 16) + (wr * 64 + lane) * 2;
+        if (wk == 1) {
+#pragma unroll
+            for (int i = 0; i < D / 32 * 4; ++i) at[64 * i] = f32x4{acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2], acc[i / 4][4 * (i % 4) + 3]};
+            stats[0] = m;
+            stats[1] = l;
+        }
+        __syncthreads();
+        if (wk == 1) return;
+        const float mo = stats[0], lo = stats[1], mn = fmaxf(m, mo);
+        // (a part that saw nothing adds nothing; one that is NaN stays so)
+        const float f0 = m == -kInf ? 0.f : fast_exp2(m - mn), f1 = mo == -kInf ? 0.f : fast_exp2(mo - mn);
+        l = l * f0 + lo * f1;
+#pragma unroll
+        for (int i = 0; i < D / 32 * 4; ++i) {
+            const f32x4 y = at[64 * i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i / 4][4 * (i % 4) + e] = acc[i / 4][4 * (i % 4) + e] * f0 + y[e] * f1;
+        }
+        m = mn;
+    }
+    if (row >= a.rows) return;
+    if (!there || t.held < 0) {                              // (whatever tiles that every row sees whole have left)
+        m = -kInf;
+        l = 0.f;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) acc[db] = attn::zeros16();
+    }
+    if (a.splits > 1) {
+        const int64_t part = (((int64_t)n * c.heads_kv + kv) * a.splits + split) * a.rows + row;
+        float *to = a.part + part * D + 4 * h;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) *reinterpret_cast<f32x4 *>(to + 32 * db + 8 * b) = f32x4{acc[db][4 * b], acc[db][4 * b + 1], acc[db][4 * b + 2], acc[db][4 * b + 3]};
+        if (h == 0) {
+            a.stats[part * 2] = m;
+            a.stats[part * 2 + 1] = l;
+        }
+        return;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t out = (((int64_t)n * a.tokens + tok) * c.heads_q + head) * D + 4 * h;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const f32x4 y = f32x4{acc[db][4 * b], acc[db][4 * b + 1], acc[db][4 * b + 2], acc[db][4 * b + 3]} * inv;
+            const int64_t w = out + 32 * db + 8 * b;
+            if (a.out_bf16) *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.o) + w) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+            else *reinterpret_cast<f32x4 *>(static_cast<float *>(a.o) + w) = y;
+        }
+}
+
+}  // namespace cache
+}  // namespace kda
+
+using namespace kda;
+using namespace kda::cache;
+
+namespace kda {
+
+int32_t cache_tree_tile_rows(int32_t rows) { return rows <= 64 ? 64 : 128; }
+
+// Workgroups of a tile of rows: enough for two on every compute unit, each with two tiles of keys at least.
+int32_t cache_tree_splits(const Cache &, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
+{
+    int64_t keys = most_keys;
+    if (window && window + tokens + sinks + 2 * kKeys < keys) keys = window + tokens + sinks + 2 * kKeys;
+    const int64_t steps = (keys + kKeys - 1) / kKeys, most = (steps + 1) / 2, want = (512 + tiles - 1) / (tiles > 0 ? tiles : 1);
+    const int64_t n = want < most ? want : most;
+    return (int32_t)(n < 1 ? 1 : n);
+}
+
+namespace {
+template <int D, int WR> hipError_t launch(const Cache &c, const TreeAttend &a, hipStream_t st)
+{
+    const uint32_t grid = (uint32_t)c.num_seqs * c.heads_kv * a.row_tiles * a.splits;
+    static std::atomic<bool> raised[64];                                  // per device: a workgroup's LDS passes the runtime's default
+    if (Lds<D>::kBytes > 65536) {
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        if (dev < 0 || dev >= 64 || !raised[dev]) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kda_cache_tree_kernel<D, WR>), hipFuncAttributeMaxDynamicSharedMemorySize, Lds<D>::kBytes);
+            if (e != hipSuccess) return e;
+            if (dev >= 0 && dev < 64) raised[dev] = true;
+        }
+    }
+    hipLaunchKernelGGL((kda_cache_tree_kernel<D, WR>), dim3(grid), dim3(256), Lds<D>::kBytes, st, c, a);
+    return hipGetLastError();
+}
+template <int D> hipError_t launch(const Cache &c, const TreeAttend &a, hipStream_t st)
+{
+    hipError_t e = cache_tree_tile_rows(a.rows) == 64 ? launch<D, 2>(c, a, st) : launch<D, 4>(c, a, st);
+    if (e == hipSuccess && a.splits > 1) e = launch_join<D>(c, a, (int64_t)c.num_seqs * c.heads_kv * a.rows, st);
+    return e;
+}
+}  // namespace
+
+kda_status cache_tree_dispatch(const Cache &c, const TreeAttend &a, int dim, hipStream_t st)
+{
+    const hipError_t e = dim == 128 ? launch<128>(c, a, st) : launch<64>(c, a, st);
+    return e == hipSuccess ? KDA_OK : fail(KDA_ERR_LAUNCH, "kda_cache_tree_attn: %s", hipGetErrorString(e));
+}
+
+}  // namespace kda

@@ -137,6 +137,29 @@ def load_library():
     lib.kda_cache_attn_workspace_size.argtypes = [vp, vp]
     lib.kda_cache_attn.restype = ctypes.c_int
     lib.kda_cache_attn.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+    i32, u32 = ctypes.c_int32, ctypes.c_uint32
+    lib.kda_rotate.restype = ctypes.c_int
+    lib.kda_rotate.argtypes = [vp] * 7
+    lib.kda_cache_tree_attn_workspace_size.restype = sz
+    lib.kda_cache_tree_attn_workspace_size.argtypes = [vp, vp]
+    lib.kda_cache_tree_attn.restype = ctypes.c_int
+    lib.kda_cache_tree_attn.argtypes = [vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.kda_cache_keep.restype = ctypes.c_int
+    lib.kda_cache_keep.argtypes = [vp, i32, vp, i32, vp]
+    lib.kda_tree_steps.restype = ctypes.c_int
+    lib.kda_tree_steps.argtypes = [dp] + [vp] * 9 + [u32, vp]
+    lib.kda_tree_commit.restype = ctypes.c_int
+    lib.kda_tree_commit.argtypes = [dp] + [vp] * 7 + [i32, u32, vp]
+    lib.kda_pages_fork.restype = ctypes.c_int
+    lib.kda_pages_fork.argtypes = [vp, i32, i32, vp, i64, vp, vp]
+    lib.kda_pages_reserve_workspace_size.restype = sz
+    lib.kda_pages_reserve_workspace_size.argtypes = [i32, i32, i64]
+    lib.kda_pages_reserve.restype = ctypes.c_int
+    lib.kda_pages_reserve.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+    lib.kda_pages_compact.restype = ctypes.c_int
+    lib.kda_pages_compact.argtypes = [vp, i32, i32, vp, i64, vp, vp, sz, vp]
+    lib.kda_cache_copy_pages.restype = ctypes.c_int
+    lib.kda_cache_copy_pages.argtypes = [vp, i32, vp, i64, vp]
     try:
         from . import _kda_host
         _kda_host.bind(*[ctypes.cast(f, vp).value for f in (lib.kda_recurrent_step, lib.kda_recurrent_steps)], _raw_stream)
