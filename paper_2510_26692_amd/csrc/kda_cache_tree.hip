@@ -5,14 +5,15 @@
 //
 //     X^T [key, row] = K Q^T,   P^T = 2^(c X^T - m),   O^T [channel, row] += V^T P^T          (32x32x16 bf16 products, statistics in fp32)
 //
-// with a page's scales on the logits and numerators of its keys, so that they may be any numbers, and 64 more to the maximum for values with a scale of
-// 2^64 or more (kda_cache_attn.hip).  With 128 rows a wave has 32 of them and all keys of a tile, with 64 half of the keys, and two
+// A page's scales are taken by its codes on their way to bf16, which is exact for the powers of two that the append makes; any others are on the logits and
+// numerators of its keys, in fp32, with 64 more to the maximum for values with a scale of 2^64 or more (kda_cache_attn.hip).  With 128 rows a wave has 32 of them and all keys of a tile, with 64 half of the keys, and two
 // waves' parts meet at the end.  The next tile's codes are on their way into registers while one is worked on, and their pages' numbers a tile
 // ahead of that.
 //
 // A row's token sees what is held (by the window and sinks of its position, len + depth) and its line, a bit for each drafted token; both
 // become one word of bits a tile, made only for tiles that some row sees in part.
 #include <atomic>
+#include <type_traits>
 
 #include "kda_attn_tile.h"
 #include "kda_cache.h"
@@ -28,6 +29,7 @@ using attn::TileReader;
 using attn::u32x2;
 using attn::u32x4;
 constexpr int kKeys = 64;            // of a tile
+constexpr int kLead = 4;             // operands read ahead of the products that take them
 
 // The visible keys of a sequence's tree as tiles: those of the sinks where the window begins behind them, then the window's and the tree's.
 struct Tiles {
@@ -55,41 +57,41 @@ __device__ __forceinline__ int32_t used_parts(const Cache &c, const TreeAttend &
     return per ? (t.count + per - 1) / per : 0;
 }
 
-// sixteen codes as two pieces of eight bf16
-__device__ __forceinline__ void widen16(const u32x4 &w, u32x4 (&o)[2])
+// sixteen codes, times a power of two, as two pieces of eight bf16 (exact)
+__device__ __forceinline__ void widen16(const u32x4 &w, float scale, u32x4 (&o)[2])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        o[i / 2][2 * (i % 2)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, false));
-        o[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, true));
+        o[i / 2][2 * (i % 2)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, false));
+        o[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true));
     }
 }
-__device__ __forceinline__ bool has_nan(const u32x4 &w)
+// A scale that the codes can take on their way to bf16: a power of two, neither large nor small.  (The append makes no others but for values next to
+// the ends of fp32's range.)
+__device__ __forceinline__ bool is_plain(float scale)
 {
-    uint32_t r = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r |= ((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-    return r != 0;
+    const uint32_t b = __float_as_uint(scale);
+    return (b & 0x807fffffu) == 0 && b - (67u << 23) <= 120u << 23;
 }
 
 // LDS: K and V of one tile, then of another; then what the waves share
 template <int D> struct Lds {
     static constexpr int kT = kKeys * D * 2;
-    static constexpr int kScales = 4 * kT;                   // [2][8] fp32: of the tile's four 16-key blocks, keys and values
-    static constexpr int kHave = kScales + 64;               // [2][4] words: the block has a page
-    static constexpr int kOdd = kHave + 32;                  // [2][4] words: of the waves, some code of a value is no number
-    static constexpr int kLine = kOdd + 32;                  // [64] of 64 bits
+    static constexpr int kScales = 4 * kT;                   // [2][8] fp32: of the tile's four 16-key blocks, keys and values, what the codes have not taken
+    static constexpr int kHave = kScales + 64;               // [2][4] words: the block has a page (1), its codes have taken its scales (2)
+    static constexpr int kLine = kHave + 32;                 // [64] of 64 bits
     static constexpr int kBytes = kLine + 512;
 };
 
-template <int D, int WR>
-__global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, const TreeAttend a)
+// A tile of rows over a split's keys.  Returns true where the walk has to be repeated with care: a value that is not finite stood where some row does
+// not see it.
+template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_tile(const Cache &c, const TreeAttend &a)
 {
     constexpr int WK = 4 / WR, KB = 2 / WK;                  // waves along the keys; 32-key blocks of a wave
     constexpr int kT = Lds<D>::kT, kChunks = D / 16, kPieces = kKeys * kChunks / 256;     // 16-code pieces of a key; of a thread, keys or values
     extern __shared__ __align__(16) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), x = lane & 31, h = lane >> 5;
-    const int wr = wave % WR, wk = wave / WR;
+    const int wr = wave % WR, wk = WK == 1 ? 0 : wave / WR;
     uint32_t id = blockIdx.x;
     const int kv = id % c.heads_kv;
     id /= c.heads_kv;
@@ -98,7 +100,7 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
     const int split = id % a.splits, n = id / a.splits;
     const Tiles t = tiles_of(c, a, n);
     const int32_t per = part_tiles(t, a.splits), begin = min(split * per, t.count), end = min(begin + per, t.count);
-    if (a.splits > 1 && begin >= end) return;                // (the join knows)
+    if (a.splits > 1 && begin >= end) return false;          // (the join knows)
 
     // ---- the trees' lines, and what the window leaves of them ----
     uint64_t *lines = reinterpret_cast<uint64_t *>(lds + Lds<D>::kLine);
@@ -116,60 +118,69 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
             if (depth - dj >= a.window && t.held + dj >= a.sinks) line &= ~(1ull << j);
         }
 
-    // ---- the loader: a thread has 16 codes of kPieces keys ----
-    const int key_of = tid / kChunks, chunk = tid % kChunks;
+    // ---- the loader: a wave has 16 keys of a tile, in one page, a thread 16 codes of kPieces of them ----
+    const int key_of = 16 * wave + lane / kChunks, chunk = lane % kChunks;
     auto first_key = [&](int32_t u) { return (u < t.sink_tiles ? u : t.low + u - t.sink_tiles) * kKeys; };
-    // the page of the 16 keys from `key` on, or -1: none, or one that no row sees (which may be another sequence's by now)
-    auto page_of = [&](int32_t key) -> int32_t {
-        const bool hidden = a.window && t.held - key - 15 >= a.window && key >= a.sinks;
-        return key < t.len && !hidden ? page_at(c, n, key >> c.page_log2) : -1;
+    // some row may see some of the wave's keys (others' entries in the table may be another sequence's by now)
+    auto sought = [&](int32_t key) -> bool {
+        return (key < t.len) & !((a.window != 0) & (t.held - key - 15 >= a.window) & (key >= a.sinks));
     };
-    int32_t pages[kPieces], scale_page = -1;
+    // (Entries are read a tile ahead of their use, and judged then.  Where there is a tile the table has a column, and the pool a page: no load needs a
+    // branch.)
+    const int32_t *row_of_table = c.table + (int64_t)n * c.max_pages;
+    int32_t entry = -1;
     auto look_up = [&](int32_t u) {
-        const int32_t k0 = first_key(u);
-#pragma unroll
-        for (int j = 0; j < kPieces; ++j) pages[j] = page_of((k0 + key_of + j * (kKeys / kPieces)) & ~15);
-        if (tid < 8) scale_page = page_of(k0 + 16 * (tid & 3));
+        const int32_t key = first_key(u) + 16 * wave;
+        entry = row_of_table[sought(key) ? key >> c.page_log2 : 0];
     };
     u32x4 kc[kPieces], vc[kPieces];
-    float scale = 0.f;
-    bool have = false;
+    float k_scale = 0.f, v_scale = 0.f;
+    int32_t count = 0;                                       // of the wave's keys, how many stand in a page
+    const uint32_t in_page = (uint32_t)(lane / kChunks) * D + 16 * chunk;
     auto fetch = [&](int32_t u) {
-        const int32_t k0 = first_key(u);
+        const int32_t key = first_key(u) + 16 * wave, e = __builtin_amdgcn_readfirstlane(entry);
+        const bool in = sought(key) & (e >= 0) & (e < c.num_pages);
+        count = in ? t.len - key : 0;
+        const int64_t page = ((int64_t)(in ? e : 0) * c.heads_kv + kv);
+        const int64_t at = (page * c.page_size + (key & (c.page_size - 1))) * D;
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-            const int32_t key = k0 + key_of + j * (kKeys / kPieces);
-            kc[j] = vc[j] = u32x4{0, 0, 0, 0};
-            if (pages[j] >= 0 && key < t.len) {
-                const int64_t at = (((int64_t)pages[j] * c.heads_kv + kv) * c.page_size + (key & (c.page_size - 1))) * D + 16 * chunk;
-                kc[j] = *reinterpret_cast<const u32x4 *>(c.k + at);
-                vc[j] = *reinterpret_cast<const u32x4 *>(c.v + at);
-            }
+            kc[j] = *reinterpret_cast<const u32x4 *>(c.k + at + (in_page + j * 1024));
+            vc[j] = *reinterpret_cast<const u32x4 *>(c.v + at + (in_page + j * 1024));
         }
-        if (tid < 8) {
-            have = scale_page >= 0;
-            scale = have ? (tid < 4 ? c.k_scale : c.v_scale)[(int64_t)scale_page * c.heads_kv + kv] : 0.f;
-        }
+        k_scale = c.k_scale[page];
+        v_scale = c.v_scale[page];
     };
-    auto leave = [&](int buf) {
-        bool odd = false;
+    auto leave = [&](uint32_t tile_at, int buf) {
+        // what stands behind the last token, or in no page of the sequence, may be anything: the product takes zeros
+        if (count < 16) {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vc[j][e] = lane / kChunks + j * (64 / kChunks) < count ? vc[j][e] : 0u;
+        }
+        const float ks = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(k_scale)));
+        const float vs = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v_scale)));
+        const bool pk = is_plain(ks), pv = is_plain(vs);
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-            const int r = key_of + j * (kKeys / kPieces);
+            const int r = key_of + j * (64 / kChunks);
             u32x4 o[2];
-            widen16(kc[j], o);
-            uint8_t *to = lds + 2 * buf * kT + r * 2 * D;
+            widen16(kc[j], pk ? ks : 1.f, o);
+            uint8_t *to = lds + tile_at + r * 2 * D;
 #pragma unroll
             for (int e = 0; e < 2; ++e) *reinterpret_cast<u32x4 *>(to + 16 * ((2 * chunk + e) ^ attn::swizzle<D>(r))) = o[e];
-            odd |= has_nan(vc[j]);
-            widen16(vc[j], o);
+            widen16(vc[j], pv ? vs : 1.f, o);
 #pragma unroll
             for (int e = 0; e < 2; ++e) *reinterpret_cast<u32x4 *>(to + kT + 16 * ((2 * chunk + e) ^ attn::swizzle<D>(r))) = o[e];
         }
-        if (tid < 8) reinterpret_cast<float *>(lds + Lds<D>::kScales)[8 * buf + tid] = scale;
-        if (tid < 4) reinterpret_cast<uint32_t *>(lds + Lds<D>::kHave)[4 * buf + tid] = have;
-        const uint32_t any = __any(odd);
-        if (lane == 0) reinterpret_cast<uint32_t *>(lds + Lds<D>::kOdd)[4 * buf + wave] = any;
+        if (lane == 0) {
+            // what is left of the scales
+            float *left = reinterpret_cast<float *>(lds + Lds<D>::kScales) + 8 * buf + wave;
+            left[0] = pk || count <= 0 ? 1.f : ks;
+            left[4] = pv || count <= 0 ? 1.f : vs;
+            reinterpret_cast<uint32_t *>(lds + Lds<D>::kHave)[4 * buf + wave] = (count > 0 ? 1u : 0u) | (pk && pv || count <= 0 ? 2u : 0u);
+        }
     };
 
     // ---- the rows ----
@@ -187,9 +198,10 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
     for (int db = 0; db < D / 32; ++db) acc[db] = attn::zeros16();
     float m = -kInf, mref = 0.f, l = 0.f;
 
-    auto work = [&](int32_t u, int buf) {
+    auto work = [&](int32_t u, auto parity) {
+        constexpr int buf = decltype(parity)::value;
+        constexpr uint32_t kt = 2 * buf * kT, vt = kt + kT;
         const int32_t k0 = first_key(u);
-        const uint32_t kt = 2 * buf * kT, vt = kt + kT;
         f32x16 st[KB];
 #pragma unroll
         for (int b = 0; b < KB; ++b) st[b] = attn::zeros16();
@@ -197,16 +209,26 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
             for (int b = 0; b < KB; ++b) st[b] = attn::mfma(rd.rows(kt, KB * wk + b, i), qf[i], st[b]);
-        const f32x4 *sc = reinterpret_cast<const f32x4 *>(lds + Lds<D>::kScales) + 2 * buf;
-        const f32x4 ks = sc[0], vs = sc[1];
+        attn::reads_ahead<kLead, 1, KB * D / 16, KB * D / 16>();
+        __builtin_amdgcn_sched_barrier(0);
         const u32x4 hv = *reinterpret_cast<const u32x4 *>(lds + Lds<D>::kHave + 16 * buf);
+        const uint32_t every = __builtin_amdgcn_readfirstlane(hv[0] & hv[1] & hv[2] & hv[3]);
+        // scales that the codes have not taken (of this wave's 16-key blocks)
+        typedef float f32xb __attribute__((ext_vector_type(2 * KB)));
+        f32xb vs;
+        bool large = false;
+        if (!(every & 2)) {
+            const f32xb ks = *reinterpret_cast<const f32xb *>(lds + Lds<D>::kScales + 32 * buf + 8 * KB * wk);
+            vs = *reinterpret_cast<const f32xb *>(lds + Lds<D>::kScales + 32 * buf + 16 + 8 * KB * wk);
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
+            for (int b = 0; b < 2 * KB; ++b) large |= (__float_as_uint(vs[b]) & 0x7fffffffu) >= kLargeScale;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) st[b][j] *= cs * ks[2 * (KB * wk + b) + j / 8];
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) st[b][j] *= ks[2 * b + j / 8];
+        }
         // some row does not see some key
-        const bool whole = hv[0] & hv[1] & hv[2] & hv[3];
-        const bool edge = __builtin_amdgcn_readfirstlane(!whole || k0 + kKeys - 1 >= t.held || (a.window && t.held + a.tokens - 1 - k0 >= a.window));
+        const bool edge = __builtin_amdgcn_readfirstlane(!(every & 1) || k0 + kKeys - 1 >= t.held || (a.window && t.held + a.tokens - 1 - k0 >= a.window));
         uint32_t seen[KB];
         if (edge) {
             const int32_t node = t.held - k0;                // the row of the first drafted token
@@ -215,7 +237,7 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
             uint64_t w = ((uint64_t)(ctx.w[1] | sinks.w[1]) << 32) | (ctx.w[0] | sinks.w[0]);
             w |= node >= 64 || node <= -64 ? 0ull : node >= 0 ? line << node : line >> -node;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) w &= hv[b] ? ~0ull : ~(0xffffull << (16 * b));
+            for (int b = 0; b < 4; ++b) w &= hv[b] & 1 ? ~0ull : ~(0xffffull << (16 * b));
             w = there ? w : 0ull;
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
@@ -224,15 +246,12 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
                 for (int j = 0; j < 16; ++j) st[b][j] = attn::where_seen(attn::seen_bit(seen[b], j), st[b][j], -kInf);
             }
         }
-        bool large = false;
-#pragma unroll
-        for (int b = 0; b < 2 * KB; ++b) large |= (__float_as_uint(vs[2 * KB * wk + b]) & 0x7fffffffu) >= kLargeScale;
         float top = st[0][0];
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, st[b][j]);
-        top = fmaxf(top, attn::other_half(top)) + (large ? kLift : 0.f);
+        top = fmaxf(top, attn::other_half(top)) * cs + (large ? kLift : 0.f);
         if (__any(top > m + 8.f)) {
             const float mn = fmaxf(m, top), f = mn == -kInf ? 1.f : fast_exp2(m - mn);
             m = mn;
@@ -249,43 +268,53 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
             float e[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                e[j] = fast_exp2(st[b][j] - mref);
+                e[j] = fast_exp2(fmaf(st[b][j], cs, -mref));
                 l += e[j];
-                e[j] *= vs[2 * (KB * wk + b) + j / 8];
             }
+            if (!(every & 2))
+#pragma unroll
+                for (int j = 0; j < 16; ++j) e[j] *= vs[2 * b + j / 8];
             p[2 * b] = attn::pack8(e);
             p[2 * b + 1] = attn::pack8(e + 8);
         }
-        const u32x4 od = *reinterpret_cast<const u32x4 *>(lds + Lds<D>::kOdd + 16 * buf);
-        if (edge && __builtin_amdgcn_readfirstlane(od[0] | od[1] | od[2] | od[3])) {
+        if (kCareful && edge) {
 #pragma unroll
             for (int db = 0; db < D / 32; ++db) attn::careful_product<D, 2 * KB>(acc[db], rd, vt, db, 2 * KB * wk, p, seen);
         } else {
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int s = 0; s < 2 * KB; ++s)
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db) acc[db] = attn::mfma(rd.transposed(vt, db, 2 * KB * wk + s), p[s], acc[db]);
+            attn::reads_ahead<2 * kLead, 2, 2 * KB * D / 16, KB * D / 16>();
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
     if (begin < end) {
         look_up(begin);
         fetch(begin);
-        if (begin + 1 < end) look_up(begin + 1);
-        for (int32_t u = begin; u < end; ++u) {
-            const int buf = (u - begin) & 1;
-            leave(buf);
-            if (u + 1 < end) {
-                fetch(u + 1);
-                if (u + 2 < end) look_up(u + 2);
-            }
+        look_up(min(begin + 1, end - 1));
+        auto step = [&](int32_t u, auto parity) {
+            constexpr int buf = decltype(parity)::value;
+            leave(2 * buf * kT, buf);
+            // (behind the last tile it is read again: a branch here would have the compiler move, and so wait for, what was read)
+            fetch(min(u + 1, end - 1));
+            look_up(min(u + 2, end - 1));
             __syncthreads();
-            if (working) work(u, buf);
+            if (working) work(u, parity);
+        };
+        int32_t u = begin;
+        for (; u + 1 < end; u += 2) {
+            step(u, std::integral_constant<int, 0>{});
+            step(u + 1, std::integral_constant<int, 1>{});
         }
+        if (u < end) step(u, std::integral_constant<int, 0>{});
     }
     l += attn::other_half(l);
 
     // ---- two waves' parts of the same rows ----
+    const bool again = !kCareful && attn::repeat(attn::not_finite(acc), 0);
     if constexpr (WK == 2) {
         __syncthreads();
         f32x4 *at = reinterpret_cast<f32x4 *>(lds) + wr * (D / 32 * 4) * 64 + lane;
@@ -297,7 +326,7 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
             stats[1] = l;
         }
         __syncthreads();
-        if (wk == 1) return;
+        if (wk == 1) return again;
         const float mo = stats[0], lo = stats[1], mn = fmaxf(m, mo);
         // (a part that saw nothing adds nothing; one that is NaN stays so)
         const float f0 = m == -kInf ? 0.f : fast_exp2(m - mn), f1 = mo == -kInf ? 0.f : fast_exp2(mo - mn);
@@ -310,7 +339,7 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
         }
         m = mn;
     }
-    if (row >= a.rows) return;
+    if (row >= a.rows) return again;
     if (!there || t.held < 0) {                              // (whatever tiles that every row sees whole have left)
         m = -kInf;
         l = 0.f;
@@ -328,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
             a.stats[part * 2] = m;
             a.stats[part * 2 + 1] = l;
         }
-        return;
+        return again;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int64_t out = (((int64_t)n * a.tokens + tok) * c.heads_q + head) * D + 4 * h;
@@ -341,6 +370,15 @@ __global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, c
             if (a.out_bf16) *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.o) + w) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
             else *reinterpret_cast<f32x4 *>(static_cast<float *>(a.o) + w) = y;
         }
+    return again;
+}
+template <int D, int WR> __device__ __noinline__ void tree_tile_again(const Cache c, const TreeAttend a) { tree_tile<D, WR, true>(c, a); }
+template <int D, int WR>
+__global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, const TreeAttend a)
+{
+    if (!tree_tile<D, WR, false>(c, a)) return;
+    __syncthreads();                                         // (LDS is read to the end)
+    tree_tile_again<D, WR>(c, a);
 }
 
 }  // namespace cache
