@@ -104,7 +104,7 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
 
     // ---- the trees' lines, and what the window leaves of them ----
     uint64_t *lines = reinterpret_cast<uint64_t *>(lds + Lds<D>::kLine);
-    if (wave == 0) lines[lane] = tree_line(a.parents + (int64_t)n * a.tokens, a.tokens);
+    if (wave == 0) lines[lane] = tree_line(lane < a.tokens ? a.parents[(int64_t)n * a.tokens + lane] : -2, a.tokens);
     __syncthreads();
     const int row0 = (tile * WR + wr) * 32, row = row0 + x;
     const bool working = row0 < a.rows;

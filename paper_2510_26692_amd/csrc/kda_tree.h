@@ -7,12 +7,11 @@ namespace kda {
 
 constexpr int kTreeTokens = 64;      // the largest tree: a token a lane
 
-// What lane t's token has above it: itself and its ancestors as bits, none where there is no such token.  Every lane of the wave takes part.
-// (Six doublings: after i of them a lane has its next 2^i ancestors, and the number of the one behind them.)
-__device__ __forceinline__ uint64_t tree_line(const int32_t *parents, int tokens)
+// What lane t's token, with the parent `up`, has above it: itself and its ancestors as bits, none where there is no such token.  Every lane of
+// the wave takes part.  (Six doublings: after i of them a lane has its next 2^i ancestors, and the number of the one behind them.)
+__device__ __forceinline__ uint64_t tree_line(int32_t up, int tokens)
 {
     const int lane = threadIdx.x & 63;
-    int32_t up = lane < tokens ? parents[lane] : -2;
     bool there = up >= -1 && up < lane && lane < tokens;
     up = there ? up : -1;
     uint32_t lo = lane < 32 ? 1u << lane : 0u, hi = lane < 32 ? 0u : 1u << (lane - 32);

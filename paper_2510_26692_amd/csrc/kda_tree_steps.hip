@@ -11,8 +11,14 @@
 // multiplication a token and channel, never as the quotient of two long products.  Everything is fp32; the two products with S_0 are
 // 16x16x4 fp32 MFMAs.
 //
-// A workgroup has one sequence and head, a wave 32 columns of its state, held in registers from the start.  What bounds it is reading the
-// states, and for large trees the fp32 matrix cores: 4 T dk dv operations a state of 4 dk dv bytes.
+// A workgroup has one sequence and head, a wave 32 columns of its state, held in registers from the start.  The sums over channels make a lower
+// triangular matrix N = -beta (sum k P k), zero but at ancestors, whose 16x16 blocks take the u of one block of tokens to the next:
+//
+//     r_m = beta (v - P k S_0) + sum_{n < m} N_mn u_n,     u_m = (I - N_mm)^-1 r_m,     o_m = scale P q S_0 + sum_{n <= m} (scale sum q P k)_mn u_n
+//
+// all of them fp32 MFMAs whose accumulators are the operands of the next, so u never leaves its registers.
+//
+// What bounds it is reading the states, and for large trees the fp32 matrix cores: 4 T dk dv operations a state of 4 dk dv bytes.
 #include "kda_tree.h"
 
 namespace kda {
@@ -30,11 +36,14 @@ struct Tree {
     int32_t heads, tokens, scalar_gate, out_bf16;
 };
 
-// four neighbours of a token's row
-__device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
-__device__ __forceinline__ f32x4 load4(const __hip_bfloat16 *p)
+// four neighbours of a token's row, as they come and in fp32
+template <typename T> struct FourOf;
+template <> struct FourOf<float> { typedef f32x4 type; };
+template <> struct FourOf<__hip_bfloat16> { typedef u32x2 type; };
+template <typename T> using Four = typename FourOf<T>::type;
+__device__ __forceinline__ f32x4 widened(const f32x4 &w) { return w; }
+__device__ __forceinline__ f32x4 widened(const u32x2 &w)
 {
-    const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
     f32x4 x;
     float lo, hi;
     unpack_bf16x2(w[0], lo, hi);
@@ -45,6 +54,7 @@ __device__ __forceinline__ f32x4 load4(const __hip_bfloat16 *p)
     x[3] = hi;
     return x;
 }
+template <typename T> __device__ __forceinline__ f32x4 load4(const T *p) { return widened(*reinterpret_cast<const Four<T> *>(p)); }
 __device__ __forceinline__ f32x2 load2(const float *p) { return *reinterpret_cast<const f32x2 *>(p); }
 __device__ __forceinline__ f32x2 load2(const __hip_bfloat16 *p)
 {
@@ -59,82 +69,114 @@ template <int kCtrl> __device__ __forceinline__ float add_rotated(float v)
 }
 __device__ __forceinline__ float over_sixteen(float v) { return add_rotated<0x121>(add_rotated<0x122>(add_rotated<0x124>(add_rotated<0x128>(v)))); }
 
-// LDS: decays, k and q of the tokens, [TM][D + 4] each, the first two replaced by what the products with S_0 give; then for each token and ancestor
-// the two sums over channels, beta (sum k P k) and scale (sum q P k).
-template <int D, int TM> struct StepLds {
-    static constexpr int kPitch = D + 4;
-    static constexpr int kRows = TM * kPitch;                // floats
-    static constexpr int kSums = 3 * kRows;
-    static constexpr int kLines = kSums + 2 * TM * TM;
-    static constexpr int kBytes = (kLines + 2 * kTreeTokens) * 4;
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+__device__ __forceinline__ f32x4 mfma16(const f32x4 &a, const f32x4 &b, f32x4 acc)      // a 16 x 16 x 16 product: slot g of step i is index 4 g + i
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], acc, 0, 0, 0);
+    return acc;
+}
+
+// LDS: decays of the tokens in fp32, then their k and q as they came, [TM][D + 4] each; in the same place P_i0 k_i and scale P_i0 q_i in fp32; and then the two
+// matrices of sums over channels, [TM][TM + 4] each.  Behind them the lines.
+template <typename Tin, int D, int TM> struct StepLds {
+    static constexpr int kPitch = D + 4, kSumPitch = TM + 4;
+    static constexpr int kRows = TM * kPitch;
+    static constexpr int kTokens = kRows * (4 + 2 * (int)sizeof(Tin)), kProducts = 2 * kRows * 4, kSums = 2 * TM * kSumPitch * 4;
+    static constexpr int kMost = kTokens > kProducts ? kTokens : kProducts, kLines = kMost > kSums ? kMost : kSums;
+    static constexpr int kBytes = kLines + kTreeTokens * 8;
 };
 
 template <typename Tin, int D, int TM>
-__global__ __launch_bounds__(2 * D) void kda_tree_steps_kernel(const Tree a)
+__global__ __launch_bounds__(2 * D, 2) void kda_tree_steps_kernel(const Tree a)
 {
-    using L = StepLds<D, TM>;
+    using L = StepLds<Tin, D, TM>;
     constexpr int kThreads = 2 * D, kGroups = D / 8, kNodes = TM / kGroups > 0 ? TM / kGroups : 1;      // groups of 16 lanes; tokens of one
     constexpr int CH = D / 16;                               // channels of a lane in a group
-    constexpr int MT = TM / 16;                              // 16-row blocks of the tokens' products, for k and for q
-    extern __shared__ __align__(16) float lds[];
-    float *al = lds, *kk = lds + L::kRows, *qq = lds + 2 * L::kRows;
-    f32x2 *sums = reinterpret_cast<f32x2 *>(lds + L::kSums);
+    constexpr int MT = TM / 16;                              // 16-token blocks
+    extern __shared__ __align__(16) uint8_t lds[];
+    float *al = reinterpret_cast<float *>(lds);
+    Tin *kk = reinterpret_cast<Tin *>(al + L::kRows), *qq = kk + L::kRows;
     uint64_t *lines = reinterpret_cast<uint64_t *>(lds + L::kLines);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, x = lane & 15, g = lane >> 4;
     const int64_t n = blockIdx.x / a.heads;
     const int h = (int)(blockIdx.x - n * a.heads), T = a.tokens;
     const int64_t row0 = n * T * a.heads + h;                // row of token 0; the next is `heads` behind
     const int64_t state = a.indices ? a.indices[n] : n;
-    auto put = [&](int t, int col, float v) {
+    const int col = 32 * wave + 2 * x;                       // the lane's columns are this and the next
+    auto put = [&](int t, float lo, float hi) {
         const int64_t at = (row0 + (int64_t)t * a.heads) * D + col;
-        if (a.out_bf16) static_cast<uint16_t *>(a.o)[at] = (uint16_t)pack_bf16x2(v, 0.f);
-        else static_cast<float *>(a.o)[at] = v;
+        if (a.out_bf16) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(a.o) + at) = pack_bf16x2(lo, hi);
+        else *reinterpret_cast<f32x2 *>(static_cast<float *>(a.o) + at) = f32x2{lo, hi};
     };
     if (state < 0) {
-        for (int i = tid; i < T * D; i += kThreads) put(i / D, i % D, 0.f);
+        for (int t = g; t < T; t += 4) put(t, 0.f, 0.f);
         return;
     }
-    // ---- the state: columns 32 wave + 2 x, and the next; rows 16 s + 4 g + i ----
+    // ---- everything is asked for at once: parents and tokens, which are needed first, then the state ----
+    int32_t up = -2;
+    if (wave == 0 && lane < T) up = a.parents[n * T + lane];
+    constexpr int kPieces = TM * (D / 4) / kThreads;         // fours of a thread
+    Four<Tin> qv[kPieces], kv[kPieces], lv[kPieces];
+    Tin lh[kPieces];
+    {
+        const Tin *q = static_cast<const Tin *>(a.q), *k = static_cast<const Tin *>(a.k), *la = static_cast<const Tin *>(a.log_alpha);
+#pragma unroll
+        for (int r = 0; r < kPieces; ++r) {
+            const int t = min((tid + kThreads * r) / (D / 4), T - 1), c = 4 * (tid % (D / 4));
+            const int64_t row = row0 + (int64_t)t * a.heads;
+            kv[r] = *reinterpret_cast<const Four<Tin> *>(k + row * D + c);
+            qv[r] = *reinterpret_cast<const Four<Tin> *>(q + row * D + c);
+            if (a.scalar_gate) lh[r] = la[row];
+            else lv[r] = *reinterpret_cast<const Four<Tin> *>(la + row * D + c);
+        }
+    }
+    f32x2 vv[MT][4];
+    float beta[MT][4];
+    auto values = [&]() {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t row = row0 + (int64_t)min(16 * m + 4 * g + e, T - 1) * a.heads;
+                vv[m][e] = load2(static_cast<const Tin *>(a.v) + row * D + col);
+                beta[m][e] = load_as_float(static_cast<const Tin *>(a.beta) + row);
+            }
+    };
+    if constexpr (MT < 4) values();                          // (a large tree's wait until there are registers for them)
+    // the state's rows 16 s + 4 g + i
     f32x2 s0[D / 16][4];
     {
-        const float *from = a.states + (state * a.heads + h) * (D * D) + (4 * g) * D + 32 * wave + 2 * x;
+        const float *from = a.states + (state * a.heads + h) * (D * D) + (4 * g) * D + col;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s)
 #pragma unroll
             for (int i = 0; i < 4; ++i) s0[s][i] = __builtin_nontemporal_load(reinterpret_cast<const f32x2 *>(from + (16 * s + i) * D));
     }
-    if (wave == 0) lines[lane] = tree_line(a.parents + n * T, T);
+    if (wave == 0) lines[lane] = tree_line(up, T);
     __syncthreads();
-
     // ---- tokens (one that is not there: no key, no query, no decay) ----
-    {
-        const Tin *q = static_cast<const Tin *>(a.q), *k = static_cast<const Tin *>(a.k), *la = static_cast<const Tin *>(a.log_alpha);
-        for (int i = tid; i < TM * (D / 4); i += kThreads) {
-            const int t = i / (D / 4), c = 4 * (i % (D / 4));
-            f32x4 qv = {0.f, 0.f, 0.f, 0.f}, kv = qv, av = {1.f, 1.f, 1.f, 1.f};
-            if (t < T && lines[t]) {
-                const int64_t row = row0 + (int64_t)t * a.heads;
-                qv = load4(q + row * D + c);
-                kv = load4(k + row * D + c);
-                if (a.scalar_gate) av = f32x4{1.f, 1.f, 1.f, 1.f} * load_as_float(la + row);
-                else av = load4(la + row * D + c);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) av[e] = fast_exp2(av[e] * kLog2e);
-            }
-            *reinterpret_cast<f32x4 *>(al + t * L::kPitch + c) = av;
-            *reinterpret_cast<f32x4 *>(kk + t * L::kPitch + c) = kv;
-            *reinterpret_cast<f32x4 *>(qq + t * L::kPitch + c) = qv;
-        }
+    for (int r = 0; r < kPieces; ++r) {
+        const int t = (tid + kThreads * r) / (D / 4), c = 4 * (tid % (D / 4));
+        const bool there = t < T && lines[t];
+        f32x4 av = f32x4{1.f, 1.f, 1.f, 1.f} * (a.scalar_gate ? load_as_float(&lh[r]) : 0.f);
+        if (!a.scalar_gate) av = widened(lv[r]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) av[e] = there ? fast_exp2(av[e] * kLog2e) : 1.f;
+        *reinterpret_cast<f32x4 *>(al + t * L::kPitch + c) = av;
+        *reinterpret_cast<Four<Tin> *>(kk + t * L::kPitch + c) = there ? kv[r] : Four<Tin>{};
+        *reinterpret_cast<Four<Tin> *>(qq + t * L::kPitch + c) = there ? qv[r] : Four<Tin>{};
     }
     __syncthreads();
 
-    // ---- up every token's line: the sums over channels, and the product of all decays ----
-    float all[kNodes][CH];
+    // ---- up every token's line: the sums over channels, column j with lane j % 16, and the product of all decays ----
     const int group = tid >> 4;
-    auto channels = [&](const float *rows, int t, float (&v)[CH]) {
+    float all[kNodes][CH], nk[kNodes][MT], nq[kNodes][MT];
+    auto channels = [&](const auto *rows, int t, float (&v)[CH]) {
 #pragma unroll
         for (int i = 0; i < CH; i += 4) {
-            const f32x4 w = *reinterpret_cast<const f32x4 *>(rows + t * L::kPitch + CH * x + i);
+            const f32x4 w = load4(rows + t * L::kPitch + CH * x + i);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[i + e] = w[e];
         }
@@ -144,13 +186,16 @@ __global__ __launch_bounds__(2 * D) void kda_tree_steps_kernel(const Tree a)
         const int t = group + kGroups * r;
 #pragma unroll
         for (int i = 0; i < CH; ++i) all[r][i] = 1.f;
-        if (t >= T) continue;
-        uint64_t line = lines[t];
-        if (!line) continue;
-        const float beta = load_as_float(static_cast<const Tin *>(a.beta) + row0 + (int64_t)t * a.heads);
-        float kt[CH], qt[CH];
-        channels(kk, t, kt);
-        channels(qq, t, qt);
+#pragma unroll
+        for (int c = 0; c < MT; ++c) nk[r][c] = nq[r][c] = 0.f;
+        uint64_t line = 0;
+        float b = 0.f, kt[CH], qt[CH];
+        if (t < TM) {
+            channels(kk, t, kt);
+            channels(qq, t, qt);
+            line = lines[t];
+            if (line) b = load_as_float(static_cast<const Tin *>(a.beta) + row0 + (int64_t)t * a.heads);
+        }
         while (line) {
             const int j = 63 - __builtin_clzll(line);
             line &= ~(1ull << j);
@@ -164,53 +209,59 @@ __global__ __launch_bounds__(2 * D) void kda_tree_steps_kernel(const Tree a)
                 dq = fmaf(qt[i], w, dq);
                 all[r][i] *= aj[i];
             }
-            dk = over_sixteen(dk);
-            dq = over_sixteen(dq);
-            if (x == 0) sums[t * TM + j] = f32x2{beta * dk, a.scale * dq};
+            dk = j < t ? -b * over_sixteen(dk) : 0.f;
+            dq = a.scale * over_sixteen(dq);
+            // (one that is not finite belongs to a token whose own r or o is not: zero here, it stays out of the others')
+            dk = finite(dk) ? dk : 0.f;
+            dq = finite(dq) ? dq : 0.f;
+#pragma unroll
+            for (int c = 0; c < MT; ++c) {
+                const bool here = x == (j & 15) && c == j >> 4;
+                nk[r][c] = here ? dk : nk[r][c];
+                nq[r][c] = here ? dq : nq[r][c];
+            }
         }
     }
     __syncthreads();
-    // ---- P_i0 k_i and scale P_i0 q_i ----
+    // ---- P_i0 k_i and scale P_i0 q_i, where the tokens stood ----
+    float *pk = reinterpret_cast<float *>(lds), *pq = pk + L::kRows;
+    {
+        float kt[kNodes][CH], qt[kNodes][CH];
 #pragma unroll
-    for (int r = 0; r < kNodes; ++r) {
-        const int t = group + kGroups * r;
-        if (t >= TM) continue;
-        float v[CH];
-        channels(kk, t, v);
+        for (int r = 0; r < kNodes; ++r) {
+            const int t = min(group + kGroups * r, TM - 1);
+            channels(kk, t, kt[r]);
+            channels(qq, t, qt[r]);
 #pragma unroll
-        for (int i = 0; i < CH; i += 4)
-            *reinterpret_cast<f32x4 *>(kk + t * L::kPitch + CH * x + i) = f32x4{v[i] * all[r][i], v[i + 1] * all[r][i + 1], v[i + 2] * all[r][i + 2], v[i + 3] * all[r][i + 3]};
-        channels(qq, t, v);
+            for (int i = 0; i < CH; ++i) {
+                kt[r][i] *= all[r][i];
+                qt[r][i] *= all[r][i] * a.scale;
+            }
+        }
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < CH; i += 4)
-            *reinterpret_cast<f32x4 *>(qq + t * L::kPitch + CH * x + i) = f32x4{v[i] * all[r][i], v[i + 1] * all[r][i + 1], v[i + 2] * all[r][i + 2], v[i + 3] * all[r][i + 3]} * a.scale;
+        for (int r = 0; r < kNodes; ++r) {
+            const int t = group + kGroups * r;
+            if (t >= TM) continue;
+#pragma unroll
+            for (int i = 0; i < CH; i += 4) {
+                *reinterpret_cast<f32x4 *>(pk + t * L::kPitch + CH * x + i) = f32x4{kt[r][i], kt[r][i + 1], kt[r][i + 2], kt[r][i + 3]};
+                *reinterpret_cast<f32x4 *>(pq + t * L::kPitch + CH * x + i) = f32x4{qt[r][i], qt[r][i + 1], qt[r][i + 2], qt[r][i + 3]};
+            }
+        }
     }
     __syncthreads();
 
-    // ---- their products with S_0; lane's rows 16 m + 4 g + e, columns 32 wave + 2 x + j ----
+    // ---- their products with S_0: tokens 16 m + 4 g + e ----
+    if constexpr (MT == 4) values();
     f32x4 acc[2][MT][2];
-    f32x2 vv[MT][4];
-    float beta[MT][4];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int t = 16 * m + 4 * g + e;
-            vv[m][e] = f32x2{0.f, 0.f};
-            beta[m][e] = 0.f;
-            if (t < T && lines[t]) {
-                const int64_t row = row0 + (int64_t)t * a.heads;
-                vv[m][e] = load2(static_cast<const Tin *>(a.v) + row * D + 32 * wave + 2 * x);
-                beta[m][e] = load_as_float(static_cast<const Tin *>(a.beta) + row);
-            }
-        }
 #pragma unroll
     for (int w = 0; w < 2; ++w)
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             acc[w][m][0] = acc[w][m][1] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (16 * m >= T) continue;
-            const float *rows = (w ? qq : kk) + (16 * m + x) * L::kPitch + 4 * g;
+            const float *rows = (w ? pq : pk) + (16 * m + x) * L::kPitch + 4 * g;
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
                 const f32x4 r = *reinterpret_cast<const f32x4 *>(rows + 16 * s);
@@ -221,40 +272,106 @@ __global__ __launch_bounds__(2 * D) void kda_tree_steps_kernel(const Tree a)
             }
         }
     __syncthreads();
-    float *u = lds, *os = lds + L::kRows;
+    // ---- the matrices, and the inverses of the first one's diagonal blocks in their places ----
+    float *sk = reinterpret_cast<float *>(lds), *sq = sk + TM * L::kSumPitch;
+#pragma unroll
+    for (int r = 0; r < kNodes; ++r) {
+        const int t = group + kGroups * r;
+        if (t >= TM) continue;
+#pragma unroll
+        for (int c = 0; c < MT; ++c) {
+            sk[t * L::kSumPitch + 16 * c + x] = nk[r][c];
+            sq[t * L::kSumPitch + 16 * c + x] = nq[r][c];
+        }
+    }
+    // r, but for what is not finite, which the descendants of its token see and no others
+    uint32_t odd = 0;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = beta[m][e] * (vv[m][e][j] - acc[0][m][j][e]);
+                const bool ok = finite(v) || !lines[16 * m + 4 * g + e];
+                acc[0][m][j][e] = finite(v) ? v : 0.f;
+                odd |= (ok ? 0u : 1u) << (8 * m + 4 * j + e);
+            }
+    __syncthreads();
+    if (group < MT) {
+        // lane x has column x of the inverse: row by row, v_i = [i == x] + sum_{k < i} N_ik v_k
+        float *block = sk + 16 * group * L::kSumPitch + 16 * group;
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float sum = i == x ? 1.f : 0.f;
+#pragma unroll
+            for (int k = 0; k < i; k += 4) {
+                const f32x4 w = *reinterpret_cast<const f32x4 *>(block + i * L::kSumPitch + k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (k + e < i) sum = fmaf(w[e], v[k + e], sum);
+            }
+            v[i] = sum;
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) block[i * L::kSumPitch + x] = v[i];
+    }
+    __syncthreads();
+
+    // ---- down the blocks of tokens ----
+    auto part = [&](const float *s, int m, int k) { return *reinterpret_cast<const f32x4 *>(s + (16 * m + x) * L::kSumPitch + 16 * k + 4 * g); };
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        if (16 * m >= T) continue;
+#pragma unroll
+        for (int k = 0; k <= m; ++k) {
+            const f32x4 w = part(sk, m, k);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[0][m][j] = k < m ? mfma16(w, acc[0][k][j], acc[0][m][j]) : mfma16(w, acc[0][m][j], f32x4{0.f, 0.f, 0.f, 0.f});
+        }
+#pragma unroll
+        for (int k = 0; k <= m; ++k) {
+            const f32x4 w = part(sq, m, k);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[1][m][j] = mfma16(w, acc[0][k][j], acc[1][m][j]);
+        }
+    }
+    if (__any(odd)) {
+        // how many tokens of each line were taken out
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const uint64_t line = lines[16 * m + x];
+            f32x4 seen[2] = {};
+#pragma unroll
+            for (int k = 0; k <= m; ++k) {
+                f32x4 w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = (line >> (16 * k + 4 * g + e)) & 1 ? 1.f : 0.f;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    f32x4 marks;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) marks[e] = (odd >> (8 * k + 4 * j + e)) & 1 ? 1.f : 0.f;
+                    seen[j] = mfma16(w, marks, seen[j]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[1][m][j][e] = seen[j][e] > 0.f ? __builtin_nanf("") : acc[1][m][j][e];
+        }
+    }
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int t = 16 * m + 4 * g + e, at = t * L::kPitch + 32 * wave + 2 * x;
-            *reinterpret_cast<f32x2 *>(u + at) = f32x2{beta[m][e] * (vv[m][e][0] - acc[0][m][0][e]), beta[m][e] * (vv[m][e][1] - acc[0][m][1][e])};
-            *reinterpret_cast<f32x2 *>(os + at) = f32x2{acc[1][m][0][e], acc[1][m][1][e]};
+            const int t = 16 * m + 4 * g + e;
+            if (t >= T) continue;
+            const bool there = lines[t] != 0;
+            put(t, there ? acc[1][m][0][e] : 0.f, there ? acc[1][m][1][e] : 0.f);
         }
-    __syncthreads();
-
-    // ---- corrections and outputs, a column a thread, down the tree ----
-    if (tid >= D) return;
-    for (int t = 0; t < T; ++t) {
-        const uint64_t mine = lines[t];
-        const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(mine >> 32)), lo = __builtin_amdgcn_readfirstlane((uint32_t)mine);
-        uint64_t line = (uint64_t)hi << 32 | lo;
-        if (!line) {
-            put(t, tid, 0.f);
-            continue;
-        }
-        line &= ~(1ull << t);
-        float ut = u[t * L::kPitch + tid], ot = os[t * L::kPitch + tid];
-        while (line) {
-            const int j = __builtin_ctzll(line);
-            line &= line - 1;
-            const f32x2 w = sums[t * TM + j];
-            const float uj = u[j * L::kPitch + tid];
-            ut = fmaf(-w[0], uj, ut);
-            ot = fmaf(w[1], uj, ot);
-        }
-        u[t * L::kPitch + tid] = ut;
-        put(t, tid, fmaf(sums[t * TM + t][1], ut, ot));
-    }
 }
 
 struct Commit {
@@ -332,7 +449,7 @@ __global__ __launch_bounds__(2 * D) void kda_tree_commit_kernel(const Commit a)
 
 template <typename Tin, int D, int TM> hipError_t launch_steps(const Tree &a, int64_t pairs, hipStream_t st)
 {
-    constexpr int kBytes = StepLds<D, TM>::kBytes;
+    constexpr int kBytes = StepLds<Tin, D, TM>::kBytes;
     if (kBytes > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kda_tree_steps_kernel<Tin, D, TM>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
