@@ -1,4 +1,4 @@
-// The decode calls of the Python binding (kda.py) and those of the softmax-attention layers (attn.py), marshalled natively: a decode step of one sequence takes the device 4 us, and the
+// The decode calls of the Python binding (kda.py), those of the softmax-attention layers (attn.py) and those of draft trees and shared pages (tree.py), marshalled natively: a decode step of one sequence takes the device 4 us, and the
 // checks, descriptors and ctypes of the general path 10 us of the host (measured in a loop of kda_recurrent_step, 1 sequence x 32
 // heads: 9.9 us a call through kda.py alone, 4.2 to 5.0 here; kda_cache_append of one token 17 and 5.2).
 //
@@ -28,6 +28,16 @@ decltype(&kda_cache_attn_workspace_size) attend_size_entry;
 decltype(&kda_window_attn_fwd) fwd_entry;
 decltype(&kda_window_attn_bwd) bwd_entry;
 decltype(&kda_window_attn_bwd_workspace_size) bwd_size_entry;
+decltype(&kda_rotate) rotate_entry;
+decltype(&kda_cache_tree_attn) tree_attend_entry;
+decltype(&kda_cache_tree_attn_workspace_size) tree_attend_size_entry;
+decltype(&kda_cache_keep) keep_entry;
+decltype(&kda_cache_copy_pages) copy_entry;
+decltype(&kda_tree_steps) tree_steps_entry;
+decltype(&kda_tree_commit) tree_commit_entry;
+decltype(&kda_pages_fork) fork_entry;
+decltype(&kda_pages_reserve) reserve_entry;
+decltype(&kda_pages_reserve_workspace_size) reserve_size_entry;
 PyObject *raw_stream;                                        // device index -> current stream, as a number
 
 struct Irregular {};
@@ -422,6 +432,285 @@ PyObject *window_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+const int32_t *int32s(PyObject *x, const Checked &check, at::IntArrayRef shape) { return static_cast<const int32_t *>(check(x, at::kInt, shape).data_ptr()); }
+PyObject *nothing(kda_status st)
+{
+    if (st != KDA_OK) return PyLong_FromLong((long)st);
+    Py_RETURN_TRUE;                                          // (None is a call that this way leaves to the other)
+}
+
+// rotate(q, k, positions, inv_freq, axes, interleaved, inverse, q_out, k_out); axes: None or bytes
+PyObject *rotate(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 9 || !rotate_entry) throw Irregular{};
+        const at::Tensor &q = plain(a[0]), &pos = plain(a[2]), &f = plain(a[3]);
+        if (q.dim() != 4 || f.dim() != 1 || (pos.dim() != 2 && pos.dim() != 3)) throw Irregular{};
+        const Checked check(q);
+        const at::ScalarType type = q.scalar_type();
+        check(q, type, q.sizes());
+        const int64_t B = q.size(0), T = q.size(1);
+        kda_rotation r{};
+        r.batch = narrow(B); r.seqlen = T; r.heads_q = narrow(q.size(2)); r.dim = narrow(q.size(3)); r.dtype = (kda_dtype)code(type);
+        at::Tensor k, q_out, k_out;
+        if (a[1] != Py_None) {
+            k = plain(a[1]);
+            if (k.dim() != 4) throw Irregular{};
+            check(k, type, {B, T, k.size(2), q.size(3)});
+            r.heads_k = narrow(k.size(2));
+            k_out = a[8] != Py_None ? check(a[8], type, k.sizes()) : at::empty(k.sizes(), k.options());
+        } else if (a[8] != Py_None) {
+            throw Irregular{};
+        }
+        q_out = a[7] != Py_None ? check(a[7], type, q.sizes()) : at::empty(q.sizes(), q.options());
+        r.axes = pos.dim() == 3 ? narrow(pos.size(0)) : 1;
+        if (pos.dim() == 3) check(pos, at::kInt, {r.axes, B, T});
+        else check(pos, at::kInt, {B, T});
+        r.num_freqs = narrow(f.size(0));
+        r.inv_freq = static_cast<const float *>(check(f, at::kFloat, f.sizes()).data_ptr());
+        if (a[4] != Py_None) {
+            if (!PyBytes_CheckExact(a[4]) || PyBytes_GET_SIZE(a[4]) != r.num_freqs) throw Irregular{};
+            r.axis_of_freq = reinterpret_cast<const uint8_t *>(PyBytes_AS_STRING(a[4]));
+        }
+        r.interleaved = truth(a[5]);
+        r.inverse = truth(a[6]);
+        const Current on(q.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = rotate_entry(&r, q.data_ptr(), k.defined() ? k.data_ptr() : nullptr, static_cast<const int32_t *>(pos.data_ptr()), q_out.data_ptr(),
+                          k_out.defined() ? k_out.data_ptr() : nullptr, stream);
+        Py_END_ALLOW_THREADS
+        return pair(st, a[7], q_out, a[8], k_out);
+    });
+}
+
+// tree_attend(q, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, parents, window, sinks, scale, max_kv_len, o, out_dtype)
+PyObject *tree_attend(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 14 || !tree_attend_entry) throw Irregular{};
+        const at::Tensor &q = plain(a[0]), &kc = plain(a[1]);
+        if (q.dim() != 4 || kc.dim() != 4) throw Irregular{};
+        const int64_t N = q.size(0), T = q.size(1), Hq = q.size(2), d = q.size(3);
+        const Checked check(q);
+        check(q, at::kBFloat16, {N, T, Hq, d});
+        const kda_cache c = cache_of(a + 1, check, N, Hq, kc.size(1), d);
+        const int32_t *parents = int32s(a[7], check, {N, T});
+        const at::Tensor o = output(a[12], a[13], q, check);
+        kda_cache_query query{};
+        query.tokens = narrow(T); query.window = whole(a[8]); query.sinks = narrow(whole(a[9])); query.scale = attn_scale(a[10], d);
+        query.max_kv_len = whole(a[11]); query.out_dtype = (kda_dtype)code(o.scalar_type());
+        const size_t need = tree_attend_size_entry(&c, &query);
+        const at::Tensor ws = need ? bytes(need, q) : at::Tensor();
+        const Current on(q.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = tree_attend_entry(&c, &query, q.data_ptr(), parents, o.data_ptr(), need ? ws.data_ptr() : nullptr, need, stream);
+        Py_END_ALLOW_THREADS
+        return finish(st, a[12], o);
+    });
+}
+
+// A layer's or a stack's cache a[0..3], and its layers.
+kda_cache stack_of(PyObject *const *a, const at::Tensor &k, const Checked &check, int32_t &layers)
+{
+    if (k.dim() != 4 && k.dim() != 5) throw Irregular{};
+    const int at = k.dim() - 4;
+    layers = at ? narrow(k.size(0)) : 1;
+    check(k, at::kFloat8_e4m3fn, k.sizes());
+    kda_cache c{};
+    c.num_pages = k.size(at); c.heads_q = c.heads_kv = narrow(k.size(at + 1)); c.page_size = narrow(k.size(at + 2)); c.dim = narrow(k.size(at + 3));
+    c.k = k.data_ptr(); c.v = check(a[1], at::kFloat8_e4m3fn, k.sizes()).data_ptr();
+    c.k_scale = static_cast<float *>(check(a[2], at::kFloat, k.sizes().slice(0, at + 2)).data_ptr());
+    c.v_scale = static_cast<float *>(check(a[3], at::kFloat, k.sizes().slice(0, at + 2)).data_ptr());
+    return c;
+}
+
+// keep(k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, kept)
+PyObject *keep(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 7 || !keep_entry) throw Irregular{};
+        const at::Tensor &k = plain(a[0]), &table = plain(a[4]), &kept = plain(a[6]);
+        if (table.dim() != 2 || kept.dim() != 2) throw Irregular{};
+        const Checked check(k);
+        int32_t layers;
+        kda_cache c = stack_of(a, k, check, layers);
+        const int64_t N = table.size(0);
+        c.num_seqs = narrow(N); c.max_pages = narrow(table.size(1));
+        c.block_table = int32s(a[4], check, {N, table.size(1)});
+        c.kv_lens = int32s(a[5], check, {N});
+        const int32_t *path = int32s(a[6], check, {N, kept.size(1)});
+        const Current on(k.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = keep_entry(&c, layers, path, narrow(kept.size(1)), stream);
+        Py_END_ALLOW_THREADS
+        return nothing(st);
+    });
+}
+
+// copy_pages(k_cache, v_cache, k_scale, v_scale, pairs)
+PyObject *copy_pages(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 5 || !copy_entry) throw Irregular{};
+        const at::Tensor &k = plain(a[0]), &pairs = plain(a[4]);
+        if (pairs.dim() != 2) throw Irregular{};
+        const Checked check(k);
+        int32_t layers;
+        const kda_cache c = stack_of(a, k, check, layers);
+        const int32_t *list = int32s(a[4], check, {pairs.size(0), 2});
+        const Current on(k.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = copy_entry(&c, layers, list, pairs.size(0), stream);
+        Py_END_ALLOW_THREADS
+        return nothing(st);
+    });
+}
+
+// fork(block_table, page_refs, source)
+PyObject *fork_rows(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 3 || !fork_entry) throw Irregular{};
+        const at::Tensor &table = plain(a[0]), &refs = plain(a[1]);
+        if (table.dim() != 2 || refs.dim() != 1) throw Irregular{};
+        const Checked check(table);
+        check(table, at::kInt, table.sizes());
+        check(refs, at::kInt, refs.sizes());
+        const int32_t *source = int32s(a[2], check, {table.size(0)});
+        const Current on(table.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = fork_entry(static_cast<int32_t *>(table.data_ptr()), narrow(table.size(0)), narrow(table.size(1)), static_cast<int32_t *>(refs.data_ptr()),
+                        refs.size(0), source, stream);
+        Py_END_ALLOW_THREADS
+        return nothing(st);
+    });
+}
+
+// reserve(block_table, kv_lens, new_lens, page_refs, page_size, copies, missing)
+PyObject *reserve(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 7 || !reserve_entry) throw Irregular{};
+        const at::Tensor &table = plain(a[0]), &refs = plain(a[3]);
+        if (table.dim() != 2 || refs.dim() != 1) throw Irregular{};
+        const Checked check(table);
+        check(table, at::kInt, table.sizes());
+        check(refs, at::kInt, refs.sizes());
+        const int64_t N = table.size(0);
+        const int32_t *lens = int32s(a[1], check, {N}), *after = int32s(a[2], check, {N});
+        const at::Tensor copies = a[5] != Py_None ? check(a[5], at::kInt, {N, 2}) : at::empty({N, 2}, table.options());
+        const at::Tensor missing = a[6] != Py_None ? check(a[6], at::kInt, {1}) : at::empty({1}, table.options());
+        const int32_t rows = narrow(N), columns = narrow(table.size(1)), page = narrow(whole(a[4]));
+        const size_t need = reserve_size_entry(rows, columns, refs.size(0));
+        const at::Tensor ws = need ? bytes(need, table) : at::Tensor();
+        const Current on(table.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = reserve_entry(static_cast<int32_t *>(table.data_ptr()), rows, columns, page, static_cast<int32_t *>(refs.data_ptr()), refs.size(0), lens, after,
+                           static_cast<int32_t *>(copies.data_ptr()), static_cast<int32_t *>(missing.data_ptr()), need ? ws.data_ptr() : nullptr, need, stream);
+        Py_END_ALLOW_THREADS
+        return pair(st, a[5], copies, a[6], missing);
+    });
+}
+
+// What kda_tree_steps and kda_tree_commit share: a[0..5] are k, v, log_alpha, beta, S_pool, state_indices.
+struct Delta {
+    kda_dims d;
+    const void *k, *v, *la, *beta;
+    float *S;
+    const int32_t *indices = nullptr;
+    Delta(PyObject *const *a, const at::Tensor &kt, const Checked &check, bool scalar_gate, int out, float scale)
+    {
+        const at::Tensor &vt = plain(a[1]), &St = plain(a[4]);
+        if (kt.dim() != 4 || vt.dim() != 4 || St.dim() != 4) throw Irregular{};
+        const int64_t N = kt.size(0), T = kt.size(1), H = kt.size(2), dk = kt.size(3), dv = vt.size(3);
+        const at::ScalarType type = kt.scalar_type();
+        k = check(kt, type, {N, T, H, dk}).data_ptr();
+        v = check(vt, type, {N, T, H, dv}).data_ptr();
+        la = scalar_gate ? check(a[2], type, {N, T, H}).data_ptr() : check(a[2], type, {N, T, H, dk}).data_ptr();
+        beta = check(a[3], type, {N, T, H}).data_ptr();
+        S = static_cast<float *>(check(St, at::kFloat, {St.size(0), H, dk, dv}).data_ptr());
+        if (a[5] != Py_None) indices = int32s(a[5], check, {N});
+        else if (St.size(0) < N) throw Irregular{};
+        d = decode_dims(N, T, H, dk, dv, code(type), out, scale);
+    }
+};
+
+// tree_steps(k, v, log_alpha, beta, S_pool, state_indices, q, parents, scale, o, out_dtype, scalar_gate)
+PyObject *tree_steps(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 12 || !tree_steps_entry) throw Irregular{};
+        const at::Tensor &k = plain(a[0]), &v = plain(a[1]);
+        const Checked check(k);
+        const bool scalar = truth(a[11]);
+        const at::Tensor o = output(a[9], a[10], v, check);
+        const Delta x(a, k, check, scalar, code(o.scalar_type()), number(a[8]));
+        const at::Tensor &q = check(a[6], k.scalar_type(), k.sizes());
+        const int32_t *parents = int32s(a[7], check, {k.size(0), k.size(1)});
+        const Current on(k.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = tree_steps_entry(&x.d, q.data_ptr(), x.k, x.v, x.la, x.beta, x.S, x.indices, parents, o.data_ptr(), scalar ? KDA_STEPS_SCALAR_GATE : 0, stream);
+        Py_END_ALLOW_THREADS
+        return finish(st, a[9], o);
+    });
+}
+
+// tree_commit(k, v, log_alpha, beta, S_pool, state_indices, kept, scalar_gate)
+PyObject *tree_commit(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 8 || !tree_commit_entry) throw Irregular{};
+        const at::Tensor &k = plain(a[0]), &kept = plain(a[6]);
+        if (kept.dim() != 2) throw Irregular{};
+        const Checked check(k);
+        const bool scalar = truth(a[7]);
+        const Delta x(a, k, check, scalar, KDA_F32, 1.f);
+        const int32_t *path = int32s(a[6], check, {k.size(0), kept.size(1)});
+        const Current on(k.device());
+        void *stream = stream_of(check.device);
+        kda_status st;
+        Py_BEGIN_ALLOW_THREADS
+        st = tree_commit_entry(&x.d, x.k, x.v, x.la, x.beta, x.S, x.indices, path, narrow(kept.size(1)), scalar ? KDA_STEPS_SCALAR_GATE : 0, stream);
+        Py_END_ALLOW_THREADS
+        return nothing(st);
+    });
+}
+
+// bind_tree(addresses of kda_rotate, kda_cache_tree_attn, kda_cache_tree_attn_workspace_size, kda_cache_keep, kda_cache_copy_pages, kda_tree_steps,
+// kda_tree_commit, kda_pages_fork, kda_pages_reserve, kda_pages_reserve_workspace_size), after bind
+PyObject *bind_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 10) { PyErr_SetString(PyExc_TypeError, "bind_tree takes ten arguments"); return nullptr; }
+    void *p[10];
+    for (int i = 0; i < 10; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+    rotate_entry = reinterpret_cast<decltype(rotate_entry)>(p[0]);
+    tree_attend_entry = reinterpret_cast<decltype(tree_attend_entry)>(p[1]);
+    tree_attend_size_entry = reinterpret_cast<decltype(tree_attend_size_entry)>(p[2]);
+    keep_entry = reinterpret_cast<decltype(keep_entry)>(p[3]);
+    copy_entry = reinterpret_cast<decltype(copy_entry)>(p[4]);
+    tree_steps_entry = reinterpret_cast<decltype(tree_steps_entry)>(p[5]);
+    tree_commit_entry = reinterpret_cast<decltype(tree_commit_entry)>(p[6]);
+    fork_entry = reinterpret_cast<decltype(fork_entry)>(p[7]);
+    reserve_entry = reinterpret_cast<decltype(reserve_entry)>(p[8]);
+    reserve_size_entry = reinterpret_cast<decltype(reserve_size_entry)>(p[9]);
+    Py_RETURN_NONE;
+}
+
 // bind_attn(addresses of kda_cache_append, kda_cache_attn, kda_cache_attn_workspace_size, kda_window_attn_fwd, kda_window_attn_bwd,
 // kda_window_attn_bwd_workspace_size), after bind
 PyObject *bind_attn(PyObject *, PyObject *const *a, Py_ssize_t n)
@@ -462,6 +751,15 @@ PyMethodDef methods[] = {
     {"attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attend)), METH_FASTCALL, nullptr},
     {"window_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(window_fwd)), METH_FASTCALL, nullptr},
     {"window_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(window_bwd)), METH_FASTCALL, nullptr},
+    {"bind_tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind_tree)), METH_FASTCALL, nullptr},
+    {"rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(rotate)), METH_FASTCALL, nullptr},
+    {"tree_attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(tree_attend)), METH_FASTCALL, nullptr},
+    {"keep", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(keep)), METH_FASTCALL, nullptr},
+    {"copy_pages", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(copy_pages)), METH_FASTCALL, nullptr},
+    {"fork", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(fork_rows)), METH_FASTCALL, nullptr},
+    {"reserve", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(reserve)), METH_FASTCALL, nullptr},
+    {"tree_steps", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(tree_steps)), METH_FASTCALL, nullptr},
+    {"tree_commit", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(tree_commit)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kda_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -166,6 +166,9 @@ def load_library():
         _kda_host.bind_attn(*[ctypes.cast(f, vp).value for f in (lib.kda_cache_append, lib.kda_cache_attn, lib.kda_cache_attn_workspace_size,
                                                                  lib.kda_window_attn_fwd, lib.kda_window_attn_bwd,
                                                                  lib.kda_window_attn_bwd_workspace_size)])
+        _kda_host.bind_tree(*[ctypes.cast(f, vp).value for f in (lib.kda_rotate, lib.kda_cache_tree_attn, lib.kda_cache_tree_attn_workspace_size,
+                                                                 lib.kda_cache_keep, lib.kda_cache_copy_pages, lib.kda_tree_steps, lib.kda_tree_commit,
+                                                                 lib.kda_pages_fork, lib.kda_pages_reserve, lib.kda_pages_reserve_workspace_size)])
         _native = _kda_host
     except ImportError as e:                # (missing, or built for another torch or interpreter: right all the same, but no secret)
         warnings.warn("decode calls are marshalled in Python, at about twice the host time: %s (build it with "

@@ -7,7 +7,7 @@ import ctypes
 
 import torch
 
-from .attn import KdaCache, KdaCacheQuery, _cache, _device, _token_stride
+from .attn import KdaCache, KdaCacheQuery, _cache, _device, _native, _token_stride
 from .kda import KdaDims, _DTYPE_CODE, _SCALAR_GATE, _call, _check_dev, _out_dtype, _ptr, load_library
 
 
@@ -31,6 +31,11 @@ def kda_rotate(q, k, positions, inv_freq, axes=None, interleaved=False, inverse=
     (2 i, 2 i + 1); those from 2 n on stay as they are.  inverse=True turns back, which is the rotation's gradient too: dq, dk from those of
     the outputs.  Returns (q_out, k_out or None), contiguous, of the inputs' dtype; either may be given and be the (contiguous) input itself."""
     lib = load_library()
+    if axes is not None:
+        axes = bytes(list(axes))            # (numbers beyond a byte are refused here, those beyond the axes by the library)
+    done = _native("rotate", q, k, positions, inv_freq, axes, interleaved, inverse, q_out, k_out)
+    if done is not None:
+        return done
     dev = _device(q, k, positions, inv_freq, q_out, k_out)
     if q.dim() != 4 or q.dtype not in _DTYPE_CODE:
         raise ValueError("q must be bf16 or fp32 [B,T,Hq,d]")
@@ -47,10 +52,8 @@ def kda_rotate(q, k, positions, inv_freq, axes=None, interleaved=False, inverse=
     if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq must be contiguous fp32 [n]")
     n, A = inv_freq.numel(), positions.shape[0] if positions.dim() == 3 else 1
-    if axes is not None:
-        axes = bytes(axes)                  # (numbers beyond a byte are refused here, those beyond the axes by the library)
-        if len(axes) != n:
-            raise ValueError("axes must hold a number for each of the %d frequencies" % n)
+    if axes is not None and len(axes) != n:
+        raise ValueError("axes must hold a number for each of the %d frequencies" % n)
     for t, like, name in ((q_out, q, "q_out"), (k_out, k, "k_out")):
         if t is not None and (t.dtype != like.dtype or t.shape != like.shape or not t.is_contiguous()):
             raise ValueError("%s must be contiguous, of the shape and dtype of what is turned" % name)
@@ -73,6 +76,10 @@ def kda_cache_tree_attn(q, k_cache, v_cache, k_scale, v_scale, block_table, kv_l
     token.  A token sees what is held (within window and sinks, from the position kv_lens + its depth), its ancestors and itself.
     max_kv_len: upper bound of kv_lens + Tq if known.  Returns o [N,Tq,Hq,d] as kda_cache_attn; rows of tokens that are not there are zero."""
     lib = load_library()
+    if workspace is None:
+        done = _native("tree_attend", q, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, parents, window, sinks, scale, max_kv_len, o, out_dtype)
+        if done is not None:
+            return done
     dev = _device(q, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, parents, o, workspace)
     if q.dim() != 4 or q.dtype != torch.bfloat16:
         raise ValueError("q must be bf16 [N,Tq,Hq,d]")
@@ -115,6 +122,8 @@ def kda_cache_keep(k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, kep
     dimension of layers in front of all four.  block_table int32 [N,pages] and kv_lens int32 [N] (without the drafted tokens; negative: skip;
     not changed here) are the layers' own in common; kept int32 [N,up to 64]: increasing indices of drafted tokens, ended by a negative one."""
     lib = load_library()
+    if _native("keep", k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, kept):
+        return
     dev = _check_dev(k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, kept)
     L, P, Hk, page, d = _layers(k_cache, v_cache, k_scale, v_scale)
     if block_table.dtype != torch.int32 or block_table.dim() != 2:
@@ -133,6 +142,8 @@ def kda_cache_copy_pages(k_cache, v_cache, k_scale, v_scale, pairs):
     """Copies pages, codes and scales, of one layer's cache or of a whole stack's (as for kda_cache_keep), in place.  pairs int32 [M,2]: (from,
     to); a pair with an entry that is no page, like (-1, -1), is skipped.  No page may be written by two pairs, or by one and read by another."""
     lib = load_library()
+    if _native("copy_pages", k_cache, v_cache, k_scale, v_scale, pairs):
+        return
     dev = _check_dev(k_cache, v_cache, k_scale, v_scale, pairs)
     L, P, Hk, page, d = _layers(k_cache, v_cache, k_scale, v_scale)
     if pairs.dtype != torch.int32 or pairs.dim() != 2 or pairs.shape[1] != 2:
@@ -155,6 +166,8 @@ def kda_pages_fork(block_table, page_refs, source):
     row n is row source[n] (source int32 [N]; n itself, or N and above: it stays), or empty where source[n] is negative, which frees the
     pages that no other row has.  A page with no reference is free."""
     lib = load_library()
+    if _native("fork", block_table, page_refs, source):
+        return
     dev, N, columns, P = _pages(block_table, page_refs, source)
     _int32(source, (N,), "source")
     _call(dev, lib.kda_pages_fork, _ptr(block_table), N, columns, _ptr(page_refs), P, _ptr(source))
@@ -166,6 +179,10 @@ def kda_pages_reserve(block_table, kv_lens, new_lens, page_refs, page_size, copi
     [N,2], missing int32 [1]): copies for kda_cache_copy_pages, (-1, -1) where a sequence needs none; missing is how many pages were too few, and
     then nothing has changed."""
     lib = load_library()
+    if workspace is None:
+        done = _native("reserve", block_table, kv_lens, new_lens, page_refs, page_size, copies, missing)
+        if done is not None:
+            return done
     dev, N, columns, P = _pages(block_table, page_refs, kv_lens, new_lens, copies, missing, workspace)
     _int32(kv_lens, (N,), "kv_lens")
     _int32(new_lens, (N,), "new_lens")
@@ -222,6 +239,9 @@ def kda_tree_steps(q, k, v, log_alpha, beta, S_pool, parents, state_indices=None
     sequences may share a state.  Returns o [N,Tq,H,dv], fp32 unless out_dtype (or the `o` passed in) is torch.bfloat16; rows of skipped
     sequences and of tokens that are not there are zero."""
     lib = load_library()
+    done = _native("tree_steps", k, v, log_alpha, beta, S_pool, state_indices, q, parents, scale, o, out_dtype, scalar_gate)
+    if done is not None:
+        return done
     dev = _check_dev(q, k, v, log_alpha, beta, S_pool, parents, state_indices, o)
     N, Tq, H, dk, dv = _delta(k, v, log_alpha, beta, S_pool, state_indices, scalar_gate)
     if q.shape != k.shape or q.dtype != k.dtype:
@@ -243,6 +263,8 @@ def kda_tree_commit(k, v, log_alpha, beta, S_pool, kept, state_indices=None, sca
     """Takes the states of S_pool, in place, through the accepted tokens of the trees that kda_tree_steps had: kept int32 [N,up to 64],
     increasing indices ended by a negative one.  The other arguments are those of kda_tree_steps."""
     lib = load_library()
+    if _native("tree_commit", k, v, log_alpha, beta, S_pool, state_indices, kept, scalar_gate):
+        return
     dev = _check_dev(k, v, log_alpha, beta, S_pool, state_indices, kept)
     N, Tq, H, dk, dv = _delta(k, v, log_alpha, beta, S_pool, state_indices, scalar_gate)
     if kept.dtype != torch.int32 or kept.dim() != 2 or kept.shape[0] != N:
