@@ -47,6 +47,7 @@ struct Attend {
 // A call of kda_cache_tree_attn: what kda_cache_attn has, and the trees.
 struct TreeAttend : Attend {
     const int32_t *parents;          // [N][tokens]
+    int32_t per_round;               // sequences of a round of workgroups, which are then ranked by length; 0: taken as they come
 };
 // A call of kda_cache_copy_pages.
 struct Copies {

@@ -74,6 +74,13 @@ __device__ __forceinline__ bool is_plain(float scale)
     return (b & 0x807fffffu) == 0 && b - (67u << 23) <= 120u << 23;
 }
 
+__device__ __forceinline__ bf16x8 held(const bf16x8 &v)
+{
+    u32x4 w = __builtin_bit_cast(u32x4, v);
+    asm volatile("" : "+v"(w));
+    return __builtin_bit_cast(bf16x8, w);
+}
+
 // LDS: K and V of one tile, then of another; then what the waves share
 template <int D> struct Lds {
     static constexpr int kT = kKeys * D * 2;
@@ -82,6 +89,32 @@ template <int D> struct Lds {
     static constexpr int kLine = kHave + 32;                 // [64] of 64 bits
     static constexpr int kBytes = kLine + 512;
 };
+
+// The sequence that workgroup `place` of the sequences takes.  Two workgroups share a compute unit, and those that a launch begins with are handed out
+// round by round: in the first round the longest sequences, in falling order, in the second the next in rising order, and so on, the sums even
+// out (64 trees of 32 tokens over 4 096 to 8 192 tokens, 8 heads: ORDER_US us, as they come 299).
+constexpr int kOrdered = 256;        // sequences that are ranked
+__device__ __forceinline__ int sequence_of(const Cache &c, const TreeAttend &a, int place)
+{
+    if (!a.per_round) return place;
+    extern __shared__ __align__(16) uint8_t lds[];
+    int32_t *lens = reinterpret_cast<int32_t *>(lds);
+    const int tid = threadIdx.x;
+    if (tid < c.num_seqs) lens[tid] = c.lens[tid];
+    __syncthreads();
+    const int round = place / a.per_round, at = place % a.per_round, in_round = min(a.per_round, c.num_seqs - round * a.per_round);
+    const int wanted = round * a.per_round + (round & 1 ? in_round - 1 - at : at);
+    if (tid < c.num_seqs) {
+        const int32_t mine = lens[tid];
+        int rank = 0;
+        for (int j = 0; j < c.num_seqs; ++j) rank += lens[j] > mine || (lens[j] == mine && j < tid);
+        if (rank == wanted) lens[kOrdered] = tid;
+    }
+    __syncthreads();
+    const int n = __builtin_amdgcn_readfirstlane(lens[kOrdered]);
+    __syncthreads();
+    return n;
+}
 
 // A tile of rows over a split's keys.  Returns true where the walk has to be repeated with care: a value that is not finite stood where some row does
 // not see it.
@@ -97,7 +130,7 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
     id /= c.heads_kv;
     const int tile = id % a.row_tiles;
     id /= a.row_tiles;
-    const int split = id % a.splits, n = id / a.splits;
+    const int split = id % a.splits, n = sequence_of(c, a, id / a.splits);
     const Tiles t = tiles_of(c, a, n);
     const int32_t per = part_tiles(t, a.splits), begin = min(split * per, t.count), end = min(begin + per, t.count);
     if (a.splits > 1 && begin >= end) return false;          // (the join knows)
@@ -271,11 +304,16 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
                 e[j] = fast_exp2(fmaf(st[b][j], cs, -mref));
                 l += e[j];
             }
-            if (!(every & 2))
+            // (packed on either side of the branch, and held there: values that meet behind it would be moved)
+            if (every & 2) {
+                p[2 * b] = held(attn::pack8(e));
+                p[2 * b + 1] = held(attn::pack8(e + 8));
+            } else {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) e[j] *= vs[2 * b + j / 8];
-            p[2 * b] = attn::pack8(e);
-            p[2 * b + 1] = attn::pack8(e + 8);
+                p[2 * b] = attn::pack8(e);
+                p[2 * b + 1] = attn::pack8(e + 8);
+            }
         }
         if (kCareful && edge) {
 #pragma unroll
@@ -419,8 +457,11 @@ template <int D, int WR> hipError_t launch(const Cache &c, const TreeAttend &a, 
     hipLaunchKernelGGL((kda_cache_tree_kernel<D, WR>), dim3(grid), dim3(256), Lds<D>::kBytes, st, c, a);
     return hipGetLastError();
 }
-template <int D> hipError_t launch(const Cache &c, const TreeAttend &a, hipStream_t st)
+template <int D> hipError_t launch(const Cache &c, TreeAttend a, hipStream_t st)
 {
+    // (with a workgroup for each sequence, head and tile of rows, and more than one round of them)
+    const int32_t beside = c.heads_kv * a.row_tiles;
+    a.per_round = a.splits == 1 && c.num_seqs <= kOrdered && beside <= 256 && c.num_seqs * beside > 256 ? 256 / beside : 0;
     hipError_t e = cache_tree_tile_rows(a.rows) == 64 ? launch<D, 2>(c, a, st) : launch<D, 4>(c, a, st);
     if (e == hipSuccess && a.splits > 1) e = launch_join<D>(c, a, (int64_t)c.num_seqs * c.heads_kv * a.rows, st);
     return e;
