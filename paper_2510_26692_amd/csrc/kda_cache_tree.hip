@@ -92,7 +92,7 @@ template <int D> struct Lds {
 
 // The sequence that workgroup `place` of the sequences takes.  Two workgroups share a compute unit, and those that a launch begins with are handed out
 // round by round: in the first round the longest sequences, in falling order, in the second the next in rising order, and so on, the sums even
-// out (64 trees of 32 tokens over 4 096 to 8 192 tokens, 8 heads: ORDER_US us, as they come 299).
+// out (64 trees of 32 tokens over 4 096 to 8 192 tokens, 8 heads: 266 us, as they come 285).
 constexpr int kOrdered = 256;        // sequences that are ranked
 __device__ __forceinline__ int sequence_of(const Cache &c, const TreeAttend &a, int place)
 {
@@ -236,6 +236,8 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
         constexpr uint32_t kt = 2 * buf * kT, vt = kt + kT;
         const int32_t k0 = first_key(u);
         f32x16 st[KB];
+        // (a wave at its products goes ahead of one at its exponentials: 2 %)
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int b = 0; b < KB; ++b) st[b] = attn::zeros16();
 #pragma unroll
@@ -244,6 +246,7 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
             for (int b = 0; b < KB; ++b) st[b] = attn::mfma(rd.rows(kt, KB * wk + b, i), qf[i], st[b]);
         attn::reads_ahead<kLead, 1, KB * D / 16, KB * D / 16>();
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
         const u32x4 hv = *reinterpret_cast<const u32x4 *>(lds + Lds<D>::kHave + 16 * buf);
         const uint32_t every = __builtin_amdgcn_readfirstlane(hv[0] & hv[1] & hv[2] & hv[3]);
         // scales that the codes have not taken (of this wave's 16-key blocks)
@@ -320,12 +323,14 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
             for (int db = 0; db < D / 32; ++db) attn::careful_product<D, 2 * KB>(acc[db], rd, vt, db, 2 * KB * wk, p, seen);
         } else {
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int s = 0; s < 2 * KB; ++s)
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db) acc[db] = attn::mfma(rd.transposed(vt, db, 2 * KB * wk + s), p[s], acc[db]);
             attn::reads_ahead<2 * kLead, 2, 2 * KB * D / 16, KB * D / 16>();
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
         }
     };
 
