@@ -616,7 +616,8 @@ kda_status kda_tree_commit(const kda_dims *dims, const void *k, const void *v, c
  * ---- Pages that several sequences share ----
  *
  * block_table as in kda_cache; page_refs [num_pages] int32: how many of its entries name a page.  A page with none is free.
- * Entries outside [0, num_pages) are no page and not counted.
+ * Entries outside [0, num_pages) are no page and not counted.  Counts are the caller's to begin with (zeros beside a table of -1) and kept by these calls;
+ * they are 16-byte aligned.
  */
 
 /*
@@ -634,6 +635,7 @@ kda_status kda_pages_fork(int32_t *block_table, int32_t num_seqs, int32_t max_pa
  * columns; a page that is replaced loses a reference.  Tokens behind the table's columns get no page.
  *   copies      [num_seqs,2] int32, written: (from, to) for a sequence whose page of column kv_lens[n] / page_size is replaced and holds older
  *               tokens, for kda_cache_copy_pages; else (-1, -1)
+ *               (a page whose last reference goes is free from then on: the copies have to be made before anything else takes or writes it)
  *   missing     [1] int32, written: 0, or by how many pages the free ones fall short: then nothing else is changed, and copies are all (-1, -1)
  * num_seqs at most 8192, num_seqs * max_pages below 2^31.  workspace: kda_pages_reserve_workspace_size bytes, 256-byte aligned.
  */

@@ -206,7 +206,7 @@ __global__ __launch_bounds__(kThreads) void kda_pages_moves_kernel(const Compact
         for (int i = 0; i < 16; ++i) {
             const int64_t p = at + i;
             const int32_t r = s.v[i / 4][i % 4];
-            if (p < used && r == 0) a.moves[2 * (p - n) + 1] = (int32_t)p;
+            if (p < used && r <= 0) a.moves[2 * (p - n) + 1] = (int32_t)p;          // (every page that is not in use: ranks have no gaps)
             if (p >= used && p < a.pages) {
                 a.rank[p] = r > 0 ? n - below : -1;
                 if (r > 0) a.moves[2 * (n - below)] = (int32_t)p;
