@@ -434,13 +434,18 @@ namespace kda {
 
 int32_t cache_tree_tile_rows(int32_t rows) { return rows <= 64 ? 64 : 128; }
 
-// Workgroups of a tile of rows: enough for two on every compute unit, each with two tiles of keys at least.
+// Workgroups of a tile of rows: enough for two on every compute unit, or one where that leaves each fewer than five tiles of keys, and each with two at
+// least; none is split where one a compute unit has at most 16.  us with two / one on every compute unit (16 tokens x 32 heads over 8): four sequences of 2 000
+// tokens 22.4 / 19.6, one of 16 000 22.5 / 21.6, 16 of 8 000 62 / 88; eight of 4 000 with trees of 32 36.3 / 38.7; 32 of 1 000 split in two / whole 34.3 / 27.8.
 int32_t cache_tree_splits(const Cache &, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
 {
     int64_t keys = most_keys;
     if (window && window + tokens + sinks + 2 * kKeys < keys) keys = window + tokens + sinks + 2 * kKeys;
-    const int64_t steps = (keys + kKeys - 1) / kKeys, most = (steps + 1) / 2, want = (512 + tiles - 1) / (tiles > 0 ? tiles : 1);
-    const int64_t n = want < most ? want : most;
+    const int64_t steps = (keys + kKeys - 1) / kKeys, most = (steps + 1) / 2, all = tiles > 0 ? tiles : 1;
+    int64_t n = (512 + all - 1) / all;
+    if (steps < 5 * n) n = (256 + all - 1) / all;
+    if (all >= 256 && steps <= 16) n = 1;
+    n = n < most ? n : most;
     return (int32_t)(n < 1 ? 1 : n);
 }
 
