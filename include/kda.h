@@ -572,7 +572,7 @@ kda_status kda_rotate(const kda_rotation *rotation, const void *q, const void *k
  *   query       tokens 0..64, the rest as for kda_cache_attn; max_kv_len: upper bound of kv_lens[n] + tokens
  *   parents     [num_seqs,tokens] int32
  *   workspace   at least kda_cache_tree_attn_workspace_size bytes (0 for some calls), 256-byte aligned
- * Scales and what is not finite: as for kda_cache_attn.
+ * Scales and what is not finite: as for kda_cache_attn.  o must not alias an input.
  */
 size_t kda_cache_tree_attn_workspace_size(const kda_cache *cache, const kda_cache_query *query);
 kda_status kda_cache_tree_attn(const kda_cache *cache, const kda_cache_query *query, const void *q, const int32_t *parents, void *o,
@@ -599,7 +599,7 @@ kda_status kda_cache_keep(const kda_cache *cache, int32_t layers, const int32_t 
  *   parents        [N,Tq] int32
  *   o              [N,Tq,H,dv]   out_dtype, either with either in_dtype
  *   flags          KDA_STEPS_SCALAR_GATE: log_alpha is [N,Tq,H]
- * All arithmetic is fp32.  No workspace.
+ * All arithmetic is fp32.  What is not finite in a token reaches its own row and its descendants' alone.  o must not alias an input.  No workspace.
  */
 kda_status kda_tree_steps(const kda_dims *dims, const void *q, const void *k, const void *v, const void *log_alpha, const void *beta,
                           const float *S_pool, const int32_t *state_indices, const int32_t *parents, void *o, uint32_t flags, void *hip_stream);

@@ -1,4 +1,5 @@
-"""MI355X-native Kimi Delta Attention (KDA), forward and backward: thin binding over libkda.so.
+"""MI355X-native Kimi Delta Attention (KDA), forward and backward, the softmax attention of a hybrid stack's other layers, and draft trees through
+both: thin binding over libkda.so.
 
 The package holds the HIP sources (``csrc/``), the in-tree build script and a
 ctypes binding whose functions carry the names of the C entry points in

@@ -18,7 +18,9 @@
 //
 // all of them fp32 MFMAs whose accumulators are the operands of the next, so u never leaves its registers.
 //
-// What bounds it is reading the states, and for large trees the fp32 matrix cores: 4 T dk dv operations a state of 4 dk dv bytes.
+// What bounds it is reading the states, and for large trees the fp32 matrix cores: 4 T dk dv operations a state of 4 dk dv bytes.  256 trees of up
+// to 16 tokens, 32 heads: 151 us (0.68 GB, 4.5 TB/s); 64 of 64 tokens: 169, the matrix cores 44 % busy.  (With a column a thread and a loop over
+// each token's ancestors in place of the blocks: 231 and 474.)
 #include "kda_tree.h"
 
 namespace kda {
@@ -383,7 +385,7 @@ struct Commit {
 constexpr int kAtOnce = 8;           // tokens in LDS
 
 // The accepted tokens, as the decode kernel steps (kda_step.hip): a wave has 32 columns of a state, 8 row groups by 8 groups of four columns, in
-// registers from the first token to the last.
+// registers from the first token to the last.  256 x 32 states of 64 KiB through paths of up to 16 tokens in 192 us, 5.6 TB/s.
 template <typename Tin, int D>
 __global__ __launch_bounds__(2 * D) void kda_tree_commit_kernel(const Commit a)
 {
