@@ -9,6 +9,8 @@ kda_status cache_attn_dispatch(const cache::Cache &, const cache::Attend &, int 
 kda_status cache_tree_dispatch(const cache::Cache &, const cache::TreeAttend &, int dim, hipStream_t);
 int32_t cache_tree_splits(const cache::Cache &, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens);
 int32_t cache_tree_tile_rows(int32_t rows);
+int32_t cache_few_rows(int dim);
+kda_status cache_few_dispatch(const cache::Cache &, const cache::TreeAttend &, int dim, hipStream_t);
 kda_status cache_copy_dispatch(const cache::Cache &, cache::Copies, hipStream_t);
 kda_status cache_keep_dispatch(const cache::Cache &, const cache::Keep &, int dim, hipStream_t);
 int32_t cache_attn_splits(const cache::Cache &, int64_t pairs, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens);
@@ -87,11 +89,12 @@ kda_status check(const kda_cache *d, bool buffers, const kda_cache_query *q, boo
     a.out_bf16 = q->out_dtype == KDA_BF16;
     if (const kda_status st = stride_of(q->q_stride, (int64_t)d->heads_q * d->dim, "q", a.q_stride); st != KDA_OK) return st;
     a.rows = q->tokens * c.group;
-    const int32_t tile = tree ? cache_tree_tile_rows(a.rows) : 32;
+    const bool few = tree && a.rows <= cache_few_rows(d->dim);
+    const int32_t tile = tree && !few ? cache_tree_tile_rows(a.rows) : 32;
     a.row_tiles = (a.rows + tile - 1) / tile;
     const int64_t pairs = (int64_t)c.num_seqs * c.heads_kv, held = (int64_t)d->max_pages * d->page_size;
     const int64_t most = q->max_kv_len && q->max_kv_len < held ? q->max_kv_len : held;
-    a.splits = !pairs || !a.rows ? 1 : (tree ? cache_tree_splits : cache_attn_splits)(c, pairs * a.row_tiles, most, a.window, a.sinks, a.tokens);
+    a.splits = !pairs || !a.rows ? 1 : (tree && !few ? cache_tree_splits : cache_attn_splits)(c, pairs * a.row_tiles, most, a.window, a.sinks, a.tokens);
     // (a launch has fewer than 2^32 threads: 256 a workgroup, and 64 a row of the join)
     if (pairs * a.row_tiles * a.splits > 0xffffff || pairs * a.rows > 0x3ffffff) return fail(KDA_ERR_UNSUPPORTED, "more than 2^24 workgroups");
     return KDA_OK;
@@ -211,7 +214,7 @@ extern "C" kda_status kda_cache_tree_attn(const kda_cache *cache, const kda_cach
     a.q = static_cast<const uint16_t *>(q);
     a.o = o;
     a.parents = parents;
-    return cache_tree_dispatch(c, a, cache->dim, static_cast<hipStream_t>(hip_stream));
+    return (a.rows <= cache_few_rows(cache->dim) ? cache_few_dispatch : cache_tree_dispatch)(c, a, cache->dim, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" kda_status kda_cache_keep(const kda_cache *cache, int32_t layers, const int32_t *kept, int32_t max_kept, void *hip_stream)

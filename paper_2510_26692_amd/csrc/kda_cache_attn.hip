@@ -20,6 +20,7 @@
 // sequence and head (as many as fill the device) through the workspace and a second kernel, in a fixed order.
 #include "kda_cache.h"
 #include "kda_cache_join.h"
+#include "kda_tree.h"
 
 namespace kda {
 namespace cache {
@@ -29,14 +30,25 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int kStep = 32;            // keys of a step
 
+// A call of kda_cache_tree_attn whose rows are few (a type of its own: its parts are this file's steps).
+struct FewRows : TreeAttend {};
+
+// Places that a sequence's tokens take, the new ones among them.
+__device__ __forceinline__ int32_t places(const Cache &c, const Attend &, int n) { return c.lens[n]; }
+__device__ __forceinline__ int32_t places(const Cache &c, const FewRows &a, int n)
+{
+    const int32_t held = c.lens[n];
+    return held < 0 ? -1 : min(held, 1 << 30) + a.tokens;
+}
+
 // The visible keys of a sequence's new tokens as steps: those of the sinks where the window begins behind them, then the window's.
 struct Steps {
     int32_t len, low;                // keys; first step of the window
     int32_t sink_steps, count;
 };
-__device__ __forceinline__ Steps steps_of(const Cache &c, const Attend &a, int n)
+template <typename A> __device__ __forceinline__ Steps steps_of(const Cache &c, const A &a, int n)
 {
-    const int32_t most = c.max_pages << c.page_log2, l = c.lens[n];          // (below 2^31)
+    const int32_t most = c.max_pages << c.page_log2, l = places(c, a, n);    // (below 2^31)
     Steps s;
     s.len = l < 0 ? 0 : min(l, most);
     // the first new token's window begins at l - tokens - window + 1
@@ -71,9 +83,11 @@ template <typename F> __device__ __forceinline__ float over_groups(float v, F f)
 
 // RB: blocks of 16 rows.  More than 32 rows go to several workgroups, side by side, which meet in the L2: 64 sequences of up to 8192 tokens,
 // 64 rows, 225 us with two of 32, 334 with four of 16; with one of 64 most of its values stand in scratch (1922).
-template <int D, int RB>
-__global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Cache c, const Attend a)
+//
+// The new tokens of a draft tree (FewRows) see of the places from qfirst on their own lines alone, and stand at the position of their depth.
+template <int D, int RB, typename A> __device__ __forceinline__ void attend(const Cache &c, const A &a)
 {
+    constexpr bool kTree = !__is_same(A, Attend);
     constexpr int KW = D / 64;                               // 16-byte pieces of a key that a lane reads
     constexpr int VW = D / 64;                               // dwords of a key's values that a lane reads
     constexpr int CB = D / 16;                               // blocks of 16 channels
@@ -90,15 +104,29 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Ca
     if (a.splits > 1 && split * kWaves * per >= st.count) return;          // (the join knows)
 
     // position of the first new token (a sequence of no length has no step)
-    const int32_t qfirst = max(c.lens[n], 0) - a.tokens;
+    const int32_t qfirst = kTree ? max(places(c, a, n) - a.tokens, 0) : max(c.lens[n], 0) - a.tokens;
     // rows of this tile: (token, head of the group)
     bf16x8 qf[RB][D / 32];
     int32_t qpos[RB], row[RB];
+    [[maybe_unused]] uint64_t line[RB];
+    [[maybe_unused]] bool there[RB];
+    [[maybe_unused]] uint64_t mine = 0;                      // lane's token's line
+    if constexpr (kTree) mine = tree_line(lane < a.tokens ? a.parents[(int64_t)n * a.tokens + lane] : -2, a.tokens);
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         row[r] = (tile * RB + r) * 16 + x;
         const int rr = row[r] < a.rows ? row[r] : a.rows - 1, t = rr / c.group, head = kv * c.group + rr - t * c.group;
-        qpos[r] = qfirst + t;
+        if constexpr (kTree) {
+            line[r] = (uint64_t)(uint32_t)__shfl((int)(mine >> 32), t) << 32 | (uint32_t)__shfl((int)mine, t);
+            there[r] = line[r] != 0;
+            const int32_t depth = __popcll(line[r]) - 1;
+            qpos[r] = qfirst + depth;
+            if (a.window && a.window < kTreeTokens)
+                for (int j = 0; j < a.tokens; ++j) {
+                    const int32_t dj = __popcll((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)mine, j)) - 1;
+                    if (depth - dj >= a.window && qfirst + dj >= a.sinks) line[r] &= ~(1ull << j);
+                }
+        } else qpos[r] = qfirst + t;
         const uint16_t *from = a.q + ((int64_t)n * a.tokens + t) * a.q_stride + (int64_t)head * D + D / 4 * g;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) qf[r][i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(from + 8 * i));
@@ -168,7 +196,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Ca
     auto work = [&](int32_t u, Codes &w) {
         const int32_t key0 = first_key(u);
         // some row does not see some key, or there is none
-        const bool edge = key0 + kStep - 1 > qfirst || (a.window && qfirst + a.tokens - 1 - key0 >= a.window) || w.page[0] < 0 || w.page[1] < 0;
+        const bool edge = key0 + kStep - 1 + (kTree ? 1 : 0) > qfirst || (a.window && qfirst + a.tokens - 1 - key0 >= a.window) || w.page[0] < 0 || w.page[1] < 0;
         // logits of all rows, then their terms, then the values: K's and V's widened codes are not held at once
         f32x4 s[RB][2];
 #pragma unroll
@@ -197,7 +225,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Ca
                     const bool none = w.page[b] < 0 || key >= st.len;
 #pragma unroll
                     for (int r = 0; r < RB; ++r) {
-                        const bool ok = !none && key <= qpos[r] && (a.window == 0 || qpos[r] - key < a.window || key < a.sinks);
+                        const bool near = a.window == 0 || qpos[r] - key < a.window || key < a.sinks;
+                        bool ok;
+                        if constexpr (kTree) ok = !none && there[r] && (key < qfirst ? near : (line[r] >> ((key - qfirst) & 63)) & 1);
+                        else ok = !none && key <= qpos[r] && near;
                         s[r][b][i] = ok ? s[r][b][i] : -kInf;
                         seen[r] |= (ok ? 1u : 0u) << (4 * b + i);
                     }
@@ -314,6 +345,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Ca
         }
     }
 
+    if constexpr (kTree) {
+        // (rows of nobody, whatever steps that every row sees whole have left in them)
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+            if (!there[r]) {
+                m[r] = -kInf;
+                l[r] = 0.f;
+#pragma unroll
+                for (int j = 0; j < CB; ++j) acc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+    }
+
     // ---- the four waves' parts: a row's maximum, sum and numerators' sums ----
     constexpr int kPitch = D + 4;
     extern __shared__ __align__(16) float lds[];             // [2][16 RB][D + 4] and [2][16 RB][2]
@@ -392,13 +435,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Ca
     }
 }
 
+template <int D, int RB> __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_attn_kernel(const Cache c, const Attend a) { attend<D, RB>(c, a); }
+template <int D, int RB> __global__ __launch_bounds__(64 * kWaves, 2) void kda_cache_few_kernel(const Cache c, const FewRows a) { attend<D, RB>(c, a); }
+
 // parts of a sequence and head that hold something
-__device__ __forceinline__ int32_t used_parts(const Cache &c, const Attend &a, int n)
+template <typename A> __device__ __forceinline__ int32_t parts_of(const Cache &c, const A &a, int n)
 {
     const Steps st = steps_of(c, a, n);
     const int32_t per = wave_steps(st, a.splits) * kWaves;
     return per ? (st.count + per - 1) / per : 0;
 }
+__device__ __forceinline__ int32_t used_parts(const Cache &c, const Attend &a, int n) { return parts_of(c, a, n); }
+__device__ __forceinline__ int32_t used_parts(const Cache &c, const FewRows &a, int n) { return parts_of(c, a, n); }
 
 }  // namespace cache
 }  // namespace kda
@@ -423,15 +471,25 @@ int32_t cache_attn_splits(const Cache &c, int64_t pairs, int64_t most_keys, int6
 }
 
 namespace {
-template <int D, int RB> hipError_t launch(const Cache &c, const Attend &a, hipStream_t st)
+template <int D, int RB> void launch_rows(const Cache &c, const Attend &a, dim3 grid, size_t lds, hipStream_t st)
+{
+    hipLaunchKernelGGL((kda_cache_attn_kernel<D, RB>), grid, dim3(64 * kWaves), lds, st, c, a);
+}
+template <int D, int RB> void launch_rows(const Cache &c, const FewRows &a, dim3 grid, size_t lds, hipStream_t st)
+{
+    hipLaunchKernelGGL((kda_cache_few_kernel<D, RB>), grid, dim3(64 * kWaves), lds, st, c, a);
+}
+template <int D, int RB, typename A> hipError_t launch(const Cache &c, const A &a, hipStream_t st)
 {
     const uint32_t grid = (uint32_t)c.num_seqs * c.heads_kv * a.row_tiles * a.splits;
-    hipLaunchKernelGGL((kda_cache_attn_kernel<D, RB>), dim3(grid), dim3(64 * kWaves), 2 * 16 * RB * (D + 4 + 2) * 4, st, c, a);
+    launch_rows<D, RB>(c, a, dim3(grid), 2 * 16 * RB * (D + 4 + 2) * 4, st);
     return hipGetLastError();
 }
-template <int D> hipError_t launch(const Cache &c, Attend a, hipStream_t st)
+template <int D, typename A> hipError_t launch(const Cache &c, const A &a, hipStream_t st)
 {
-    hipError_t e = a.row_tiles == 1 && a.rows <= 16 ? launch<D, 1>(c, a, st) : launch<D, 2>(c, a, st);
+    hipError_t e;
+    if constexpr (__is_same(A, FewRows) && D == 128) e = launch<D, 1>(c, a, st);           // (cache_few_rows)
+    else e = a.row_tiles == 1 && a.rows <= 16 ? launch<D, 1>(c, a, st) : launch<D, 2>(c, a, st);
     if (e == hipSuccess && a.splits > 1) {
         const int64_t items = (int64_t)c.num_seqs * c.heads_kv * a.rows;
         e = launch_join<D>(c, a, items, st);
@@ -444,6 +502,19 @@ kda_status cache_attn_dispatch(const Cache &c, const Attend &a, int dim, hipStre
 {
     const hipError_t e = dim == 128 ? launch<128>(c, a, st) : launch<64>(c, a, st);
     return e == hipSuccess ? KDA_OK : fail(KDA_ERR_LAUNCH, "kda_cache_attn: %s", hipGetErrorString(e));
+}
+
+// Rows of a key head up to which a draft tree's tokens come here, where keys go from memory to registers, and not to tiles that waves share through LDS
+// (kda_cache_tree.hip).  us here / there: heads of 64, 32 rows, 64 sequences of up to 8 000 tokens 83 / 124, one of 2 000 11.8 / 11.5, one of 300 8.4 / 11.0; heads of
+// 128, 16 rows, the same 155 / 165, 11.9 / 12.6 and 7.8 / 11.8, but 32 rows 173 / 165, 14.5 / 12.8 and 10.9 / 12.0.
+int32_t cache_few_rows(int dim) { return dim == 64 ? 32 : 16; }
+
+kda_status cache_few_dispatch(const Cache &c, const TreeAttend &tree, int dim, hipStream_t st)
+{
+    FewRows a;
+    static_cast<TreeAttend &>(a) = tree;
+    const hipError_t e = dim == 128 ? launch<128>(c, a, st) : launch<64>(c, a, st);
+    return e == hipSuccess ? KDA_OK : fail(KDA_ERR_LAUNCH, "kda_cache_tree_attn: %s", hipGetErrorString(e));
 }
 
 }  // namespace kda

@@ -13,6 +13,13 @@ def test_tree_kernels_keep_their_waves(resources):  # noqa: F811
         assert r["Occupancy [waves/SIMD]"] >= (3 if "Li16E" in name or "commit" in name else 2), (name, r)
 
 
+def test_kernels_of_few_rows_are_the_cache_attention_s(resources):  # noqa: F811
+    few = _kernels(resources, "kda_cache_few_kernel")
+    assert len(few) == 3                                     # heads of 64 with 16 and 32 rows, of 128 with 16
+    for name, r in few.items():
+        assert r["Occupancy [waves/SIMD]"] >= 2 and r["VGPRs Spill"] == 0, (name, r)
+
+
 def test_moving_and_turning_kernels_use_no_scratch(resources):  # noqa: F811
     some = {}
     for n in ("kda_rotate_kernel", "kda_cache_copy_kernel", "kda_cache_keep_kernel", "kda_pages_"):

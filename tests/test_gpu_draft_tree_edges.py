@@ -236,3 +236,29 @@ def test_compaction_of_counts_below_zero_stays_inside():
     table = int32([[0, 3, 6, 7]])
     moves = kda.kda_pages_compact(table, refs)
     assert table.tolist() == [[0, 3, 1, 2]] and moves.tolist() == [[6, 1], [7, 2], [-1, -1], [-1, -1]] and refs.tolist()[:4] == [1, 1, 1, 2]
+
+
+@pytest.mark.parametrize("d,T,Hq,Hk", [(64, 8, 8, 2), (64, 32, 2, 2), (64, 33, 2, 2), (128, 16, 2, 2), (128, 17, 2, 2), (128, 4, 8, 2), (64, 3, 8, 1), (128, 5, 5, 1), (64, 1, 64, 1)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (40, 4), (3, 2)])
+def test_few_rows_a_key_head(d, T, Hq, Hk, window, sinks):
+    """Either side of where a tree's rows go to the kernel without tiles: masks, codes that are no numbers behind the last token, pages that are not
+    there, skipped sequences, long ones that are split."""
+    lens = [0, 15, 16, 33, 700, 3000, -1, 64]
+    N = len(lens)
+    pool = Pool(N, Hk, d, 16, 3000 + T, d + T, nan_behind=[max(0, n) + T for n in lens])
+    pool.table[4, 9] = -1
+    q, parents = _tokens(N, T, Hq, d, 3), random_trees(N, T, 4, T, max(1, T // 2), roots=True)
+    for out_dtype in (torch.float32, torch.bfloat16):
+        got = _attend(pool, q, lens, parents, window, sinks, out_dtype)
+        _within(got, *_attend_refs(pool, q, lens, parents, window, sinks), out_dtype)
+    # a value that is not a number, of the context and of the tree
+    n, held = 5, 3000
+    for slot in (held - 2, held):
+        page, at = pool.table[n, slot // 16], slot % 16
+        was = pool.v[page, 0, at, 7]
+        pool.v[page, 0, at, 7] = 0x7F
+        got = np.isnan(_np(_attend(pool, q, lens, parents, window, sinks))[n])
+        pool.v[page, 0, at, 7] = was
+        want = np.zeros(got.shape, bool)
+        want[dt.tree_mask(parents[n], held, window, sinks)[:, slot], :Hq // Hk, 7] = True
+        assert np.array_equal(got, want)
