@@ -80,17 +80,20 @@ __device__ __forceinline__ f32x4 mfma16(const f32x4 &a, const f32x4 &b, f32x4 ac
 }
 
 // LDS: decays of the tokens in fp32, then their k and q as they came, [TM][D + 4] each; in the same place P_i0 k_i and scale P_i0 q_i in fp32; and then the two
-// matrices of sums over channels, [TM][TM + 4] each.  Behind them the lines.
+// matrices of sums over channels, [TM][TM + 4] each.  Behind them the lines, and v and beta.
 template <typename Tin, int D, int TM> struct StepLds {
     static constexpr int kPitch = D + 4, kSumPitch = TM + 4;
     static constexpr int kRows = TM * kPitch;
     static constexpr int kTokens = kRows * (4 + 2 * (int)sizeof(Tin)), kProducts = 2 * kRows * 4, kSums = 2 * TM * kSumPitch * 4;
     static constexpr int kMost = kTokens > kProducts ? kTokens : kProducts, kLines = kMost > kSums ? kMost : kSums;
-    static constexpr int kBytes = kLines + kTreeTokens * 8;
+    // (values and betas of trees of up to 32 tokens; a large tree's would leave one workgroup a compute unit)
+    static constexpr bool kHasValues = TM < 64;
+    static constexpr int kValues = kLines + kTreeTokens * 8, kBetas = kValues + (kHasValues ? kRows * (int)sizeof(Tin) : 0);
+    static constexpr int kBytes = kBetas + (kHasValues ? TM * 4 : 0);
 };
 
 template <typename Tin, int D, int TM>
-__global__ __launch_bounds__(2 * D, 2) void kda_tree_steps_kernel(const Tree a)
+__global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel(const Tree a)
 {
     using L = StepLds<Tin, D, TM>;
     constexpr int kThreads = 2 * D, kGroups = D / 8, kNodes = TM / kGroups > 0 ? TM / kGroups : 1;      // groups of 16 lanes; tokens of one
@@ -100,6 +103,8 @@ __global__ __launch_bounds__(2 * D, 2) void kda_tree_steps_kernel(const Tree a)
     float *al = reinterpret_cast<float *>(lds);
     Tin *kk = reinterpret_cast<Tin *>(al + L::kRows), *qq = kk + L::kRows;
     uint64_t *lines = reinterpret_cast<uint64_t *>(lds + L::kLines);
+    [[maybe_unused]] Tin *vs = reinterpret_cast<Tin *>(lds + L::kValues);
+    [[maybe_unused]] float *betas = reinterpret_cast<float *>(lds + L::kBetas);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, x = lane & 15, g = lane >> 4;
     const int64_t n = blockIdx.x / a.heads;
     const int h = (int)(blockIdx.x - n * a.heads), T = a.tokens;
@@ -133,19 +138,16 @@ __global__ __launch_bounds__(2 * D, 2) void kda_tree_steps_kernel(const Tree a)
             else lv[r] = *reinterpret_cast<const Four<Tin> *>(la + row * D + c);
         }
     }
-    f32x2 vv[MT][4];
-    float beta[MT][4];
-    auto values = [&]() {
+    [[maybe_unused]] Four<Tin> values[kPieces];
+    [[maybe_unused]] float own_beta = 0.f;
+    if constexpr (L::kHasValues) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t row = row0 + (int64_t)min(16 * m + 4 * g + e, T - 1) * a.heads;
-                vv[m][e] = load2(static_cast<const Tin *>(a.v) + row * D + col);
-                beta[m][e] = load_as_float(static_cast<const Tin *>(a.beta) + row);
-            }
-    };
-    if constexpr (MT < 4) values();                          // (a large tree's wait until there are registers for them)
+        for (int r = 0; r < kPieces; ++r) {
+            const int t = min((tid + kThreads * r) / (D / 4), T - 1), c = 4 * (tid % (D / 4));
+            values[r] = *reinterpret_cast<const Four<Tin> *>(static_cast<const Tin *>(a.v) + (row0 + (int64_t)t * a.heads) * D + c);
+        }
+        own_beta = load_as_float(static_cast<const Tin *>(a.beta) + row0 + (int64_t)min(tid, T - 1) * a.heads);
+    }
     // the state's rows 16 s + 4 g + i
     f32x2 s0[D / 16][4];
     {
@@ -169,7 +171,9 @@ __global__ __launch_bounds__(2 * D, 2) void kda_tree_steps_kernel(const Tree a)
         *reinterpret_cast<f32x4 *>(al + t * L::kPitch + c) = av;
         *reinterpret_cast<Four<Tin> *>(kk + t * L::kPitch + c) = there ? kv[r] : Four<Tin>{};
         *reinterpret_cast<Four<Tin> *>(qq + t * L::kPitch + c) = there ? qv[r] : Four<Tin>{};
+        if constexpr (L::kHasValues) *reinterpret_cast<Four<Tin> *>(vs + t * L::kPitch + c) = values[r];
     }
+    if (L::kHasValues && tid < TM) betas[tid] = own_beta;
     __syncthreads();
 
     // ---- up every token's line: the sums over channels, column j with lane j % 16, and the product of all decays ----
@@ -196,7 +200,7 @@ __global__ __launch_bounds__(2 * D, 2) void kda_tree_steps_kernel(const Tree a)
             channels(kk, t, kt);
             channels(qq, t, qt);
             line = lines[t];
-            if (line) b = load_as_float(static_cast<const Tin *>(a.beta) + row0 + (int64_t)t * a.heads);
+            if (line) b = L::kHasValues ? betas[t] : load_as_float(static_cast<const Tin *>(a.beta) + row0 + (int64_t)t * a.heads);
         }
         while (line) {
             const int j = 63 - __builtin_clzll(line);
@@ -255,7 +259,19 @@ __global__ __launch_bounds__(2 * D, 2) void kda_tree_steps_kernel(const Tree a)
     __syncthreads();
 
     // ---- their products with S_0: tokens 16 m + 4 g + e ----
-    if constexpr (MT == 4) values();
+    // (what of v and beta is not in LDS is asked for now that there are registers for it)
+    f32x2 vv[MT][4];
+    float beta[MT][4];
+    if constexpr (!L::kHasValues) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t row = row0 + (int64_t)min(16 * m + 4 * g + e, T - 1) * a.heads;
+                vv[m][e] = load2(static_cast<const Tin *>(a.v) + row * D + col);
+                beta[m][e] = load_as_float(static_cast<const Tin *>(a.beta) + row);
+            }
+    }
     f32x4 acc[2][MT][2];
 #pragma unroll
     for (int w = 0; w < 2; ++w)
@@ -285,6 +301,15 @@ __global__ __launch_bounds__(2 * D, 2) void kda_tree_steps_kernel(const Tree a)
             sk[t * L::kSumPitch + 16 * c + x] = nk[r][c];
             sq[t * L::kSumPitch + 16 * c + x] = nq[r][c];
         }
+    }
+    if constexpr (L::kHasValues) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                vv[m][e] = load2(vs + (16 * m + 4 * g + e) * L::kPitch + col);
+                beta[m][e] = betas[16 * m + 4 * g + e];
+            }
     }
     // r, but for what is not finite, which the descendants of its token see and no others
     uint32_t odd = 0;
