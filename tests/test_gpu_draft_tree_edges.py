@@ -262,3 +262,61 @@ def test_few_rows_a_key_head(d, T, Hq, Hk, window, sinks):
         want = np.zeros(got.shape, bool)
         want[dt.tree_mask(parents[n], held, window, sinks)[:, slot], :Hq // Hk, 7] = True
         assert np.array_equal(got, want)
+
+
+KINDS = [(64, 16, 4, 2), (64, 40, 4, 1), (128, 8, 2, 1), (128, 20, 2, 2), (128, 40, 8, 2), (128, 64, 4, 1)]        # few rows, 64 and 128 a workgroup
+
+
+@pytest.mark.parametrize("d,T,Hq,Hk", KINDS)
+def test_scales_of_any_size_whichever_the_kernel(d, T, Hq, Hk):
+    """Scales that are no powers of two, that differ from page to page, that are negative, large, small or zero: exact in fp32, and finite where the
+    result is."""
+    held = [500, 40]
+    pool = Pool(2, Hk, d, 16, 500 + T, d + T)
+    g = np.random.default_rng(3)
+    ks, vs = pool.ks.copy(), pool.vs.copy()
+    q, parents = _tokens(2, T, Hq, d, 3), random_trees(2, T, 4, 5)
+    for kind in range(6):
+        pool.ks, pool.vs = ks.copy(), vs.copy()
+        if kind == 0:
+            pool.ks = np.float32(ks * g.uniform(0.5, 2, ks.shape))
+        elif kind == 1:
+            pool.vs = np.float32(vs * g.uniform(-2, 2, vs.shape))
+        elif kind == 2:
+            pool.vs = np.float32(vs * 2.0 ** 100)
+        elif kind == 3:
+            pool.vs = np.float32(vs * 2.0 ** -70)
+        elif kind == 4:
+            pool.vs = np.float32(np.where(g.random(vs.shape) < 0.5, 2.0 ** 118, 2.0 ** 90))
+        else:
+            pool.ks[::2], pool.vs[1::3] = 0, 0
+        got = _attend(pool, q, held, parents)
+        assert bool(torch.isfinite(got).all())
+        _within(got, *_attend_refs(pool, q, held, parents), torch.float32)
+
+
+@pytest.mark.parametrize("d,T,Hq,Hk", KINDS)
+def test_rows_that_see_nothing_and_other_sequences_pages(d, T, Hq, Hk):
+    """A window with no page under it; and pages that no row sees, whose scales and codes are no numbers."""
+    pool = Pool(2, Hk, d, 16, 700 + T, 9)
+    q, parents = _tokens(2, T, Hq, d, 3), random_trees(2, T, 3, 1)
+    pool.table[0, :] = -1
+    before = 600 // 16 - 3
+    for p in pool.table[1, :before]:                         # (behind every row's window)
+        pool.k[p], pool.v[p] = 0x7F, 0xFF
+        pool.ks[p] = pool.vs[p] = math.nan
+    got = _attend(pool, q, [600, 600], parents, 20, 0)
+    assert not bool(got[0].any())
+    _within(got, *_attend_refs(pool, q, [600, 600], parents, 20, 0), torch.float32)
+
+
+@pytest.mark.parametrize("d,T,Hq,Hk", KINDS)
+def test_scales_at_float32_s_edge_in_the_keys(d, T, Hq, Hk):
+    """Keys' scales of 2^80 with a scale of 2^-91 for the logits, and the other way round: what is multiplied first does not matter."""
+    pool = Pool(1, Hk, d, 32, 300 + T, 9)
+    q, parents = _tokens(1, T, Hq, d, 3), random_trees(1, T, 4, 5)
+    for up in (80, -80):                                     # (the logits' scale has to be within 1e-30 to 1e30)
+        pool.ks[:] = np.float32(2.0 ** up)
+        scale = 2.0 ** (-up - 11)
+        got = _attend(pool, q, [300], parents, scale=scale)
+        _within(got, *_attend_refs(pool, q, [300], parents, scale=scale), torch.float32)
