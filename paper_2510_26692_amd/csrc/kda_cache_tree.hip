@@ -94,7 +94,7 @@ template <int D> struct Lds {
     static constexpr int kBytes = kLine + 512;
 };
 
-// The sequence that workgroup `place` of the sequences takes.  Two workgroups share a compute unit, and those that a launch begins with are handed out
+// The sequence that workgroup `place` of the sequences takes.  Two workgroups or three share a compute unit, and those that a launch begins with are handed out
 // round by round: in the first round the longest sequences, in falling order, in the second the next in rising order, and so on, the sums even
 // out (64 trees of 32 tokens over 4 096 to 8 192 tokens, 8 heads: 266 us, as they come 285).
 constexpr int kOrdered = 256;        // sequences that are ranked
@@ -420,8 +420,9 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
     return again;
 }
 template <int D, int WR> __device__ __noinline__ void tree_tile_again(const Cache c, const TreeAttend a) { tree_tile<D, WR, true>(c, a); }
+// (of heads of 64, three on a compute unit, as cache_tree_splits counts on)
 template <int D, int WR>
-__global__ __launch_bounds__(256, 2) void kda_cache_tree_kernel(const Cache c, const TreeAttend a)
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void kda_cache_tree_kernel(const Cache c, const TreeAttend a)
 {
     if (!tree_tile<D, WR, false>(c, a)) return;
     __syncthreads();                                         // (LDS is read to the end)
@@ -441,12 +442,15 @@ int32_t cache_tree_tile_rows(int32_t rows) { return rows <= 64 ? 64 : 128; }
 // Workgroups of a tile of rows: enough for two on every compute unit, or one where that leaves each fewer than five tiles of keys, and each with two at
 // least; none is split where one a compute unit has at most 16.  us with two / one on every compute unit (16 tokens x 32 heads over 8): four sequences of 2 000
 // tokens 22.4 / 19.6, one of 16 000 22.5 / 21.6, 16 of 8 000 62 / 88; eight of 4 000 with trees of 32 36.3 / 38.7; 32 of 1 000 split in two / whole 34.3 / 27.8.
-int32_t cache_tree_splits(const Cache &, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
+// Of heads of 64, as many as three on every compute unit hold where each has 16 tiles at least.  us with two / three: four of up to 100 000 with trees of
+// 64 tokens 233 / 214, 16 of 8 000 with 64 rows 47 / 43, but eight of 4 000 with 32 28.5 / 33, and, in more than one round, 64 of 8 000 178 / 220.
+int32_t cache_tree_splits(int dim, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
 {
     int64_t keys = most_keys;
     if (window && window + tokens + sinks + 2 * kKeys < keys) keys = window + tokens + sinks + 2 * kKeys;
     const int64_t steps = (keys + kKeys - 1) / kKeys, most = (steps + 1) / 2, all = tiles > 0 ? tiles : 1;
     int64_t n = (512 + all - 1) / all;
+    if (dim == 64 && 768 / all > n && steps >= 16 * (768 / all)) n = 768 / all;
     if (steps < 5 * n) n = (256 + all - 1) / all;
     if (all >= 256 && steps <= 16) n = 1;
     n = n < most ? n : most;
