@@ -439,9 +439,11 @@ namespace kda {
 
 int32_t cache_tree_tile_rows(int32_t rows) { return rows <= 64 ? 64 : 128; }
 
-// Workgroups of a tile of rows: enough for two on every compute unit, or one where that leaves each fewer than five tiles of keys, and each with two at
+// Workgroups of a tile of rows: as many as two on every compute unit hold, or one where that leaves each fewer than five tiles of keys, and each with two at
 // least; none is split where one a compute unit has at most 16.  us with two / one on every compute unit (16 tokens x 32 heads over 8): four sequences of 2 000
 // tokens 22.4 / 19.6, one of 16 000 22.5 / 21.6, 16 of 8 000 62 / 88; eight of 4 000 with trees of 32 36.3 / 38.7; 32 of 1 000 split in two / whole 34.3 / 27.8.
+// A few more than they hold would leave a second round to a few of them: with the count rounded up / down, trees of 32 tokens, five sequences of 2 000 29.5 / 25.8,
+// seven of 16 000 90 / 79, 20 of 4 000 82 / 70, 48 of 2 000 111 / 65.
 // Of heads of 64, as many as three on every compute unit hold where each has 16 tiles at least.  us with two / three: four of up to 100 000 with trees of
 // 64 tokens 233 / 214, 16 of 8 000 with 64 rows 47 / 43, but eight of 4 000 with 32 28.5 / 33, and, in more than one round, 64 of 8 000 178 / 220.
 int32_t cache_tree_splits(int dim, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
@@ -449,9 +451,9 @@ int32_t cache_tree_splits(int dim, int64_t tiles, int64_t most_keys, int64_t win
     int64_t keys = most_keys;
     if (window && window + tokens + sinks + 2 * kKeys < keys) keys = window + tokens + sinks + 2 * kKeys;
     const int64_t steps = (keys + kKeys - 1) / kKeys, most = (steps + 1) / 2, all = tiles > 0 ? tiles : 1;
-    int64_t n = (512 + all - 1) / all;
+    int64_t n = all < 512 ? 512 / all : 1;
     if (dim == 64 && 768 / all > n && steps >= 16 * (768 / all)) n = 768 / all;
-    if (steps < 5 * n) n = (256 + all - 1) / all;
+    if (steps < 5 * n) n = all < 256 ? 256 / all : 1;
     if (all >= 256 && steps <= 16) n = 1;
     n = n < most ? n : most;
     return (int32_t)(n < 1 ? 1 : n);
