@@ -469,6 +469,18 @@ int32_t cache_attn_splits(const Cache &c, int64_t pairs, int64_t most_keys, int6
     const int64_t n = want < most ? want : most;
     return (int32_t)(n < 1 ? 1 : n);
 }
+// Of a tree's few rows; and where that would leave parts of more than 16 384 keys, parts of about 4 096 and up to 2 048 workgroups, as in
+// cache_tree_splits.  us without / with that, four new tokens, 32 heads over 8: 64 sequences of 32 000 583 / 579, one in 64 so long and the others of 500 to
+// 2 000 269 / 105, one in eight 392 / 190; 16 of 100 000 451 / 473, one in eight 311 / 131.
+int32_t cache_few_splits(const Cache &c, int64_t pairs, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
+{
+    const int64_t n = cache_attn_splits(c, pairs, most_keys, window, sinks, tokens);
+    int64_t keys = most_keys;
+    if (window && window + tokens + sinks + 2 * kStep < keys) keys = window + tokens + sinks + 2 * kStep;
+    if (keys <= 16384 * n || 2048 / pairs <= n) return (int32_t)n;
+    const int64_t want = (keys + 4095) / 4096;
+    return (int32_t)(want < 2048 / pairs ? want : 2048 / pairs);
+}
 
 namespace {
 template <int D, int RB> void launch_rows(const Cache &c, const Attend &a, dim3 grid, size_t lds, hipStream_t st)

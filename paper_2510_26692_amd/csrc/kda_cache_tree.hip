@@ -446,6 +446,9 @@ int32_t cache_tree_tile_rows(int32_t rows) { return rows <= 64 ? 64 : 128; }
 // seven of 16 000 90 / 79, 20 of 4 000 82 / 70, 48 of 2 000 111 / 65.
 // Of heads of 64, as many as three on every compute unit hold where each has 16 tiles at least.  us with two / three: four of up to 100 000 with trees of
 // 64 tokens 233 / 214, 16 of 8 000 with 64 rows 47 / 43, but eight of 4 000 with 32 28.5 / 33, and, in more than one round, 64 of 8 000 178 / 220.
+// Where that would leave parts of more than 256 tiles, parts of about 64 and up to 2 048 workgroups: of a batch one sequence may be long and the others not, which
+// only the device knows.  us for 64 sequences of 32 000 / one of them in 64, the others of 500 to 2 000: in 512 workgroups 994 / 784, in 2 048 1 060 / 276; 36 of
+// 50 000, one in eight so long, 1 224 / 305; eight of 65 000 to 131 072 with trees of 64 1 058 / 1 005.
 int32_t cache_tree_splits(int dim, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
 {
     int64_t keys = most_keys;
@@ -455,6 +458,7 @@ int32_t cache_tree_splits(int dim, int64_t tiles, int64_t most_keys, int64_t win
     if (dim == 64 && 768 / all > n && steps >= 16 * (768 / all)) n = 768 / all;
     if (steps < 5 * n) n = all < 256 ? 256 / all : 1;
     if (all >= 256 && steps <= 16) n = 1;
+    if (steps > 256 * n && 2048 / all > n) n = steps / 64 < 2048 / all ? steps / 64 : 2048 / all;
     n = n < most ? n : most;
     return (int32_t)(n < 1 ? 1 : n);
 }

@@ -320,3 +320,22 @@ def test_scales_at_float32_s_edge_in_the_keys(d, T, Hq, Hk):
         scale = 2.0 ** (-up - 11)
         got = _attend(pool, q, [300], parents, scale=scale)
         _within(got, *_attend_refs(pool, q, [300], parents, scale=scale), torch.float32)
+
+
+@pytest.mark.parametrize("d,T,Hq", [(128, 3, 8), (128, 20, 8), (64, 40, 8), (128, 35, 16), (64, 5, 16)])
+def test_one_long_sequence_of_a_batch(d, T, Hq):
+    """Of 64 sequences one is of 17 000 tokens and walked in parts, with the others' few pages walked in the same launch."""
+    N, Hk, page, long = 64, 8, 128, 17000
+    pool = Pool(N, Hk, d, page, 256, T)
+    g = np.random.default_rng(T)
+    held = g.integers(0, 256 - T, N)
+    held[[3, 40]] = -1, 0
+    wide = np.full((N, (long + T + page - 1) // page), -1, pool.table.dtype)
+    wide[:, :pool.table.shape[1]] = pool.table
+    wide[17] = g.integers(0, pool.P, wide.shape[1])          # (read only, so the pages may be others' too)
+    held[17] = long
+    pool.table = wide
+    q, parents = _tokens(N, T, Hq, d, 3), random_trees(N, T, 4, T, (T + 1) // 2)
+    got = _attend(pool, q, held, parents, max_kv_len=long + T)
+    _within(got, *_attend_refs(pool, q, held, parents), torch.float32)
+    assert torch.equal(got, _attend(pool, q, held, parents))
