@@ -11,8 +11,8 @@
 // ahead of that.
 //
 // What bounds it is the products and, beside them, the exponentials and the rest of the softmax, which do not overlap on a SIMD (issued in turn by one wave
-// they take the same time): four sequences of up to 131 072 tokens, 8 key heads, trees of 64 tokens and 32 heads, in 533 us (830 TFLOP/s of visible pairs;
-// a library product of 8192^3 1 379), 64 of up to 8 192 with 20 to 32 tokens in 268.
+// they take the same time): four sequences of up to 131 072 tokens, 8 key heads, trees of 64 tokens and 32 heads, in 533 to 543 us (820 TFLOP/s of visible pairs;
+// a library product of 8192^3 1 379), 64 of up to 8 192 with 20 to 32 tokens in 268 to 280.
 //
 // A row's token sees what is held (by the window and sinks of its position, len + depth) and its line, a bit for each drafted token; both
 // become one word of bits a tile, made only for tiles that some row sees in part.

@@ -19,7 +19,7 @@
 // all of them fp32 MFMAs whose accumulators are the operands of the next, so u never leaves its registers.
 //
 // What bounds it is reading the states, and for large trees the fp32 matrix cores: 4 T dk dv operations a state of 4 dk dv bytes.  256 trees of up
-// to 16 tokens, 32 heads: 151 us (0.68 GB, 4.5 TB/s); 64 of 64 tokens: 169, the matrix cores 44 % busy.  (With a column a thread and a loop over
+// to 16 tokens, 32 heads: 136 us (0.68 GB, 5.0 TB/s); 64 of 64 tokens: 170, the matrix cores 44 % busy.  (With a column a thread and a loop over
 // each token's ancestors in place of the blocks: 231 and 474.)
 #include "kda_tree.h"
 
