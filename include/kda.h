@@ -623,7 +623,7 @@ kda_status kda_tree_commit(const kda_dims *dims, const void *k, const void *v, c
 /*
  * Rows of the table become copies of other rows, in place: row n what row source[n] was (source[n] == n or >= num_seqs: it stays), or
  * empty (-1) where source[n] < 0, which frees what it alone had.  Beams that are carried on, dropped or doubled, prompts that are shared,
- * and sequences that end.  page_refs follows.  num_seqs at most 8192.
+ * and sequences that end.  page_refs follows.  num_seqs at most 8192, max_pages below 2^24.
  */
 kda_status kda_pages_fork(int32_t *block_table, int32_t num_seqs, int32_t max_pages, int32_t *page_refs, int64_t num_pages,
                           const int32_t *source, void *hip_stream);
@@ -637,7 +637,7 @@ kda_status kda_pages_fork(int32_t *block_table, int32_t num_seqs, int32_t max_pa
  *               tokens, for kda_cache_copy_pages; else (-1, -1)
  *               (a page whose last reference goes is free from then on: the copies have to be made before anything else takes or writes it)
  *   missing     [1] int32, written: 0, or by how many pages the free ones fall short: then nothing else is changed, and copies are all (-1, -1)
- * num_seqs at most 8192, num_seqs * max_pages below 2^31.  workspace: kda_pages_reserve_workspace_size bytes, 256-byte aligned.
+ * num_seqs at most 8192, num_seqs * max_pages below 2^31 - 1024.  workspace: kda_pages_reserve_workspace_size bytes, 256-byte aligned.
  */
 size_t kda_pages_reserve_workspace_size(int32_t num_seqs, int32_t max_pages, int64_t num_pages);
 kda_status kda_pages_reserve(int32_t *block_table, int32_t num_seqs, int32_t max_pages, int32_t page_size, int32_t *page_refs, int64_t num_pages,

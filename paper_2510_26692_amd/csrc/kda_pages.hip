@@ -277,11 +277,14 @@ extern "C" kda_status kda_pages_fork(int32_t *block_table, int32_t num_seqs, int
     if (!source || !aligned(source, 4)) return fail(KDA_ERR_INVALID_ARG, "source is NULL or misaligned");
     // columns of a workgroup: up to half a cache line's, as far as its rows fit the LDS and 64 workgroups are left (128 sequences x 17 columns: 7.6 us
     // with 16 columns, 4.1 with one)
-    int32_t width = (max_pages + 63) / 64;
+    int64_t width = ((int64_t)max_pages + 63) / 64;
     width = width > kForkEntries / num_seqs ? kForkEntries / num_seqs : width;
     width = width > 16 ? 16 : width;
-    hipLaunchKernelGGL(kda_pages_fork_kernel, dim3((max_pages + width - 1) / width), dim3(256), (size_t)num_seqs * width * 4,
-                       static_cast<hipStream_t>(hip_stream), block_table, num_seqs, max_pages, width, page_refs, num_pages, source);
+    const int64_t blocks = (max_pages + width - 1) / width;
+    // (a launch has fewer than 2^32 threads)
+    if (blocks > 0xffffff) return fail(KDA_ERR_UNSUPPORTED, "more than 2^24 workgroups (max_pages %d)", max_pages);
+    hipLaunchKernelGGL(kda_pages_fork_kernel, dim3((uint32_t)blocks), dim3(256), (size_t)num_seqs * width * 4, static_cast<hipStream_t>(hip_stream),
+                       block_table, num_seqs, max_pages, (int32_t)width, page_refs, num_pages, source);
     return launched("kda_pages_fork");
 }
 
@@ -300,7 +303,8 @@ extern "C" kda_status kda_pages_reserve(int32_t *block_table, int32_t num_seqs, 
     if (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128)
         return fail(KDA_ERR_UNSUPPORTED, "page_size must be 16, 32, 64 or 128, got %d", page_size);
     if (num_seqs > kMaxRows) return fail(KDA_ERR_UNSUPPORTED, "at most %d sequences, got %d", kMaxRows, num_seqs);
-    if ((int64_t)num_seqs * max_pages > 0x7fffffffLL) return fail(KDA_ERR_UNSUPPORTED, "a table of 2^31 entries or more");
+    // (entries are counted in 32 bits, a workgroup's threads at a time)
+    if ((int64_t)num_seqs * max_pages >= 0x7fffffffLL - kThreads + 1) return fail(KDA_ERR_UNSUPPORTED, "a table of 2^31 - 1024 entries or more");
     if (!missing || (num_seqs && (!kv_lens || !new_lens || !copies))) return fail(KDA_ERR_INVALID_ARG, "kv_lens, new_lens, copies or missing is NULL");
     for (const void *p : {(const void *)kv_lens, (const void *)new_lens, (const void *)copies, (const void *)missing})
         if (!aligned(p, 4)) return fail(KDA_ERR_INVALID_ARG, "kv_lens, new_lens, copies or missing is misaligned");

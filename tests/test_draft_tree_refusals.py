@@ -168,3 +168,14 @@ def test_the_binding_refuses_what_is_not_on_a_device_or_of_another_kind():
         kda.kda_pages_reserve(i(2, 3).long(), i(2), i(2), i(5), 16)
     with pytest.raises(ValueError, match="device"):
         kda.kda_pages_compact(i(2, 3), i(5))
+
+
+def test_tables_too_large_for_a_launch_are_refused():
+    def reserve(n, cols):
+        return _lib().kda_pages_reserve(SOME, n, cols, 64, SOME, 10, SOME, SOME, SOME, SOME, SOME, ctypes.c_size_t(0), None)
+    # (one workgroup counts entries in steps of 1024, in 32 bits)
+    assert reserve(1, 2 ** 31 - 1) == UNSUPPORTED and reserve(1, 2 ** 31 - 1024) == UNSUPPORTED and reserve(8192, 262144) == UNSUPPORTED
+    assert reserve(1, 2 ** 31 - 1025) == WORKSPACE and reserve(8192, 262143) == WORKSPACE
+    fork = lambda n, cols: _lib().kda_pages_fork(SOME, n, cols, SOME, 10, SOME, None)
+    assert fork(1, 2 ** 31 - 1) == UNSUPPORTED and fork(8192, 1 << 24) == UNSUPPORTED and fork(1, 16 * (1 << 24) - 15) == UNSUPPORTED
+    assert kda.kda_last_error()
