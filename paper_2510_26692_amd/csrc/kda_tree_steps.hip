@@ -9,7 +9,10 @@
 //
 // so that S_0 is read once, whatever the tree, and no token's state is formed.  Products of decays are formed going up a line, one
 // multiplication a token and channel, never as the quotient of two long products.  Everything is fp32; the two products with S_0 are
-// 16x16x4 fp32 MFMAs.
+// 16x16x4 fp32 MFMAs for trees of up to 16 tokens.  For larger ones their factors are written as three bf16 each, x = h + m + l exactly, and six
+// products of those, the largest, are summed in fp32 by 16x16x32 MFMAs: what is left out is below 2^-22 of a term and of either sign, the result as near as
+// with fp32 MFMAs (1.6 10^-7 in the mean square, 2.0 with those), in 3/8 of their time.  (Pieces below 2^-126 may be lost: of states below 2^-110 that is more than
+// fp32's own steps.)  A large tree's q goes to the lanes that need it without LDS, so that two workgroups share a compute unit in fp32 too.
 //
 // A workgroup has one sequence and head, a wave 32 columns of its state, held in registers from the start.  The sums over channels make a lower
 // triangular matrix N = -beta (sum k P k), zero but at ancestors, whose 16x16 blocks take the u of one block of tokens to the next:
@@ -18,9 +21,10 @@
 //
 // all of them fp32 MFMAs whose accumulators are the operands of the next, so u never leaves its registers.
 //
-// What bounds it is reading the states, and for large trees the fp32 matrix cores: 4 T dk dv operations a state of 4 dk dv bytes.  256 trees of up
-// to 16 tokens, 32 heads: 136 us (0.68 GB, 5.0 TB/s); 64 of 64 tokens: 170, the matrix cores 44 % busy.  (With a column a thread and a loop over
-// each token's ancestors in place of the blocks: 231 and 474.)
+// What bounds it is reading the states, and for large trees what a workgroup does one after the other: lines, pieces, products, blocks.  256 trees of up
+// to 16 tokens, 32 heads: 136 us (0.68 GB, 5.0 TB/s); 64 of 64 tokens: 139, with fp32 MFMAs 170; in fp32 153, with those and q in LDS 271; 64 chains of 64: 274
+// and 320, 128 trees of 20 99 and 126.  (Pieces for trees of 16, too: the same time in bf16, 172 for 156 in fp32.  With a column a thread and a loop over each token's
+// ancestors in place of the blocks: 231 and 474.)
 #include "kda_tree.h"
 
 namespace kda {
@@ -28,6 +32,7 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct Tree {
     const void *q, *k, *v, *log_alpha, *beta;
@@ -72,6 +77,17 @@ template <int kCtrl> __device__ __forceinline__ float add_rotated(float v)
 __device__ __forceinline__ float over_sixteen(float v) { return add_rotated<0x121>(add_rotated<0x122>(add_rotated<0x124>(add_rotated<0x128>(v)))); }
 
 __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+// x = h + m + l in bf16, exactly: h what bf16's bits have of x, m and l the rest rounded, for two values each
+__device__ __forceinline__ void three_of(float x0, float x1, uint32_t &h, uint32_t &m, uint32_t &l)
+{
+    const uint32_t b0 = __float_as_uint(x0) & 0xffff0000u, b1 = __float_as_uint(x1) & 0xffff0000u;
+    h = b0 >> 16 | b1;
+    float r0 = x0 - __uint_as_float(b0), r1 = x1 - __uint_as_float(b1), m0, m1;
+    m = pack_bf16x2(r0, r1);
+    unpack_bf16x2(m, m0, m1);
+    l = pack_bf16x2(r0 - m0, r1 - m1);
+}
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ f32x4 mfma16(const f32x4 &a, const f32x4 &b, f32x4 acc)      // a 16 x 16 x 16 product: slot g of step i is index 4 g + i
 {
 #pragma unroll
@@ -79,12 +95,16 @@ __device__ __forceinline__ f32x4 mfma16(const f32x4 &a, const f32x4 &b, f32x4 ac
     return acc;
 }
 
-// LDS: decays of the tokens in fp32, then their k and q as they came, [TM][D + 4] each; in the same place P_i0 k_i and scale P_i0 q_i in fp32; and then the two
-// matrices of sums over channels, [TM][TM + 4] each.  Behind them the lines, and v and beta.
+// LDS: decays of the tokens in fp32, then their k and, of small trees, q as they came, [TM][D + 4] each; in the same place P_i0 k_i and scale P_i0 q_i in fp32, or of
+// larger trees their pieces; and then the two matrices of sums over channels, [TM][TM + 4] each.  Behind them the lines, and v and beta.
 template <typename Tin, int D, int TM> struct StepLds {
     static constexpr int kPitch = D + 4, kSumPitch = TM + 4;
     static constexpr int kRows = TM * kPitch;
-    static constexpr int kTokens = kRows * (4 + 2 * (int)sizeof(Tin)), kProducts = 2 * kRows * 4, kSums = 2 * TM * kSumPitch * 4;
+    // (the products with S_0 are of bf16 pieces: three planes of half the channels of P_i0 k_i, three of scale P_i0 q_i, [TM][D / 2 + 8] each)
+    static constexpr bool kPlanes = TM >= 32;
+    static constexpr int kPlanePitch = D / 2 + 8, kPlane = TM * kPlanePitch * 2;
+    static constexpr int kTokens = kRows * (4 + (kPlanes ? 1 : 2) * (int)sizeof(Tin)),
+                         kProducts = kPlanes ? 6 * kPlane : 2 * kRows * 4, kSums = 2 * TM * kSumPitch * 4;
     static constexpr int kMost = kTokens > kProducts ? kTokens : kProducts, kLines = kMost > kSums ? kMost : kSums;
     // (values and betas of trees of up to 32 tokens; a large tree's would leave one workgroup a compute unit)
     static constexpr bool kHasValues = TM < 64;
@@ -112,9 +132,9 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
     const int64_t state = a.indices ? a.indices[n] : n;
     const int col = 32 * wave + 2 * x;                       // the lane's columns are this and the next
     auto put = [&](int t, float lo, float hi) {
-        const int64_t at = (row0 + (int64_t)t * a.heads) * D + col;
-        if (a.out_bf16) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(a.o) + at) = pack_bf16x2(lo, hi);
-        else *reinterpret_cast<f32x2 *>(static_cast<float *>(a.o) + at) = f32x2{lo, hi};
+        const uint32_t at = (uint32_t)(t * a.heads) * D + col;           // (below 2^30)
+        if (a.out_bf16) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(a.o) + row0 * D + at) = pack_bf16x2(lo, hi);
+        else *reinterpret_cast<f32x2 *>(static_cast<float *>(a.o) + row0 * D + at) = f32x2{lo, hi};
     };
     if (state < 0) {
         for (int t = g; t < T; t += 4) put(t, 0.f, 0.f);
@@ -124,18 +144,34 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
     int32_t up = -2;
     if (wave == 0 && lane < T) up = a.parents[n * T + lane];
     constexpr int kPieces = TM * (D / 4) / kThreads;         // fours of a thread
-    Four<Tin> qv[kPieces], kv[kPieces], lv[kPieces];
+    const int group = tid >> 4;
+    auto own = [&](int i) { return L::kPlanes ? D / CH * i + 4 * x : CH * x + i; };      // a lane's channels in a group: four from here on
+    [[maybe_unused]] Four<Tin> queries[kNodes][CH / 4];      // of large trees, of the group's own tokens
+    [[maybe_unused]] Four<Tin> qv[kPieces];
+    Four<Tin> kv[kPieces], lv[kPieces];
     Tin lh[kPieces];
     {
         const Tin *q = static_cast<const Tin *>(a.q), *k = static_cast<const Tin *>(a.k), *la = static_cast<const Tin *>(a.log_alpha);
+        auto row_of = [&](int r) { return row0 + (int64_t)min((tid + kThreads * r) / (D / 4), T - 1) * a.heads; };
+        const int c = 4 * (tid % (D / 4));
 #pragma unroll
         for (int r = 0; r < kPieces; ++r) {
-            const int t = min((tid + kThreads * r) / (D / 4), T - 1), c = 4 * (tid % (D / 4));
-            const int64_t row = row0 + (int64_t)t * a.heads;
-            kv[r] = *reinterpret_cast<const Four<Tin> *>(k + row * D + c);
-            qv[r] = *reinterpret_cast<const Four<Tin> *>(q + row * D + c);
-            if (a.scalar_gate) lh[r] = la[row];
-            else lv[r] = *reinterpret_cast<const Four<Tin> *>(la + row * D + c);
+            kv[r] = *reinterpret_cast<const Four<Tin> *>(k + row_of(r) * D + c);
+            if constexpr (!L::kPlanes) qv[r] = *reinterpret_cast<const Four<Tin> *>(q + row_of(r) * D + c);
+        }
+        if (a.scalar_gate) {
+#pragma unroll
+            for (int r = 0; r < kPieces; ++r) lh[r] = la[row_of(r)];
+        } else {
+#pragma unroll
+            for (int r = 0; r < kPieces; ++r) lv[r] = *reinterpret_cast<const Four<Tin> *>(la + row_of(r) * D + c);
+        }
+        if constexpr (L::kPlanes) {
+#pragma unroll
+            for (int r = 0; r < kNodes; ++r)
+#pragma unroll
+                for (int i = 0; i < CH; i += 4)
+                    queries[r][i / 4] = *reinterpret_cast<const Four<Tin> *>(q + (row0 + (int64_t)min(group + kGroups * r, T - 1) * a.heads) * D + own(i));
         }
     }
     [[maybe_unused]] Four<Tin> values[kPieces];
@@ -170,22 +206,32 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
         for (int e = 0; e < 4; ++e) av[e] = there ? fast_exp2(av[e] * kLog2e) : 1.f;
         *reinterpret_cast<f32x4 *>(al + t * L::kPitch + c) = av;
         *reinterpret_cast<Four<Tin> *>(kk + t * L::kPitch + c) = there ? kv[r] : Four<Tin>{};
-        *reinterpret_cast<Four<Tin> *>(qq + t * L::kPitch + c) = there ? qv[r] : Four<Tin>{};
+        if constexpr (!L::kPlanes) *reinterpret_cast<Four<Tin> *>(qq + t * L::kPitch + c) = there ? qv[r] : Four<Tin>{};
         if constexpr (L::kHasValues) *reinterpret_cast<Four<Tin> *>(vs + t * L::kPitch + c) = values[r];
     }
     if (L::kHasValues && tid < TM) betas[tid] = own_beta;
     __syncthreads();
 
     // ---- up every token's line: the sums over channels, column j with lane j % 16, and the product of all decays ----
-    const int group = tid >> 4;
     float all[kNodes][CH], nk[kNodes][MT], nq[kNodes][MT];
     auto channels = [&](const auto *rows, int t, float (&v)[CH]) {
 #pragma unroll
         for (int i = 0; i < CH; i += 4) {
-            const f32x4 w = load4(rows + t * L::kPitch + CH * x + i);
+            const f32x4 w = load4(rows + t * L::kPitch + own(i));
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[i + e] = w[e];
         }
+    };
+    auto block_of = [](int r) constexpr { return (kGroups * r + kGroups - 1) / 16; };       // of a group's token r, and so of its ancestors the last
+    auto query = [&](int r, int t, float (&v)[CH]) {
+        if constexpr (!L::kPlanes) channels(qq, t, v);
+        else
+#pragma unroll
+            for (int i = 0; i < CH; i += 4) {
+                const f32x4 w = widened(queries[r][i / 4]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[i + e] = lines[t] ? w[e] : 0.f;
+            }
     };
 #pragma unroll
     for (int r = 0; r < kNodes; ++r) {
@@ -198,7 +244,7 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
         float b = 0.f, kt[CH], qt[CH];
         if (t < TM) {
             channels(kk, t, kt);
-            channels(qq, t, qt);
+            query(r, t, qt);
             line = lines[t];
             if (line) b = L::kHasValues ? betas[t] : load_as_float(static_cast<const Tin *>(a.beta) + row0 + (int64_t)t * a.heads);
         }
@@ -222,6 +268,7 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
             dq = finite(dq) ? dq : 0.f;
 #pragma unroll
             for (int c = 0; c < MT; ++c) {
+                if (c > block_of(r)) continue;
                 const bool here = x == (j & 15) && c == j >> 4;
                 nk[r][c] = here ? dk : nk[r][c];
                 nq[r][c] = here ? dq : nq[r][c];
@@ -229,9 +276,99 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
         }
     }
     __syncthreads();
-    // ---- P_i0 k_i and scale P_i0 q_i, where the tokens stood ----
-    float *pk = reinterpret_cast<float *>(lds), *pq = pk + L::kRows;
-    {
+    f32x2 vv[MT][4];
+    float beta[MT][4];
+    // (what of v and beta is not in LDS is asked for when there are registers for it)
+    auto ask = [&]() {
+        if constexpr (!L::kHasValues) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t row = row0 + (int64_t)min(16 * m + 4 * g + e, T - 1) * a.heads;
+                    vv[m][e] = load2(static_cast<const Tin *>(a.v) + row * D + col);
+                    beta[m][e] = load_as_float(static_cast<const Tin *>(a.beta) + row);
+                }
+        }
+    };
+    f32x4 acc[2][MT][2];
+    // ---- P_i0 k_i and scale P_i0 q_i, where the tokens stood, and their products with S_0: tokens 16 m + 4 g + e ----
+    if constexpr (L::kPlanes) {
+        float kt[kNodes][CH], qt[kNodes][CH];
+#pragma unroll
+        for (int r = 0; r < kNodes; ++r) {
+            const int t = group + kGroups * r;
+            channels(kk, t, kt[r]);
+            query(r, t, qt[r]);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                kt[r][i] *= all[r][i];
+                qt[r][i] *= all[r][i] * a.scale;
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[w][m][0] = acc[w][m][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // a pass has half of the channels; channel 32 s + 16 i + 4 g + e of it stands at 32 s + 8 g + 4 i + e
+        const int at = 32 * (D == 128 ? x >> 3 : 0) + 8 * (x & 3) + 4 * ((x >> 2) & 1);
+#pragma unroll
+        for (int pass = 0; pass < 2; ++pass) {
+            __syncthreads();
+            if (D == 128 || x >> 3 == pass)
+#pragma unroll
+                for (int r = 0; r < kNodes; ++r)
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const float *from = (w ? qt[r] : kt[r]) + (D == 128 ? 4 * pass : 0);
+                        uint32_t p[2][3];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) three_of(from[2 * i], from[2 * i + 1], p[i][0], p[i][1], p[i][2]);
+#pragma unroll
+                        for (int i = 0; i < 3; ++i)
+                            *reinterpret_cast<u32x2 *>(lds + (3 * w + i) * L::kPlane + 2 * ((group + kGroups * r) * L::kPlanePitch + at)) = u32x2{p[0][i], p[1][i]};
+                    }
+            __syncthreads();
+#pragma unroll
+            for (int s = 0; s < D / 64; ++s) {
+                bf16x8 b[2][3];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    u32x4 p[3];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x2 *of = s0[D / 32 * pass + 2 * s + i / 2] + 2 * (i % 2);
+                        uint32_t hi, mid, lo;
+                        three_of(of[0][j], of[1][j], hi, mid, lo);
+                        p[0][i] = hi;
+                        p[1][i] = mid;
+                        p[2][i] = lo;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) b[j][i] = __builtin_bit_cast(bf16x8, p[i]);
+                }
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        if (16 * m >= T) continue;
+                        bf16x8 r[3];
+#pragma unroll
+                        for (int i = 0; i < 3; ++i)
+                            r[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(lds + (3 * w + i) * L::kPlane + 2 * ((16 * m + x) * L::kPlanePitch + 32 * s + 8 * g)));
+                        // small ones first; what is left out is below 2^-22 of a product
+#pragma unroll
+                        for (int i = 2; i >= 0; --i)
+#pragma unroll
+                            for (int k = 0; k <= i; ++k)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) acc[w][m][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[k], b[j][i - k], acc[w][m][j], 0, 0, 0);
+                    }
+                if (pass == 1 && s == 0) ask();
+            }
+        }
+    } else {
+        float *pk = reinterpret_cast<float *>(lds), *pq = pk + L::kRows;
         float kt[kNodes][CH], qt[kNodes][CH];
 #pragma unroll
         for (int r = 0; r < kNodes; ++r) {
@@ -255,40 +392,24 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
                 *reinterpret_cast<f32x4 *>(pq + t * L::kPitch + CH * x + i) = f32x4{qt[r][i], qt[r][i + 1], qt[r][i + 2], qt[r][i + 3]};
             }
         }
-    }
-    __syncthreads();
-
-    // ---- their products with S_0: tokens 16 m + 4 g + e ----
-    // (what of v and beta is not in LDS is asked for now that there are registers for it)
-    f32x2 vv[MT][4];
-    float beta[MT][4];
-    if constexpr (!L::kHasValues) {
+        __syncthreads();
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int w = 0; w < 2; ++w)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t row = row0 + (int64_t)min(16 * m + 4 * g + e, T - 1) * a.heads;
-                vv[m][e] = load2(static_cast<const Tin *>(a.v) + row * D + col);
-                beta[m][e] = load_as_float(static_cast<const Tin *>(a.beta) + row);
+            for (int m = 0; m < MT; ++m) {
+                acc[w][m][0] = acc[w][m][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (16 * m >= T) continue;
+                const float *rows = (w ? pq : pk) + (16 * m + x) * L::kPitch + 4 * g;
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s) {
+                    const f32x4 r = *reinterpret_cast<const f32x4 *>(rows + 16 * s);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) acc[w][m][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(r[i], s0[s][i][j], acc[w][m][j], 0, 0, 0);
+                }
             }
     }
-    f32x4 acc[2][MT][2];
-#pragma unroll
-    for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            acc[w][m][0] = acc[w][m][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (16 * m >= T) continue;
-            const float *rows = (w ? pq : pk) + (16 * m + x) * L::kPitch + 4 * g;
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s) {
-                const f32x4 r = *reinterpret_cast<const f32x4 *>(rows + 16 * s);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[w][m][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(r[i], s0[s][i][j], acc[w][m][j], 0, 0, 0);
-            }
-        }
     __syncthreads();
     // ---- the matrices, and the inverses of the first one's diagonal blocks in their places ----
     float *sk = reinterpret_cast<float *>(lds), *sq = sk + TM * L::kSumPitch;
@@ -298,8 +419,8 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
         if (t >= TM) continue;
 #pragma unroll
         for (int c = 0; c < MT; ++c) {
-            sk[t * L::kSumPitch + 16 * c + x] = nk[r][c];
-            sq[t * L::kSumPitch + 16 * c + x] = nq[r][c];
+            sk[t * L::kSumPitch + 16 * c + x] = c > block_of(r) ? 0.f : nk[r][c];
+            sq[t * L::kSumPitch + 16 * c + x] = c > block_of(r) ? 0.f : nq[r][c];
         }
     }
     if constexpr (L::kHasValues) {

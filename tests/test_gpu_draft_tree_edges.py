@@ -339,3 +339,39 @@ def test_one_long_sequence_of_a_batch(d, T, Hq):
     got = _attend(pool, q, held, parents, max_kv_len=long + T)
     _within(got, *_attend_refs(pool, q, held, parents), torch.float32)
     assert torch.equal(got, _attend(pool, q, held, parents))
+
+
+@pytest.mark.parametrize("T,d", [(24, 64), (24, 128), (64, 64), (64, 128)])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_a_state_that_is_not_finite_reaches_its_columns_in_larger_trees(T, d, value):
+    import paper_2510_26692_amd as kda
+    x = [y.cuda() for y in _inputs(2, T, 2, d, torch.float32, 1)]
+    S = (torch.randn(2, 2, d, d, generator=torch.Generator().manual_seed(2)) * 0.3).cuda()
+    parents = random_trees(2, T, 3, 5)
+    parents[0, T - 5:] = -2
+    want = kda.kda_tree_steps(*x, S, int32(parents))
+    S[0, 1, d - 3, 41] = value
+    got = kda.kda_tree_steps(*x, S, int32(parents))
+    odd = torch.zeros(2, T, 2, d, dtype=torch.bool, device="cuda")
+    odd[0, :T - 5, 1, 41] = True
+    assert bool(torch.equal(got[~odd], want[~odd])) and not bool(torch.isfinite(got[odd]).any())
+
+
+@pytest.mark.parametrize("T,d", [(16, 128), (17, 64), (32, 128), (50, 64), (64, 128)])
+def test_states_of_any_size(T, d):
+    """The largest numbers, some far apart, and small ones down to 2^-90: products with the state are off by fp32's steps of its columns."""
+    import paper_2510_26692_amd as kda
+    x = list(_inputs(1, T, 2, d, torch.float32, T))
+    parents = random_trees(1, T, 3, T)
+    run = lambda S: _check_steps(*x, S, None, parents, 2.0 ** -6, torch.float32,
+                                 kda.kda_tree_steps(*(y.cuda() for y in x), S.cuda(), int32(parents), scale=2.0 ** -6))
+    g = torch.Generator().manual_seed(2)
+    S = torch.randn(1, 2, d, d, generator=g) * 2.0 ** torch.randint(-30, 31, (1, 2, d, d), generator=g)
+    run(S)
+    run(S * 2.0 ** 85)
+    x[2] = x[2] * 2.0 ** -90
+    run(torch.randn(1, 2, d, d, generator=g) * 2.0 ** -90)
+    x[2] = x[2] * 0
+    S = torch.zeros(1, 2, d, d)
+    S[0, :, 5, 3], S[0, :, d - 1, 8] = torch.finfo(torch.float32).max, -3.4e38
+    run(S)
