@@ -21,7 +21,8 @@
 //
 // all of them fp32 MFMAs whose accumulators are the operands of the next, so u never leaves its registers.
 //
-// What bounds it is reading the states, and for large trees what a workgroup does one after the other: lines, pieces, products, blocks.  256 trees of up
+// What bounds it is reading the states, and for large trees vector instructions (54 % busy, half of
+// them the sums up the lines) beside the matrix cores (29 %).  256 trees of up
 // to 16 tokens, 32 heads: 136 us (0.68 GB, 5.0 TB/s); 64 of 64 tokens: 139, with fp32 MFMAs 170; in fp32 153, with those and q in LDS 271; 64 chains of 64: 274
 // and 320, 128 trees of 20 99 and 126.  (Pieces for trees of 16, too: the same time in bf16, 172 for 156 in fp32.  With a column a thread and a loop over each token's
 // ancestors in place of the blocks: 231 and 474.)
