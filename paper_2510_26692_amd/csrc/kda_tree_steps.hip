@@ -23,8 +23,9 @@
 //
 // What bounds it is reading the states, and for large trees vector instructions (54 % busy, half of
 // them the sums up the lines) beside the matrix cores (29 %).  256 trees of up
-// to 16 tokens, 32 heads: 136 us (0.68 GB, 5.0 TB/s); 64 of 64 tokens: 139, with fp32 MFMAs 170; in fp32 153, with those and q in LDS 271; 64 chains of 64: 274
-// and 320, 128 trees of 20 99 and 126.  (Pieces for trees of 16, too: the same time in bf16, 172 for 156 in fp32.  With a column a thread and a loop over each token's
+// to 16 tokens, 32 heads: 136 us (0.68 GB, 5.0 TB/s); 64 of 64 tokens: 130, in fp32 150; 64 chains of 64: 230;
+// 128 trees of 20: 99.  With fp32 MFMAs and q in LDS these were 170, 271, 320 and 126.  A step up a line is some 65 vector instructions for a group: scales
+// and what is not finite are looked at behind it (chains 278 -> 230).  (Pieces for trees of 16, too: the same time in bf16, 172 for 156 in fp32.  With a column a thread and a loop over each token's
 // ancestors in place of the blocks: 231 and 474.)
 #include "kda_tree.h"
 
@@ -97,7 +98,7 @@ __device__ __forceinline__ f32x4 mfma16(const f32x4 &a, const f32x4 &b, f32x4 ac
 }
 
 // LDS: decays of the tokens in fp32, then their k and, of small trees, q as they came, [TM][D + 4] each; in the same place P_i0 k_i and scale P_i0 q_i in fp32, or of
-// larger trees their pieces; and then the two matrices of sums over channels, [TM][TM + 4] each.  Behind them the lines, and v and beta.
+// larger trees their pieces; and then the two matrices of sums over channels, [TM][TM + 4] each.  Behind them the lines, parents, v and beta.
 template <typename Tin, int D, int TM> struct StepLds {
     static constexpr int kPitch = D + 4, kSumPitch = TM + 4;
     static constexpr int kRows = TM * kPitch;
@@ -109,7 +110,7 @@ template <typename Tin, int D, int TM> struct StepLds {
     static constexpr int kMost = kTokens > kProducts ? kTokens : kProducts, kLines = kMost > kSums ? kMost : kSums;
     // (values and betas of trees of up to 32 tokens; a large tree's would leave one workgroup a compute unit)
     static constexpr bool kHasValues = TM < 64;
-    static constexpr int kValues = kLines + kTreeTokens * 8, kBetas = kValues + (kHasValues ? kRows * (int)sizeof(Tin) : 0);
+    static constexpr int kParents = kLines + kTreeTokens * 8, kValues = kParents + kTreeTokens * 4, kBetas = kValues + (kHasValues ? kRows * (int)sizeof(Tin) : 0);
     static constexpr int kBytes = kBetas + (kHasValues ? TM * 4 : 0);
 };
 
@@ -124,16 +125,21 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
     float *al = reinterpret_cast<float *>(lds);
     Tin *kk = reinterpret_cast<Tin *>(al + L::kRows), *qq = kk + L::kRows;
     uint64_t *lines = reinterpret_cast<uint64_t *>(lds + L::kLines);
+    int32_t *parents = reinterpret_cast<int32_t *>(lds + L::kParents);       // (of tokens that are there: -1 ends a line)
     [[maybe_unused]] Tin *vs = reinterpret_cast<Tin *>(lds + L::kValues);
     [[maybe_unused]] float *betas = reinterpret_cast<float *>(lds + L::kBetas);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, x = lane & 15, g = lane >> 4;
-    const int64_t n = blockIdx.x / a.heads;
+    int seq = (int)(blockIdx.x / (uint32_t)a.heads);
+    asm("" : "+s"(seq));                                     // (a division's result stands in vector registers, and all that is made of it)
+    const int64_t n = seq;
     const int h = (int)(blockIdx.x - n * a.heads), T = a.tokens;
     const int64_t row0 = n * T * a.heads + h;                // row of token 0; the next is `heads` behind
+    // a token's row behind that: below 2^22, and so a channel's place below 2^29
+    auto row_of = [&](int t) { return (uint32_t)(min(t, T - 1) * a.heads); };
     const int64_t state = a.indices ? a.indices[n] : n;
     const int col = 32 * wave + 2 * x;                       // the lane's columns are this and the next
     auto put = [&](int t, float lo, float hi) {
-        const uint32_t at = (uint32_t)(t * a.heads) * D + col;           // (below 2^30)
+        const uint32_t at = row_of(t) * D + col;
         if (a.out_bf16) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(a.o) + row0 * D + at) = pack_bf16x2(lo, hi);
         else *reinterpret_cast<f32x2 *>(static_cast<float *>(a.o) + row0 * D + at) = f32x2{lo, hi};
     };
@@ -152,27 +158,23 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
     Four<Tin> kv[kPieces], lv[kPieces];
     Tin lh[kPieces];
     {
-        const Tin *q = static_cast<const Tin *>(a.q), *k = static_cast<const Tin *>(a.k), *la = static_cast<const Tin *>(a.log_alpha);
-        auto row_of = [&](int r) { return row0 + (int64_t)min((tid + kThreads * r) / (D / 4), T - 1) * a.heads; };
-        const int c = 4 * (tid % (D / 4));
+        const Tin *q = static_cast<const Tin *>(a.q) + row0 * D, *k = static_cast<const Tin *>(a.k) + row0 * D;
+        const Tin *la = static_cast<const Tin *>(a.log_alpha) + (a.scalar_gate ? row0 : row0 * D);
+        const uint32_t c = 4 * (tid % (D / 4));
 #pragma unroll
         for (int r = 0; r < kPieces; ++r) {
-            kv[r] = *reinterpret_cast<const Four<Tin> *>(k + row_of(r) * D + c);
-            if constexpr (!L::kPlanes) qv[r] = *reinterpret_cast<const Four<Tin> *>(q + row_of(r) * D + c);
-        }
-        if (a.scalar_gate) {
-#pragma unroll
-            for (int r = 0; r < kPieces; ++r) lh[r] = la[row_of(r)];
-        } else {
-#pragma unroll
-            for (int r = 0; r < kPieces; ++r) lv[r] = *reinterpret_cast<const Four<Tin> *>(la + row_of(r) * D + c);
+            const uint32_t row = row_of((tid + kThreads * r) / (D / 4));
+            kv[r] = *reinterpret_cast<const Four<Tin> *>(k + (row * D + c));
+            if constexpr (!L::kPlanes) qv[r] = *reinterpret_cast<const Four<Tin> *>(q + (row * D + c));
+            if (a.scalar_gate) lh[r] = la[row];
+            else lv[r] = *reinterpret_cast<const Four<Tin> *>(la + (row * D + c));
         }
         if constexpr (L::kPlanes) {
 #pragma unroll
             for (int r = 0; r < kNodes; ++r)
 #pragma unroll
                 for (int i = 0; i < CH; i += 4)
-                    queries[r][i / 4] = *reinterpret_cast<const Four<Tin> *>(q + (row0 + (int64_t)min(group + kGroups * r, T - 1) * a.heads) * D + own(i));
+                    queries[r][i / 4] = *reinterpret_cast<const Four<Tin> *>(q + (row_of(group + kGroups * r) * D + (uint32_t)own(i)));
         }
     }
     [[maybe_unused]] Four<Tin> values[kPieces];
@@ -180,10 +182,10 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
     if constexpr (L::kHasValues) {
 #pragma unroll
         for (int r = 0; r < kPieces; ++r) {
-            const int t = min((tid + kThreads * r) / (D / 4), T - 1), c = 4 * (tid % (D / 4));
-            values[r] = *reinterpret_cast<const Four<Tin> *>(static_cast<const Tin *>(a.v) + (row0 + (int64_t)t * a.heads) * D + c);
+            const uint32_t c = 4 * (tid % (D / 4)), row = row_of((tid + kThreads * r) / (D / 4));
+            values[r] = *reinterpret_cast<const Four<Tin> *>(static_cast<const Tin *>(a.v) + row0 * D + (row * D + c));
         }
-        own_beta = load_as_float(static_cast<const Tin *>(a.beta) + row0 + (int64_t)min(tid, T - 1) * a.heads);
+        own_beta = load_as_float(static_cast<const Tin *>(a.beta) + row0 + row_of(tid));
     }
     // the state's rows 16 s + 4 g + i
     f32x2 s0[D / 16][4];
@@ -194,7 +196,10 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
 #pragma unroll
             for (int i = 0; i < 4; ++i) s0[s][i] = __builtin_nontemporal_load(reinterpret_cast<const f32x2 *>(from + (16 * s + i) * D));
     }
-    if (wave == 0) lines[lane] = tree_line(up, T);
+    if (wave == 0) {
+        lines[lane] = tree_line(up, T);
+        parents[lane] = up;
+    }
     __syncthreads();
     // ---- tokens (one that is not there: no key, no query, no decay) ----
 #pragma unroll
@@ -241,17 +246,17 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
         for (int i = 0; i < CH; ++i) all[r][i] = 1.f;
 #pragma unroll
         for (int c = 0; c < MT; ++c) nk[r][c] = nq[r][c] = 0.f;
-        uint64_t line = 0;
         float b = 0.f, kt[CH], qt[CH];
+        int j = -1;
         if (t < TM) {
             channels(kk, t, kt);
             query(r, t, qt);
-            line = lines[t];
-            if (line) b = L::kHasValues ? betas[t] : load_as_float(static_cast<const Tin *>(a.beta) + row0 + (int64_t)t * a.heads);
+            if (lines[t]) {
+                b = L::kHasValues ? betas[t] : load_as_float(static_cast<const Tin *>(a.beta) + row0 + row_of(t));
+                j = t;
+            }
         }
-        while (line) {
-            const int j = 63 - __builtin_clzll(line);
-            line &= ~(1ull << j);
+        while (j >= 0) {
             float kj[CH], aj[CH], dk = 0.f, dq = 0.f;
             channels(kk, j, kj);
             channels(al, j, aj);
@@ -262,18 +267,24 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
                 dq = fmaf(qt[i], w, dq);
                 all[r][i] *= aj[i];
             }
-            dk = j < t ? -b * over_sixteen(dk) : 0.f;
-            dq = a.scale * over_sixteen(dq);
-            // (one that is not finite belongs to a token whose own r or o is not: zero here, it stays out of the others')
-            dk = finite(dk) ? dk : 0.f;
-            dq = finite(dq) ? dq : 0.f;
+            dk = over_sixteen(dk);
+            dq = over_sixteen(dq);
 #pragma unroll
             for (int c = 0; c < MT; ++c) {
                 if (c > block_of(r)) continue;
-                const bool here = x == (j & 15) && c == j >> 4;
+                const bool here = x == j - 16 * c;
                 nk[r][c] = here ? dk : nk[r][c];
                 nq[r][c] = here ? dq : nq[r][c];
             }
+            j = parents[j];
+        }
+#pragma unroll
+        for (int c = 0; c < MT; ++c) {
+            if (c > block_of(r)) continue;
+            const float dk = x + 16 * c == t ? 0.f : -b * nk[r][c], dq = a.scale * nq[r][c];
+            // (one that is not finite belongs to a token whose own r or o is not: zero here, it stays out of the others')
+            nk[r][c] = finite(dk) ? dk : 0.f;
+            nq[r][c] = finite(dq) ? dq : 0.f;
         }
     }
     __syncthreads();
@@ -286,9 +297,9 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int64_t row = row0 + (int64_t)min(16 * m + 4 * g + e, T - 1) * a.heads;
-                    vv[m][e] = load2(static_cast<const Tin *>(a.v) + row * D + col);
-                    beta[m][e] = load_as_float(static_cast<const Tin *>(a.beta) + row);
+                    const uint32_t row = row_of(16 * m + 4 * g + e);
+                    vv[m][e] = load2(static_cast<const Tin *>(a.v) + row0 * D + (row * D + (uint32_t)col));
+                    beta[m][e] = load_as_float(static_cast<const Tin *>(a.beta) + row0 + row);
                 }
         }
     };
