@@ -21,8 +21,8 @@
 //
 // all of them fp32 MFMAs whose accumulators are the operands of the next, so u never leaves its registers.
 //
-// What bounds it is reading the states, and for large trees vector instructions (54 % busy, half of them the sums up the lines) beside the matrix cores
-// (29 %).  256 trees of up to 16 tokens, 32 heads: 136 us (0.68 GB, 5.0 TB/s); 64 of 64 tokens: 130, in fp32 150; 64 chains of 64: 230; 128 trees of 20: 99.
+// What bounds it is reading the states, and for large trees vector instructions (53 % busy, half of them the sums up the lines) beside the matrix cores
+// (31 %).  256 trees of up to 16 tokens, 32 heads: 132 us (0.68 GB, 5.2 TB/s); 64 of 64 tokens: 128, in fp32 150; 64 chains of 64: 230; 128 trees of 20: 99.
 // With fp32 MFMAs and q in LDS these were 170, 271, 320 and 126.  A step up a line is some 65 vector instructions for a group: scales and what is not finite
 // are looked at behind it (chains 278 -> 230).  (Pieces for trees of 16, too: the same time in bf16, 172 for 156 in fp32.  With a column a thread and a loop
 // over each token's ancestors in place of the blocks: 231 and 474.)
