@@ -21,6 +21,11 @@
 //
 // all of them fp32 MFMAs whose accumulators are the operands of the next, so u never leaves its registers.
 //
+// A sum over channels may leave fp32 where u and the scale would bring it back, and entries of an inverse that do would make NaN of tokens beside their line (0 times
+// infinity).  So what is not finite is kept out of the matrices and of r, and remembered: the rows that it belongs to, and whatever rows are not finite at the end,
+// are worked through again from state to state, as kda_recurrent_steps does, a line at a time.  Only those are written again: a row is the same
+// whatever its neighbours hold.  (Looking for them costs 0.3 us of 132.  The pass itself is slow: 64 chains of 64 tokens with keys 22 long 1.5 ms for 230 us.)
+//
 // What bounds it is reading the states, and for large trees vector instructions (53 % busy, half of them the sums up the lines) beside the matrix cores
 // (31 %).  256 trees of up to 16 tokens, 32 heads: 132 us (0.68 GB, 5.2 TB/s); 64 of 64 tokens: 128, in fp32 150; 64 chains of 64: 230; 128 trees of 20: 99.
 // With fp32 MFMAs and q in LDS these were 170, 271, 320 and 126.  A step up a line is some 65 vector instructions for a group: scales and what is not finite
@@ -110,8 +115,106 @@ template <typename Tin, int D, int TM> struct StepLds {
     // (values and betas of trees of up to 32 tokens; a large tree's would leave one workgroup a compute unit)
     static constexpr bool kHasValues = TM < 64;
     static constexpr int kParents = kLines + kTreeTokens * 8, kValues = kParents + kTreeTokens * 4, kBetas = kValues + (kHasValues ? kRows * (int)sizeof(Tin) : 0);
-    static constexpr int kBytes = kBetas + (kHasValues ? TM * 4 : 0);
+    static constexpr int kLost = kBetas + (kHasValues ? TM * 4 : 0), kBytes = kLost + 16;    // tokens with a sum that is not finite, of k and of q: 64 bits each
 };
+
+// The rows of a wave's 32 columns that are not finite in o, from state to state along their lines: eight columns at a time, sixteen lanes with D / 16 channels
+// each to two of them, so that the registers of what comes before are not added to.
+template <typename Tin, int D>
+__device__ __forceinline__ void step_again(const Tree &a, const uint64_t *lines, int64_t row0, int64_t state_at)
+{
+    constexpr int CH = D / 16;                               // channels of a lane
+    const int lane = threadIdx.x & 63, x = lane & 15, T = a.tokens;
+    auto row_of = [&](int t) { return (uint32_t)(t * a.heads); };
+    auto uniform = [](uint64_t w) {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(w >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)w);
+    };
+    auto joined = [](uint64_t w, int lanes) { return w | (uint64_t)(uint32_t)__shfl_xor((int)(w >> 32), lanes) << 32 | (uint32_t)__shfl_xor((int)w, lanes); };
+    __threadfence_block();                                   // (o is read here as this wave has left it)
+#pragma unroll 1
+    for (int col = 32 * (threadIdx.x >> 6) + 2 * (lane >> 4), end = col + 32; col < end; col += 8) {
+        uint64_t odd[2] = {0, 0};                            // tokens, of the lane's columns
+#pragma unroll 1
+        for (int t = x; t < T; t += 16) {
+            if (!lines[t]) continue;
+            const int64_t at = row0 * D + (row_of(t) * D + (uint32_t)col);
+            const f32x2 o = a.out_bf16 ? load2(static_cast<const __hip_bfloat16 *>(a.o) + at) : load2(static_cast<const float *>(a.o) + at);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) odd[j] |= finite(o[j]) ? 0ull : 1ull << t;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 1; i < 16; i <<= 1) odd[j] = joined(odd[j], i);
+        uint64_t left = uniform(joined(joined(odd[0] | odd[1], 16), 32)), above = 0;          // above: the line of the token whose state is at hand
+        float S[2][CH];
+#pragma unroll 1
+        for (bool begin = true; left; begin = false) {
+            const int t = __builtin_ctzll(left);
+            left &= left - 1;
+            const uint64_t line = uniform(lines[t]);
+            if (begin || (above & ~line)) {
+                above = 0;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const f32x2 w = load2(a.states + state_at + (CH * x + i) * D + col);
+                    S[0][i] = w[0];
+                    S[1][i] = w[1];
+                }
+            }
+            uint64_t ahead = line & ~above;
+            above = line;
+#pragma unroll 1
+            while (ahead) {
+                const int n = __builtin_ctzll(ahead);
+                ahead &= ahead - 1;
+                const uint32_t row = row_of(n), at = row * D + CH * x;
+                const Tin *la = static_cast<const Tin *>(a.log_alpha) + row0 * (a.scalar_gate ? 1 : D);
+                float k[CH], w[2] = {0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < CH; i += 4) {
+                    const f32x4 kf = load4(static_cast<const Tin *>(a.k) + row0 * D + (at + i));
+                    f32x4 af = f32x4{1.f, 1.f, 1.f, 1.f} * (a.scalar_gate ? load_as_float(la + row) : 0.f);
+                    if (!a.scalar_gate) af = load4(la + (at + i));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        k[i + e] = kf[e];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            S[j][i + e] *= fast_exp2(af[e] * kLog2e);
+                            w[j] = fmaf(kf[e], S[j][i + e], w[j]);
+                        }
+                    }
+                }
+                const float b = load_as_float(static_cast<const Tin *>(a.beta) + row0 + row);
+                const f32x2 v = load2(static_cast<const Tin *>(a.v) + row0 * D + (row * D + (uint32_t)col));
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float u = b * (v[j] - over_sixteen(w[j]));
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) S[j][i] = fmaf(k[i], u, S[j][i]);
+                }
+            }
+            float y[2] = {0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < CH; i += 4) {
+                const f32x4 q = load4(static_cast<const Tin *>(a.q) + row0 * D + (row_of(t) * D + (uint32_t)(CH * x + i)));
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) y[j] = fmaf(q[e], S[j][i + e], y[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float out = a.scale * over_sixteen(y[j]);
+                if (x != 0 || !(odd[j] >> t & 1)) continue;
+                const int64_t to = row0 * D + (row_of(t) * D + (uint32_t)(col + j));
+                if (a.out_bf16) static_cast<uint16_t *>(a.o)[to] = (uint16_t)pack_bf16x2(out, 0.f);
+                else static_cast<float *>(a.o)[to] = out;
+            }
+        }
+    }
+}
 
 template <typename Tin, int D, int TM>
 __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel(const Tree a)
@@ -127,6 +230,7 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
     int32_t *parents = reinterpret_cast<int32_t *>(lds + L::kParents);       // (of tokens that are there: -1 ends a line)
     [[maybe_unused]] Tin *vs = reinterpret_cast<Tin *>(lds + L::kValues);
     [[maybe_unused]] float *betas = reinterpret_cast<float *>(lds + L::kBetas);
+    uint32_t *lost = reinterpret_cast<uint32_t *>(lds + L::kLost);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, x = lane & 15, g = lane >> 4;
     int seq = (int)(blockIdx.x / (uint32_t)a.heads);
     asm("" : "+s"(seq));                                     // (a division's result stands in vector registers, and all that is made of it)
@@ -198,6 +302,7 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
     if (wave == 0) {
         lines[lane] = tree_line(up, T);
         parents[lane] = up;
+        if (lane < 4) lost[lane] = 0u;
     }
     __syncthreads();
     // ---- tokens (one that is not there: no key, no query, no decay) ----
@@ -277,14 +382,19 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
             }
             j = parents[j];
         }
+        bool lost_k = false, lost_q = false;
 #pragma unroll
         for (int c = 0; c < MT; ++c) {
             if (c > block_of(r)) continue;
             const float dk = x + 16 * c == t ? 0.f : -b * nk[r][c], dq = a.scale * nq[r][c];
-            // (one that is not finite belongs to a token whose own r or o is not: zero here, it stays out of the others')
+            // (zero here, one that is not finite stays out of the others' rows)
+            lost_k |= !finite(dk);
+            lost_q |= !finite(dq);
             nk[r][c] = finite(dk) ? dk : 0.f;
             nq[r][c] = finite(dq) ? dq : 0.f;
         }
+        if (lost_k) atomicOr(lost + (t >> 5), 1u << (t & 31));
+        if (lost_q) atomicOr(lost + 2 + (t >> 5), 1u << (t & 31));
     }
     __syncthreads();
     f32x2 vv[MT][4];
@@ -497,8 +607,9 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
             for (int j = 0; j < 2; ++j) acc[1][m][j] = mfma16(w, acc[0][k][j], acc[1][m][j]);
         }
     }
-    if (__any(odd)) {
-        // how many tokens of each line were taken out
+    const uint64_t lost_k = lost[0] | (uint64_t)lost[1] << 32, lost_q = lost[2] | (uint64_t)lost[3] << 32;
+    if (__any(odd != 0 || (lost_k | lost_q) != 0)) {
+        // of how many tokens of each line r, or a sum of k, was taken out
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const uint64_t line = lines[16 * m + x];
@@ -512,16 +623,18 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
                 for (int j = 0; j < 2; ++j) {
                     f32x4 marks;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) marks[e] = (odd >> (8 * k + 4 * j + e)) & 1 ? 1.f : 0.f;
+                    for (int e = 0; e < 4; ++e) marks[e] = ((odd >> (8 * k + 4 * j + e)) | (uint32_t)(lost_k >> (16 * k + 4 * g + e))) & 1 ? 1.f : 0.f;
                     seen[j] = mfma16(w, marks, seen[j]);
                 }
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[1][m][j][e] = seen[j][e] > 0.f ? __builtin_nanf("") : acc[1][m][j][e];
+                for (int e = 0; e < 4; ++e)
+                    acc[1][m][j][e] = seen[j][e] > 0.f || (lost_q >> (16 * m + 4 * g + e)) & 1 ? __builtin_nanf("") : acc[1][m][j][e];
         }
     }
+    bool some = false;                                       // not finite, of a row that may be nobody's
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -529,8 +642,12 @@ __global__ __launch_bounds__(2 * D, TM == 16 ? 4 : 2) void kda_tree_steps_kernel
             const int t = 16 * m + 4 * g + e;
             if (t >= T) continue;
             const bool there = lines[t] != 0;
+            some |= !finite(acc[1][m][0][e]) || !finite(acc[1][m][1][e]);
             put(t, there ? acc[1][m][0][e] : 0.f, there ? acc[1][m][1][e] : 0.f);
         }
+    if (!__any(some)) return;
+
+    step_again<Tin, D>(a, lines, row0, (state * a.heads + h) * (D * D));
 }
 
 struct Commit {
