@@ -517,6 +517,7 @@ typedef struct {
  * nothing (kv_lens[n] <= 0, a position below zero: a batch of sequences with fewer new tokens is padded in front) gets zeros.
  *   q [num_seqs,tokens,heads_q,dim] bf16      o [num_seqs,tokens,heads_q,dim] out_dtype
  *   workspace   at least kda_cache_attn_workspace_size bytes (0 for some calls), 256-byte aligned
+ * Products in fp32, the softmax's terms rounded to bf16 ahead of the product with v, as in kda_window_attn_fwd, whatever out_dtype is.
  * Scales may be any finite numbers here, so that scale * k_scale is finite and, for full precision, v_scale is 2^-110 at least and within a factor
  * of 2^100 of the sequence and head's largest: results are finite for values up to 2^127.  What is not finite reaches the rows that see it and no
  * others, whatever stands behind the last token of a page or in pages that no row sees.
@@ -572,6 +573,8 @@ kda_status kda_rotate(const kda_rotation *rotation, const void *q, const void *k
  *   query       tokens 0..64, the rest as for kda_cache_attn; max_kv_len: upper bound of kv_lens[n] + tokens
  *   parents     [num_seqs,tokens] int32
  *   workspace   at least kda_cache_tree_attn_workspace_size bytes (0 for some calls), 256-byte aligned
+ * The softmax's terms go to the product with v rounded to bf16 where o is bf16 (to 2^-16 of themselves for heads of 128 and up to 16 rows, tokens x heads_q / heads_kv), and
+ * to 2^-16 of themselves where it is fp32, which takes about 1.3 times as long.
  * Scales and what is not finite: as for kda_cache_attn.  o must not alias an input.
  */
 size_t kda_cache_tree_attn_workspace_size(const kda_cache *cache, const kda_cache_query *query);

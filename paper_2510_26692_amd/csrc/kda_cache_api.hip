@@ -7,7 +7,7 @@ namespace kda {
 kda_status cache_append_dispatch(const cache::Cache &, const cache::Append &, int dim, hipStream_t);
 kda_status cache_attn_dispatch(const cache::Cache &, const cache::Attend &, int dim, hipStream_t);
 kda_status cache_tree_dispatch(const cache::Cache &, const cache::TreeAttend &, int dim, hipStream_t);
-int32_t cache_tree_splits(int dim, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens);
+int32_t cache_tree_splits(int dim, bool fine, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens);
 int32_t cache_tree_tile_rows(int32_t rows);
 int32_t cache_few_rows(int dim);
 int32_t cache_few_splits(const cache::Cache &, int64_t pairs, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens);
@@ -96,7 +96,7 @@ kda_status check(const kda_cache *d, bool buffers, const kda_cache_query *q, boo
     const int64_t pairs = (int64_t)c.num_seqs * c.heads_kv, held = (int64_t)d->max_pages * d->page_size;
     const int64_t most = q->max_kv_len && q->max_kv_len < held ? q->max_kv_len : held;
     if (!pairs || !a.rows) a.splits = 1;
-    else if (tree && !few) a.splits = cache_tree_splits(d->dim, pairs * a.row_tiles, most, a.window, a.sinks, a.tokens);
+    else if (tree && !few) a.splits = cache_tree_splits(d->dim, !a.out_bf16, pairs * a.row_tiles, most, a.window, a.sinks, a.tokens);
     else a.splits = (few ? cache_few_splits : cache_attn_splits)(c, pairs * a.row_tiles, most, a.window, a.sinks, a.tokens);
     // (a launch has fewer than 2^32 threads: 256 a workgroup, and 64 a row of the join)
     if (pairs * a.row_tiles * a.splits > 0xffffff || pairs * a.rows > 0x3ffffff) return fail(KDA_ERR_UNSUPPORTED, "more than 2^24 workgroups");

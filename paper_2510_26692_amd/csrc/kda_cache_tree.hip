@@ -14,6 +14,11 @@
 // they take the same time): four sequences of up to 131 072 tokens, 8 key heads, trees of 64 tokens and 32 heads, in 533 to 543 us (820 TFLOP/s of visible pairs;
 // a library product of 8192^3 1 379), 64 of up to 8 192 with 20 to 32 tokens in 268 to 280.
 //
+// The softmax's terms P are rounded to bf16 ahead of their product with V where the result is bf16: half a step, 2^-8, is what the result's own rounding may be off
+// by.  Where it is fp32 they go as two bf16, P = p + rest, of which 2^-16 is left out, and V is multiplied twice.  Off the formulas in 64 bits, in the mean square, and time, for 64
+// sequences of up to 8 192 with 20 to 32 tokens: bf16 results 2.3 10^-3 in 272 us (with two 1.7 10^-3 in 369: not taken), fp32 results 4.8 10^-6 in 354 (with one
+// 1.6 10^-3 in 277).
+//
 // A row's token sees what is held (by the window and sinks of its position, len + depth) and its line, a bit for each drafted token; both
 // become one word of bits a tile, made only for tiles that some row sees in part.
 #include <atomic>
@@ -78,6 +83,21 @@ __device__ __forceinline__ bool is_plain(float scale)
     return (b & 0x807fffffu) == 0 && b - (67u << 23) <= 120u << 23;
 }
 
+// x = p + rest in bf16: p what bf16's bits have of x, rest what is left, rounded (to 2^-16 of x)
+__device__ __forceinline__ void two_of(const float *x, bf16x8 &p, bf16x8 &rest)
+{
+    u32x4 w;
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = __float_as_uint(x[2 * i]), hi = __float_as_uint(x[2 * i + 1]);
+        w[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+        r[2 * i] = x[2 * i] - __uint_as_float(lo & 0xffff0000u);
+        r[2 * i + 1] = x[2 * i + 1] - __uint_as_float(hi & 0xffff0000u);
+    }
+    p = __builtin_bit_cast(bf16x8, w);
+    rest = attn::pack8(r);
+}
 __device__ __forceinline__ bf16x8 held(const bf16x8 &v)
 {
     u32x4 w = __builtin_bit_cast(u32x4, v);
@@ -122,7 +142,7 @@ __device__ __forceinline__ int sequence_of(const Cache &c, const TreeAttend &a, 
 
 // A tile of rows over a split's keys.  Returns true where the walk has to be repeated with care: a value that is not finite stood where some row does
 // not see it.
-template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_tile(const Cache &c, const TreeAttend &a)
+template <int D, int WR, bool kFine, bool kCareful> __device__ __forceinline__ bool tree_tile(const Cache &c, const TreeAttend &a)
 {
     constexpr int WK = 4 / WR, KB = 2 / WK;                  // waves along the keys; 32-key blocks of a wave
     constexpr int kT = Lds<D>::kT, kChunks = D / 16, kPieces = kKeys * kChunks / 256;     // 16-code pieces of a key; of a thread, keys or values
@@ -303,6 +323,7 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
                 for (int j = 0; j < 16; ++j) acc[db][j] *= f;
         }
         bf16x8 p[2 * KB];
+        [[maybe_unused]] bf16x8 rest[2 * KB];
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
             float e[16];
@@ -312,7 +333,13 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
                 l += e[j];
             }
             // (packed on either side of the branch, and held there: values that meet behind it would be moved)
-            if (every & 2) {
+            if constexpr (kFine) {
+                if (!(every & 2))
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) e[j] *= vs[2 * b + j / 8];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) two_of(e + 8 * i, p[2 * b + i], rest[2 * b + i]);
+            } else if (every & 2) {
                 p[2 * b] = held(attn::pack8(e));
                 p[2 * b + 1] = held(attn::pack8(e + 8));
             } else {
@@ -324,15 +351,23 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
         }
         if (kCareful && edge) {
 #pragma unroll
-            for (int db = 0; db < D / 32; ++db) attn::careful_product<D, 2 * KB>(acc[db], rd, vt, db, 2 * KB * wk, p, seen);
+            for (int db = 0; db < D / 32; ++db) {
+                attn::careful_product<D, 2 * KB>(acc[db], rd, vt, db, 2 * KB * wk, p, seen);
+                if constexpr (kFine) attn::careful_product<D, 2 * KB>(acc[db], rd, vt, db, 2 * KB * wk, rest, seen);
+            }
         } else {
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int s = 0; s < 2 * KB; ++s)
 #pragma unroll
-                for (int db = 0; db < D / 32; ++db) acc[db] = attn::mfma(rd.transposed(vt, db, 2 * KB * wk + s), p[s], acc[db]);
-            attn::reads_ahead<2 * kLead, 2, 2 * KB * D / 16, KB * D / 16>();
+                for (int db = 0; db < D / 32; ++db) {
+                    const bf16x8 v = rd.transposed(vt, db, 2 * KB * wk + s);
+                    acc[db] = attn::mfma(v, p[s], acc[db]);
+                    if constexpr (kFine) acc[db] = attn::mfma(v, rest[s], acc[db]);
+                }
+            if constexpr (kFine) attn::reads_ahead<2 * kLead, 1, 2 * KB * D / 16, 2 * KB * D / 16>();
+            else attn::reads_ahead<2 * kLead, 2, 2 * KB * D / 16, KB * D / 16>();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
         }
@@ -419,15 +454,19 @@ template <int D, int WR, bool kCareful> __device__ __forceinline__ bool tree_til
         }
     return again;
 }
-template <int D, int WR> __device__ __noinline__ void tree_tile_again(const Cache c, const TreeAttend a) { tree_tile<D, WR, true>(c, a); }
+template <int D, int WR, bool kFine> __device__ __noinline__ void tree_tile_again(const Cache c, const TreeAttend a) { tree_tile<D, WR, kFine, true>(c, a); }
+template <int D, int WR, bool kFine> __device__ __forceinline__ void tree_rows(const Cache &c, const TreeAttend &a)
+{
+    if (!tree_tile<D, WR, kFine, false>(c, a)) return;
+    __syncthreads();                                         // (LDS is read to the end)
+    tree_tile_again<D, WR, kFine>(c, a);
+}
 // (of heads of 64, three on a compute unit, as cache_tree_splits counts on)
 template <int D, int WR>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void kda_cache_tree_kernel(const Cache c, const TreeAttend a)
-{
-    if (!tree_tile<D, WR, false>(c, a)) return;
-    __syncthreads();                                         // (LDS is read to the end)
-    tree_tile_again<D, WR>(c, a);
-}
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void kda_cache_tree_kernel(const Cache c, const TreeAttend a) { tree_rows<D, WR, false>(c, a); }
+// for results in fp32
+template <int D, int WR>
+__global__ __launch_bounds__(256, 2) void kda_cache_tree_fine_kernel(const Cache c, const TreeAttend a) { tree_rows<D, WR, true>(c, a); }
 
 }  // namespace cache
 }  // namespace kda
@@ -444,18 +483,18 @@ int32_t cache_tree_tile_rows(int32_t rows) { return rows <= 64 ? 64 : 128; }
 // tokens 22.4 / 19.6, one of 16 000 22.5 / 21.6, 16 of 8 000 62 / 88; eight of 4 000 with trees of 32 36.3 / 38.7; 32 of 1 000 split in two / whole 34.3 / 27.8.
 // A few more than they hold would leave a second round to a few of them: with the count rounded up / down, trees of 32 tokens, five sequences of 2 000 29.5 / 25.8,
 // seven of 16 000 90 / 79, 20 of 4 000 82 / 70, 48 of 2 000 111 / 65.
-// Of heads of 64, as many as three on every compute unit hold where each has 16 tiles at least.  us with two / three: four of up to 100 000 with trees of
+// Of heads of 64 with bf16 results, as many as three on every compute unit hold where each has 16 tiles at least.  us with two / three: four of up to 100 000 with trees of
 // 64 tokens 233 / 214, 16 of 8 000 with 64 rows 47 / 43, but eight of 4 000 with 32 28.5 / 33, and, in more than one round, 64 of 8 000 178 / 220.
 // Where that would leave parts of more than 256 tiles, parts of about 64 and up to 2 048 workgroups: of a batch one sequence may be long and the others not, which
 // only the device knows.  us for 64 sequences of 32 000 / one of them in 64, the others of 500 to 2 000: in 512 workgroups 994 / 784, in 2 048 1 060 / 276; 36 of
 // 50 000, one in eight so long, 1 224 / 305; eight of 65 000 to 131 072 with trees of 64 1 058 / 1 005.
-int32_t cache_tree_splits(int dim, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
+int32_t cache_tree_splits(int dim, bool fine, int64_t tiles, int64_t most_keys, int64_t window, int32_t sinks, int32_t tokens)
 {
     int64_t keys = most_keys;
     if (window && window + tokens + sinks + 2 * kKeys < keys) keys = window + tokens + sinks + 2 * kKeys;
     const int64_t steps = (keys + kKeys - 1) / kKeys, most = (steps + 1) / 2, all = tiles > 0 ? tiles : 1;
     int64_t n = all < 512 ? 512 / all : 1;
-    if (dim == 64 && 768 / all > n && steps >= 16 * (768 / all)) n = 768 / all;
+    if (dim == 64 && !fine && 768 / all > n && steps >= 16 * (768 / all)) n = 768 / all;
     if (steps < 5 * n) n = all < 256 ? 256 / all : 1;
     if (all >= 256 && steps <= 16) n = 1;
     if (steps > 256 * n && 2048 / all > n) n = steps / 64 < 2048 / all ? steps / 64 : 2048 / all;
@@ -464,8 +503,9 @@ int32_t cache_tree_splits(int dim, int64_t tiles, int64_t most_keys, int64_t win
 }
 
 namespace {
-template <int D, int WR> hipError_t launch(const Cache &c, const TreeAttend &a, hipStream_t st)
+template <int D, int WR, bool kFine> hipError_t launch(const Cache &c, const TreeAttend &a, hipStream_t st)
 {
+    constexpr auto kernel = kFine ? &kda_cache_tree_fine_kernel<D, WR> : &kda_cache_tree_kernel<D, WR>;
     const uint32_t grid = (uint32_t)c.num_seqs * c.heads_kv * a.row_tiles * a.splits;
     static std::atomic<bool> raised[64];                                  // per device: a workgroup's LDS passes the runtime's default
     if (Lds<D>::kBytes > 65536) {
@@ -473,12 +513,12 @@ template <int D, int WR> hipError_t launch(const Cache &c, const TreeAttend &a, 
         hipError_t e = hipGetDevice(&dev);
         if (e != hipSuccess) return e;
         if (dev < 0 || dev >= 64 || !raised[dev]) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kda_cache_tree_kernel<D, WR>), hipFuncAttributeMaxDynamicSharedMemorySize, Lds<D>::kBytes);
+            e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Lds<D>::kBytes);
             if (e != hipSuccess) return e;
             if (dev >= 0 && dev < 64) raised[dev] = true;
         }
     }
-    hipLaunchKernelGGL((kda_cache_tree_kernel<D, WR>), dim3(grid), dim3(256), Lds<D>::kBytes, st, c, a);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), Lds<D>::kBytes, st, c, a);
     return hipGetLastError();
 }
 template <int D> hipError_t launch(const Cache &c, TreeAttend a, hipStream_t st)
@@ -486,7 +526,8 @@ template <int D> hipError_t launch(const Cache &c, TreeAttend a, hipStream_t st)
     // (with a workgroup for each sequence, head and tile of rows, and more than one round of them)
     const int32_t beside = c.heads_kv * a.row_tiles;
     a.per_round = a.splits == 1 && c.num_seqs <= kOrdered && beside <= 256 && c.num_seqs * beside > 256 ? 256 / beside : 0;
-    hipError_t e = cache_tree_tile_rows(a.rows) == 64 ? launch<D, 2>(c, a, st) : launch<D, 4>(c, a, st);
+    const bool small = cache_tree_tile_rows(a.rows) == 64;
+    hipError_t e = a.out_bf16 ? (small ? launch<D, 2, false>(c, a, st) : launch<D, 4, false>(c, a, st)) : small ? launch<D, 2, true>(c, a, st) : launch<D, 4, true>(c, a, st);
     if (e == hipSuccess && a.splits > 1) e = launch_join<D>(c, a, (int64_t)c.num_seqs * c.heads_kv * a.rows, st);
     return e;
 }

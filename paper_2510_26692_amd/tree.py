@@ -74,7 +74,8 @@ def kda_cache_tree_attn(q, k_cache, v_cache, k_scale, v_scale, block_table, kv_l
     kv_lens int32 [N] counts what a sequence holds WITHOUT the drafted tokens (negative: skip), whose keys and values stand behind it, token
     t's at place kv_lens + t; parents int32 [N,Tq]: the token that a token follows, -1: what the sequence holds, -2: there is no such
     token.  A token sees what is held (within window and sinks, from the position kv_lens + its depth), its ancestors and itself.
-    max_kv_len: upper bound of kv_lens + Tq if known.  Returns o [N,Tq,Hq,d] as kda_cache_attn; rows of tokens that are not there are zero."""
+    max_kv_len: upper bound of kv_lens + Tq if known.  Returns o [N,Tq,Hq,d], fp32 unless out_dtype (or the `o` passed in) is
+    torch.bfloat16, which holds the softmax's terms in bf16 and is faster; rows of tokens that are not there are zero."""
     lib = load_library()
     if workspace is None:
         done = _native("tree_attend", q, k_cache, v_cache, k_scale, v_scale, block_table, kv_lens, parents, window, sinks, scale, max_kv_len, o, out_dtype)
