@@ -10,9 +10,10 @@
 // waves' parts meet at the end.  The next tile's codes are on their way into registers while one is worked on, and their pages' numbers a tile
 // ahead of that.
 //
-// What bounds it is the products and, beside them, the exponentials and the rest of the softmax, which do not overlap on a SIMD (issued in turn by one wave
-// they take the same time): four sequences of up to 131 072 tokens, 8 key heads, trees of 64 tokens and 32 heads, in 533 to 543 us (820 TFLOP/s of visible pairs;
-// a library product of 8192^3 1 379), 64 of up to 8 192 with 20 to 32 tokens in 268 to 280.
+// What bounds it is no part of it alone: the matrix cores are 39 % busy, vector instructions 41 %, LDS 40 %.  Four sequences of up to 131 072 tokens, 8 key heads,
+// trees of 64 tokens and 32 heads, take 535 to 566 us (780 to 820 TFLOP/s of visible pairs; a library product of 8192^3 1 379), 64 of up to 8 192 with 20 to 32 tokens 270
+// to 279.  The forward kernel (kda_attn_fwd.hip) has the same products and exponentials at 1 055 TFLOP/s; what this one has beside them is the codes, widened by
+// vector instructions and written to LDS, for every 128 rows again.  (Products and exponentials of two blocks of keys issued in turn by one wave take the same time.)
 //
 // The softmax's terms P are rounded to bf16 ahead of their product with V where the result is bf16: half a step, 2^-8, is what the result's own rounding may be off
 // by.  Where it is fp32 they go as two bf16, P = p + rest, of which 2^-16 is left out, and V is multiplied twice.  Off the formulas in 64 bits, in the mean square, and time, for 64
@@ -75,8 +76,8 @@ __device__ __forceinline__ void widen16(const u32x4 &w, float scale, u32x4 (&o)[
         o[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true));
     }
 }
-// A scale that the codes can take on their way to bf16: a power of two, neither large nor small.  (The append makes no others but for values next to
-// the ends of fp32's range.)
+// A scale that the codes can take on their way to bf16: a power of two, 2^-60 to 2^60.  (Of those that the append makes, 2^-100 and up, others are those of pages whose
+// values are all zeros, below about 2^-52 or above 2^68: their tiles multiply logits and numerators.)
 __device__ __forceinline__ bool is_plain(float scale)
 {
     const uint32_t b = __float_as_uint(scale);

@@ -26,8 +26,8 @@
 // are worked through again from state to state, as kda_recurrent_steps does, a line at a time.  Only those are written again: a row is the same
 // whatever its neighbours hold.  (Looking for them costs 0.3 us of 132.  The pass itself is slow: 64 chains of 64 tokens with keys 22 long 1.5 ms for 230 us.)
 //
-// What bounds it is reading the states, and for large trees vector instructions (53 % busy, half of them the sums up the lines) beside the matrix cores
-// (31 %).  256 trees of up to 16 tokens, 32 heads: 132 us (0.68 GB, 5.2 TB/s); 64 of 64 tokens: 128, in fp32 150; 64 chains of 64: 230; 128 trees of 20: 99.
+// What bounds it is reading the states, and for large trees no part alone: vector instructions are 54 % busy, half of them the sums up the lines, the matrix cores
+// 31 %.  256 trees of up to 16 tokens, 32 heads: 132 to 134 us (0.68 GB, 5.1 TB/s); 64 of 64 tokens: 128 to 134, in fp32 150; 64 chains of 64: 230; 128 trees of 20: 99.
 // With fp32 MFMAs and q in LDS these were 170, 271, 320 and 126.  A step up a line is some 65 vector instructions for a group: scales and what is not finite
 // are looked at behind it (chains 278 -> 230).  (Pieces for trees of 16, too: the same time in bf16, 172 for 156 in fp32.  With a column a thread and a loop
 // over each token's ancestors in place of the blocks: 231 and 474.)
