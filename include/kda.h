@@ -604,7 +604,7 @@ kda_status kda_cache_keep(const kda_cache *cache, int32_t layers, const int32_t 
  *   flags          KDA_STEPS_SCALAR_GATE: log_alpha is [N,Tq,H]
  * All arithmetic is of fp32's precision (of states, and of keys and queries with a line's decays, below 2^-110: to 2^-126; sums over channels of two
  * tokens' vectors, with the scale, to 2^-126 ahead of the values that they weigh).  Where such sums or what they weigh leave fp32's range, the rows
- * concerned are formed from state to state: finite where kda_recurrent_steps along the token's line is, and in a time that grows with the lines.  What is not
+ * concerned are formed from state to state, as kda_recurrent_steps forms them along a line (but for the order of sums), and in a time that grows with the lines.  What is not
  * finite in a token, or becomes so on the way, reaches its own row and its descendants' alone.  o must not alias an input.  No workspace.
  */
 kda_status kda_tree_steps(const kda_dims *dims, const void *q, const void *k, const void *v, const void *log_alpha, const void *beta,
